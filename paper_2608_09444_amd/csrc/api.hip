@@ -195,10 +195,11 @@ struct Chunk {
 // x_ready: c.x already holds the first layer's input (the loop step's gather
 // wrote it), so its residual + norm is skipped.  pending_out: the last down
 // projection's partials are left for the caller (the loop step's exit kernel
-// adds them) instead of a closing residual kernel; not with norm_out.
+// adds them) instead of a closing residual kernel; not with norm_out.  tree: the
+// rows are drafted tokens, which attend by its bases and masks.
 static cdb_status run_layers(const Ctx& c, int first, int count, KvTarget kv, const cdb_rows& r, bool norm_out,
                              hipStream_t st, const Chunk* chunk = nullptr, int pending_in = 0, bool x_ready = false,
-                             int* pending_out = nullptr) {
+                             int* pending_out = nullptr, const cdb_tree* tree = nullptr) {
     const cdb_model_desc& d = *c.md;
     const int M = r.n_rows;
     const int32_t* dn = r.d_n_rows;  // device row count (M is then the capacity)
@@ -228,6 +229,8 @@ static cdb_status run_layers(const Ctx& c, int first, int count, KvTarget kv, co
         if (chunk)
             HIPCHK(launch_prefill_attention(c.q, kv, chunk->seq, chunk->pos0, M, d.n_heads, d.head_dim, c.x, c.err,
                                             st));
+        else if (tree)
+            HIPCHK(launch_tree_attention(c.q, kv, r.seq, *tree, M, d.n_heads, d.head_dim, c.x, c.err, st, dn));
         else
             HIPCHK(launch_attention(c.q, kv, r.seq, r.pos, c.order, M, d.n_heads, d.head_dim, c.x, c.err, st, dn,
                                     c.asplit.arrive ? &c.asplit : nullptr));
@@ -285,6 +288,21 @@ static cdb_status check_common(const cdb_model* model, const cdb_kv* kv, const c
         const int np = stage == 0 ? kv->pre_pages : (stage == 1 ? kv->core_pages : kv->coda_pages);
         if (!pool || np < 0 || !kv->page_table) return CDB_ERR_INVALID_ARG;
     }
+    return CDB_OK;
+}
+
+// Positions of a page table in 32 bits, with room for a tree behind the last one.
+constexpr int kMaxTablePages = (0x7fffffff - CDB_TREE_MAX_NODES) / kPage;
+
+// tree: NULL for the plain stage calls
+static cdb_status check_tree(const cdb_model* model, const cdb_kv* kv, const cdb_rows* rows, const cdb_tree* tree,
+                             size_t ws_bytes) {
+    if (!tree) return CDB_OK;
+    if (tree->max_nodes < 1 || tree->max_nodes > CDB_TREE_MAX_NODES) return CDB_ERR_INVALID_ARG;
+    if (rows->n_rows > 0 && (!tree->base || !tree->mask || !tree->rope_pos)) return CDB_ERR_INVALID_ARG;
+    if (kv->max_pages > kMaxTablePages) return CDB_ERR_CAPACITY;
+    const size_t own = ws_layout(model->desc, rows->n_rows, false).total;
+    if (ws_bytes < own + tree_scratch_bytes(model->desc, rows->n_rows)) return CDB_ERR_CAPACITY;
     return CDB_OK;
 }
 
@@ -353,9 +371,10 @@ cdb_status cdb_workspace_init(void* ws, size_t ws_bytes, hipStream_t st) {
     return CDB_OK;
 }
 
-cdb_status cdb_boundary_prelude(const cdb_model* model, const cdb_kv* kv, const cdb_state* state, const cdb_rows* rows,
-                                const int32_t* tokens, void* ws, size_t ws_bytes, hipStream_t st) {
+static cdb_status prelude(const cdb_model* model, const cdb_kv* kv, const cdb_state* state, const cdb_rows* rows,
+                          const cdb_tree* tree, const int32_t* tokens, void* ws, size_t ws_bytes, hipStream_t st) {
     cdb_status s = check_common(model, kv, state, rows, ws, ws_bytes, 0);
+    if (s == CDB_OK) s = check_tree(model, kv, rows, tree, ws_bytes);
     if (s != CDB_OK) return s;
     const cdb_model_desc& d = model->desc;
     if (rows->n_rows > 0 && !tokens) return CDB_ERR_INVALID_ARG;
@@ -364,19 +383,25 @@ cdb_status cdb_boundary_prelude(const cdb_model* model, const cdb_kv* kv, const 
     Ctx c = make_ctx(model, ws, rows->n_rows);
     const KvTarget t = stage_target(d, *kv, 0);
     HIPCHK(launch_embed(d, wptr(c, c.wl.embed), tokens, *rows, *kv, t, state->n_slots, c.h, c.rope, c.kvpid, c.order,
-                        c.asplit.arrive, c.err, st));
-    s = run_layers(c, 0, d.n_prelude, t, *rows, false, st);
+                        c.asplit.arrive, c.err, st, tree ? tree->rope_pos : nullptr));
+    s = run_layers(c, 0, d.n_prelude, t, *rows, false, st, nullptr, 0, false, nullptr, tree);
     if (s != CDB_OK) return s;
     HIPCHK(launch_store_state(rows->n_rows, d.d, state->n_slots, rows->slot, c.h, state->h,
                               d.injection ? state->e : nullptr, st, rows->d_n_rows));
     return CDB_OK;
 }
 
+cdb_status cdb_boundary_prelude(const cdb_model* model, const cdb_kv* kv, const cdb_state* state, const cdb_rows* rows,
+                                const int32_t* tokens, void* ws, size_t ws_bytes, hipStream_t st) {
+    return prelude(model, kv, state, rows, nullptr, tokens, ws, ws_bytes, st);
+}
+
 // err: where device errors go (NULL: the workspace's own error word)
 static cdb_status loop_step(const cdb_model* model, const cdb_kv* kv, const cdb_state* state, const cdb_rows* rows,
                             const cdb_gate* gate, const cdb_step_out* out, void* ws, size_t ws_bytes, hipStream_t st,
-                            int* err = nullptr) {
+                            int* err = nullptr, const cdb_tree* tree = nullptr) {
     cdb_status s = check_common(model, kv, state, rows, ws, ws_bytes, 1);
+    if (s == CDB_OK) s = check_tree(model, kv, rows, tree, ws_bytes);
     if (s != CDB_OK) return s;
     const cdb_model_desc& d = model->desc;
     if (!out || !out->exit_score || !out->exit_mask || !out->cont || !out->exited || !out->counts)
@@ -395,7 +420,8 @@ static cdb_status loop_step(const cdb_model* model, const cdb_kv* kv, const cdb_
         // the gather also writes the first core layer's input (the adapter's
         // input for injection models)
         HIPCHK(launch_gather(d, *state, r, *kv, t, c.h, c.h_in, d.injection ? c.x : nullptr, c.rope, c.kvpid, c.order,
-                             c.asplit.arrive, d.injection ? nullptr : c.x, c.err, st));
+                             c.asplit.arrive, d.injection ? nullptr : c.x, c.err, st,
+                             tree ? tree->rope_pos : nullptr));
         // injection models: the gather zeroed h; the adapter's split-K
         // partials become the first layer's input in its residual + norm
         if (d.injection) {
@@ -406,7 +432,7 @@ static cdb_status loop_step(const cdb_model* model, const cdb_kv* kv, const cdb_
         }
         int pending = 0;
         s = run_layers(c, d.n_prelude, d.n_core, t, r, false, st, nullptr, d.injection ? c.gm.adapter_part.S : 0,
-                       !d.injection, &pending);
+                       !d.injection, &pending, tree);
         if (s != CDB_OK) return s;
         // the exit kernel adds the last down projection's partials to h first
         HIPCHK(launch_exit(d, r, c.h, c.part, pending, c.h_in, wptr(c, c.wl.w_exit), state->h, state->n_slots, *out,
@@ -476,9 +502,11 @@ cdb_status cdb_loop_step_noalloc(const cdb_model* model, const cdb_kv* kv, const
     return loop_step(model, kv, state, rows, nullptr, out, ws, kNoAllocScratchBytes, st, d_error);
 }
 
-cdb_status cdb_boundary_coda(const cdb_model* model, const cdb_kv* kv, const cdb_state* state, const cdb_rows* rows,
-                             float* logits, int32_t* next_ids, void* ws, size_t ws_bytes, hipStream_t st) {
+static cdb_status coda(const cdb_model* model, const cdb_kv* kv, const cdb_state* state, const cdb_rows* rows,
+                       const cdb_tree* tree, float* logits, int32_t* next_ids, void* ws, size_t ws_bytes,
+                       hipStream_t st) {
     cdb_status s = check_common(model, kv, state, rows, ws, ws_bytes, 2);
+    if (s == CDB_OK) s = check_tree(model, kv, rows, tree, ws_bytes);
     if (s != CDB_OK) return s;
     const cdb_model_desc& d = model->desc;
     if (!logits || !next_ids) return CDB_ERR_INVALID_ARG;
@@ -487,8 +515,8 @@ cdb_status cdb_boundary_coda(const cdb_model* model, const cdb_kv* kv, const cdb
     Ctx c = make_ctx(model, ws, M);
     const KvTarget t = stage_target(d, *kv, 2);
     HIPCHK(launch_load_state(d, M, rows->slot, rows->seq, rows->pos, t, state->h, state->n_slots, c.h, c.rope, c.kvpid,
-                             c.order, c.asplit.arrive, c.err, st, rows->d_n_rows));
-    s = run_layers(c, d.n_prelude + d.n_core, d.n_coda, t, *rows, true, st);
+                             c.order, c.asplit.arrive, c.err, st, rows->d_n_rows, tree ? tree->rope_pos : nullptr));
+    s = run_layers(c, d.n_prelude + d.n_core, d.n_coda, t, *rows, true, st, nullptr, 0, false, nullptr, tree);
     if (s != CDB_OK) return s;
     EpiArgs ea{};
     ea.ld_out = d.vocab;
@@ -497,6 +525,11 @@ cdb_status cdb_boundary_coda(const cdb_model* model, const cdb_kv* kv, const cdb
     HIPCHK(launch_gemm(EPI_STORE, c.x, wptr(c, c.wl.lm_head), M, c.gm.lm, c.part, ea, st, rows->d_n_rows));
     HIPCHK(launch_argmax(M, d.vocab, logits, next_ids, st, rows->d_n_rows));
     return CDB_OK;
+}
+
+cdb_status cdb_boundary_coda(const cdb_model* model, const cdb_kv* kv, const cdb_state* state, const cdb_rows* rows,
+                             float* logits, int32_t* next_ids, void* ws, size_t ws_bytes, hipStream_t st) {
+    return coda(model, kv, state, rows, nullptr, logits, next_ids, ws, ws_bytes, st);
 }
 
 cdb_status cdb_prefill(const cdb_model* model, const cdb_kv* kv, int32_t seq, int32_t pos0, int32_t n_rows,
@@ -566,9 +599,10 @@ cdb_status cdb_prefill(const cdb_model* model, const cdb_kv* kv, int32_t seq, in
     return CDB_OK;
 }
 
-cdb_status cdb_paged_attention(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_rows* rows, int32_t stage,
-                               int32_t layer, const float* q, const int32_t* order, void* out, void* ws,
-                               size_t ws_bytes, hipStream_t st) {
+// What both attention calls of one layer check; *t: that layer's cache.
+static cdb_status check_attention(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_rows* rows, int32_t stage,
+                                  int32_t layer, const float* q, const void* out, const void* ws, size_t ws_bytes,
+                                  size_t need, KvTarget* t) {
     if (!desc || !kv || !rows || !q || !out || !ws) return CDB_ERR_INVALID_ARG;
     const cdb_model_desc& d = *desc;
     if (!desc_supported(d)) return CDB_ERR_UNSUPPORTED;
@@ -576,13 +610,24 @@ cdb_status cdb_paged_attention(const cdb_model_desc* desc, const cdb_kv* kv, con
     const int layers = stage == 0 ? d.n_prelude : (stage == 1 ? d.n_core : d.n_coda);
     if (layer < 0 || layer >= layers) return CDB_ERR_INVALID_ARG;
     if (rows->n_rows > kMaxRows) return CDB_ERR_CAPACITY;
-    if (ws_bytes < 256 + (size_t)kMaxRows * 4) return CDB_ERR_CAPACITY;
+    if (ws_bytes < need) return CDB_ERR_CAPACITY;
     if (rows->n_rows == 0) return CDB_OK;
     if (!rows->seq || !rows->pos || (stage == 1 && !rows->c) || !kv->page_table) return CDB_ERR_INVALID_ARG;
-    KvTarget t = stage_target(d, *kv, stage);
-    if (!t.pool) return CDB_ERR_INVALID_ARG;
-    t.layer = layer;
-    if (stage == 1) t.c_row = rows->c;
+    *t = stage_target(d, *kv, stage);
+    if (!t->pool) return CDB_ERR_INVALID_ARG;
+    t->layer = layer;
+    if (stage == 1) t->c_row = rows->c;
+    return CDB_OK;
+}
+
+cdb_status cdb_paged_attention(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_rows* rows, int32_t stage,
+                               int32_t layer, const float* q, const int32_t* order, void* out, void* ws,
+                               size_t ws_bytes, hipStream_t st) {
+    KvTarget t{};
+    const cdb_status s = check_attention(desc, kv, rows, stage, layer, q, out, ws, ws_bytes,
+                                         256 + (size_t)kMaxRows * 4, &t);
+    if (s != CDB_OK || rows->n_rows == 0) return s;
+    const cdb_model_desc& d = *desc;
     if (!order) {
         int32_t* own = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(ws) + 256);
         HIPCHK(launch_row_order(rows->pos, rows->n_rows, own, st, rows->d_n_rows));
@@ -590,6 +635,136 @@ cdb_status cdb_paged_attention(const cdb_model_desc* desc, const cdb_kv* kv, con
     }
     HIPCHK(launch_attention(q, t, rows->seq, rows->pos, order, rows->n_rows, d.n_heads, d.head_dim,
                             static_cast<uint16_t*>(out), static_cast<int*>(ws), st, rows->d_n_rows));
+    return CDB_OK;
+}
+
+// ---------------------------------------------------------------- drafted trees
+
+size_t cdb_tree_workspace_bytes(const cdb_model_desc* desc, int32_t max_rows, int32_t max_seqs) {
+    if (!desc || !desc_supported(*desc) || max_rows < 0 || max_rows > kMaxRows || max_seqs < 0) return 0;
+    // the stage layouts are not monotonic in the row count, the scratch behind them is
+    const size_t own = cdb_workspace_bytes(desc, max_rows);
+    return std::max(own + tree_scratch_bytes(*desc, max_rows), 256 + map_scratch_bytes(max_seqs));
+}
+
+cdb_status cdb_map_pages(const cdb_model_desc* desc, int32_t* page_table, int32_t max_seqs, int32_t max_pages,
+                         const cdb_page_pool* pre, const cdb_page_pool* core, const cdb_page_pool* coda,
+                         int32_t kv_layout, const int32_t* len, int32_t* mapped, void* ws, size_t ws_bytes,
+                         hipStream_t st) {
+    if (!desc || !ws || max_seqs < 0 || max_pages < 0 || kv_layout < 0 || kv_layout > 2) return CDB_ERR_INVALID_ARG;
+    const cdb_model_desc& d = *desc;
+    if (!desc_supported(d)) return CDB_ERR_UNSUPPORTED;
+    if (max_seqs > 0 && (!page_table || !len || !mapped)) return CDB_ERR_INVALID_ARG;
+    const int layers[3] = {d.n_prelude, d.n_core, d.n_coda};
+    const cdb_page_pool* pools[3] = {pre, core, coda};
+    for (int k = 0; k < 3; ++k)
+        if (layers[k] && (!pools[k] || !pools[k]->free_ids || !pools[k]->free_count || pools[k]->capacity < 0))
+            return CDB_ERR_INVALID_ARG;
+    // page and stack counts are summed in 32 bits
+    if (max_pages > kMaxTablePages || (int64_t)max_seqs * max_pages * d.r_max > 0x3fffffff) return CDB_ERR_CAPACITY;
+    if (ws_bytes < 256 + map_scratch_bytes(max_seqs)) return CDB_ERR_CAPACITY;
+    const int width = kv_layout == 0 ? d.r_max : (kv_layout == 1 || d.r_max == 1) ? 1 : 2;
+    HIPCHK(launch_map_pages(d, page_table, max_seqs, max_pages, pools, width, len, mapped,
+                            reinterpret_cast<int32_t*>(static_cast<unsigned char*>(ws) + 256), static_cast<int*>(ws), st));
+    return CDB_OK;
+}
+
+// seqs, nodes: whether the call reads the trees' sequences, and their nodes
+static cdb_status check_drafts(const cdb_drafts* d, bool seqs, bool nodes) {
+    if (!d || d->n_trees < 0 || d->max_nodes < 1 || d->max_nodes > CDB_TREE_MAX_NODES || d->max_seqs < 0)
+        return CDB_ERR_INVALID_ARG;
+    if (d->n_trees > CDB_TREE_MAX_TREES) return CDB_ERR_CAPACITY;
+    if (d->n_trees > 0 && ((seqs && (!d->seq || !d->len)) || (nodes && (!d->n_nodes || !d->parent || !d->tokens))))
+        return CDB_ERR_INVALID_ARG;
+    return CDB_OK;
+}
+
+cdb_status cdb_tree_rows(const cdb_drafts* drafts, const cdb_row_map* out, void* ws, size_t ws_bytes, hipStream_t st) {
+    const cdb_status s = check_drafts(drafts, true, true);
+    if (s != CDB_OK) return s;
+    if (!out || !ws || !out->n_rows || out->capacity < 0) return CDB_ERR_INVALID_ARG;
+    if (drafts->n_trees > 0 && !out->row0) return CDB_ERR_INVALID_ARG;
+    if (out->capacity > 0 && (!out->seq || !out->pos || !out->base || !out->rope_pos || !out->tokens || !out->mask))
+        return CDB_ERR_INVALID_ARG;
+    if (ws_bytes < 256) return CDB_ERR_CAPACITY;
+    HIPCHK(launch_tree_rows(*drafts, *out, static_cast<int*>(ws), st));
+    return CDB_OK;
+}
+
+cdb_status cdb_tree_attention(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_rows* rows,
+                              const cdb_tree* tree, int32_t stage, int32_t layer, const float* q, void* out, void* ws,
+                              size_t ws_bytes, hipStream_t st) {
+    if (!desc || !rows || !tree) return CDB_ERR_INVALID_ARG;
+    if (tree->max_nodes < 1 || tree->max_nodes > CDB_TREE_MAX_NODES) return CDB_ERR_INVALID_ARG;
+    if (!desc_supported(*desc)) return CDB_ERR_UNSUPPORTED;
+    if (rows->n_rows < 0) return CDB_ERR_INVALID_ARG;
+    if (rows->n_rows > kMaxRows) return CDB_ERR_CAPACITY;
+    KvTarget t{};
+    const cdb_status s = check_attention(desc, kv, rows, stage, layer, q, out, ws, ws_bytes,
+                                         256 + tree_scratch_bytes(*desc, rows->n_rows), &t);
+    if (s != CDB_OK || rows->n_rows == 0) return s;
+    if (!tree->base || !tree->mask || kv->max_seqs < 0 || kv->max_pages < 0) return CDB_ERR_INVALID_ARG;
+    if (kv->max_pages > kMaxTablePages) return CDB_ERR_CAPACITY;
+    HIPCHK(launch_tree_attention(q, t, rows->seq, *tree, rows->n_rows, desc->n_heads, desc->head_dim,
+                                 static_cast<uint16_t*>(out), static_cast<int*>(ws), st, rows->d_n_rows));
+    return CDB_OK;
+}
+
+cdb_status cdb_tree_prelude(const cdb_model* model, const cdb_kv* kv, const cdb_state* state, const cdb_rows* rows,
+                            const cdb_tree* tree, const int32_t* tokens, void* ws, size_t ws_bytes, hipStream_t st) {
+    if (!tree) return CDB_ERR_INVALID_ARG;
+    return prelude(model, kv, state, rows, tree, tokens, ws, ws_bytes, st);
+}
+
+cdb_status cdb_tree_step(const cdb_model* model, const cdb_kv* kv, const cdb_state* state, const cdb_rows* rows,
+                         const cdb_tree* tree, const cdb_gate* gate, const cdb_step_out* out, void* ws,
+                         size_t ws_bytes, hipStream_t st) {
+    if (!tree) return CDB_ERR_INVALID_ARG;
+    return loop_step(model, kv, state, rows, gate, out, ws, ws_bytes, st, nullptr, tree);
+}
+
+cdb_status cdb_tree_coda(const cdb_model* model, const cdb_kv* kv, const cdb_state* state, const cdb_rows* rows,
+                         const cdb_tree* tree, float* logits, int32_t* next_ids, void* ws, size_t ws_bytes,
+                         hipStream_t st) {
+    if (!tree) return CDB_ERR_INVALID_ARG;
+    return coda(model, kv, state, rows, tree, logits, next_ids, ws, ws_bytes, st);
+}
+
+cdb_status cdb_tree_accept(const cdb_drafts* drafts, const int32_t* row0, const int32_t* next_ids, int32_t n_rows,
+                           const int32_t* first_ids, const cdb_accepted* out, void* ws, size_t ws_bytes,
+                           hipStream_t st) {
+    const cdb_status s = check_drafts(drafts, false, true);
+    if (s != CDB_OK) return s;
+    if (!out || !ws || n_rows < 0) return CDB_ERR_INVALID_ARG;
+    if (ws_bytes < 256) return CDB_ERR_CAPACITY;
+    if (drafts->n_trees == 0) return CDB_OK;
+    if (!row0 || !first_ids || (n_rows > 0 && !next_ids) || !out->path || !out->count || !out->next)
+        return CDB_ERR_INVALID_ARG;
+    HIPCHK(launch_tree_accept(*drafts, row0, next_ids, n_rows, first_ids, *out, static_cast<int*>(ws), st));
+    return CDB_OK;
+}
+
+cdb_status cdb_tree_commit(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_drafts* drafts,
+                           const cdb_accepted* accepted, void* ws, size_t ws_bytes, hipStream_t st) {
+    if (!desc || !kv || !accepted || !ws) return CDB_ERR_INVALID_ARG;
+    const cdb_model_desc& d = *desc;
+    if (!desc_supported(d)) return CDB_ERR_UNSUPPORTED;
+    const cdb_status s = check_drafts(drafts, true, false);
+    if (s != CDB_OK) return s;
+    if (kv->max_seqs < 0 || kv->max_pages < 0) return CDB_ERR_INVALID_ARG;
+    if (kv->max_pages > kMaxTablePages) return CDB_ERR_CAPACITY;
+    if (ws_bytes < 256) return CDB_ERR_CAPACITY;
+    if (drafts->n_trees == 0) return CDB_OK;
+    if (!accepted->path || !accepted->count || !kv->page_table) return CDB_ERR_INVALID_ARG;
+    for (int stage = 0; stage < 3; ++stage) {
+        const KvTarget t = stage_target(d, *kv, stage);
+        if (t.n_layers > 0 && (!t.pool || t.n_pages < 0)) return CDB_ERR_INVALID_ARG;
+    }
+    for (int stage = 0; stage < 3; ++stage) {
+        const KvTarget t = stage_target(d, *kv, stage);
+        HIPCHK(launch_tree_commit(d, t, stage == 1 ? 1 : t.plane_fixed, stage == 1 ? d.r_max : 1, *drafts, *accepted,
+                                  static_cast<int*>(ws), st));
+    }
     return CDB_OK;
 }
 

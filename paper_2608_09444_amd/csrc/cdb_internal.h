@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "../../include/libcdb.h"
+#include "../../include/libcdb_tree.h"
 
 namespace cdb {
 
@@ -185,19 +186,21 @@ hipError_t launch_resid_norm(float* h, const float* part, int S, int M, int d, f
 // `order` is non-null (at most kMaxRows rows), and clear the rows' arrival
 // counters of the split attention when `arrive` is.  The gather writes either
 // the adapter input xcat = [h; e] or, with xn set, the first core layer's input
-// xn = bf16(RMSNorm(h)), both in fragment layout.
+// xn = bf16(RMSNorm(h)), both in fragment layout.  rpos: the rows' RoPE positions
+// where they are not pos (drafted trees).
 hipError_t launch_gather(const cdb_model_desc& md, const cdb_state& s, const cdb_rows& r, const cdb_kv& kv,
                          const KvTarget& kt, float* h, float* h_in, uint16_t* xcat, float2* rope, int32_t* kvpid,
-                         int32_t* order, int* arrive, uint16_t* xn, int* err, hipStream_t st);
+                         int32_t* order, int* arrive, uint16_t* xn, int* err, hipStream_t st,
+                         const int32_t* rpos = nullptr);
 hipError_t launch_embed(const cdb_model_desc& md, const uint16_t* embed, const int32_t* tokens, const cdb_rows& r,
                         const cdb_kv& kv, const KvTarget& kt, int n_slots, float* h, float2* rope, int32_t* kvpid,
-                        int32_t* order, int* arrive, int* err, hipStream_t st);
+                        int32_t* order, int* arrive, int* err, hipStream_t st, const int32_t* rpos = nullptr);
 hipError_t launch_store_state(int M, int d, int n_slots, const int32_t* slot, const float* h, float* state_h,
                               float* state_e, hipStream_t st, const int32_t* dn = nullptr);
 hipError_t launch_load_state(const cdb_model_desc& md, int M, const int32_t* slot, const int32_t* seq,
                              const int32_t* pos, const KvTarget& kt, const float* state_h, int n_slots, float* h,
                              float2* rope, int32_t* kvpid, int32_t* order, int* arrive, int* err, hipStream_t st,
-                             const int32_t* dn = nullptr);
+                             const int32_t* dn = nullptr, const int32_t* rpos = nullptr);
 // h += the S split-K partials in part (split order) first; gate: NULL replays
 // rows.depth; deff[M] receives each exiting row's depth.
 hipError_t launch_exit(const cdb_model_desc& md, const cdb_rows& r, float* h, const float* part, int S,
@@ -221,6 +224,26 @@ hipError_t launch_pack(int kind, const uint16_t* a, const uint16_t* b, const uin
                        uint16_t* dst, hipStream_t st);
 hipError_t launch_copy_bf16(const uint16_t* src, size_t n, uint16_t* dst, hipStream_t st);
 hipError_t launch_ws_init(int* err, hipStream_t st);
+
+// ---------------------------------------------------------------- drafted trees
+// bytes of the tree attention's scratch behind a stage call's workspace (or its
+// first 256 bytes), and of cdb_map_pages' behind the first 256
+size_t tree_scratch_bytes(const cdb_model_desc& d, int rows);
+inline size_t map_scratch_bytes(int max_seqs) { return (4 + (size_t)max_seqs) * 4; }
+// attention of drafted rows (base, mask as in cdb_tree)
+hipError_t launch_tree_attention(const float* q, const KvTarget& kv, const int32_t* seq, const cdb_tree& tree, int M,
+                                 int H, int hd, uint16_t* out, int* err, hipStream_t st, const int32_t* dn);
+// pools: prelude, core, coda; core_width: distinct core pages per token page;
+// scratch: 4 + S ints
+hipError_t launch_map_pages(const cdb_model_desc& md, int32_t* table, int S, int P, const cdb_page_pool* const* pools,
+                            int core_width, const int32_t* len, int32_t* mapped, int32_t* scratch, int* err,
+                            hipStream_t st);
+hipError_t launch_tree_rows(const cdb_drafts& d, const cdb_row_map& out, int* err, hipStream_t st);
+hipError_t launch_tree_accept(const cdb_drafts& d, const int32_t* row0, const int32_t* next_ids, int n_rows,
+                              const int32_t* first_ids, const cdb_accepted& out, int* err, hipStream_t st);
+// one stage: planes plane0 .. plane0 + n_planes - 1 of kv's pool
+hipError_t launch_tree_commit(const cdb_model_desc& md, const KvTarget& kv, int plane0, int n_planes,
+                              const cdb_drafts& d, const cdb_accepted& acc, int* err, hipStream_t st);
 
 enum PackKind : int { PACK_PLAIN = 0, PACK_QKV = 1, PACK_GU = 2 };
 
