@@ -1,91 +1,647 @@
 // Attention of drafted token trees over the paged, depth-indexed KV cache: row i
 // attends to positions 0..base-1 of its sequence and to the positions base + j
 // whose bit j of its mask is set (its ancestors and itself), in its own plane.
+//
+// The rows of one tree share their context, so its K and V are read once for up
+// to 16, 32 or 64 of them and multiplied on MFMA (v_mfma_f32_16x16x32_bf16); with
+// so few rows per byte the kernel is bound by HBM.
+//
+// k_tree_plan (one workgroup, once per stage call) cuts the rows into tiles:
+// adjacent rows of one sequence, plane and base, at most 16 NT of them.  A tile's
+// context is cut into segments (tree_segment_pages, by its base alone), and a
+// work item is one segment of one tile, for each head.
+//
+// k_tree_attn: a workgroup takes items in turn; its 4 waves deal the segment's
+// pages among them in pairs (32 keys), and each keeps an online softmax of its
+// own for the tile's rows.  Per pair:
+//   S^T = K Q^T: A = the K rows as loaded from the cache (lane = key, 16 bytes of
+//     it), B = q, split into bf16 hi + lo parts (about 16 bits of it).  A lane then
+//     holds one row's scores at 4 keys of either page.
+//   online softmax per row in the exp2 domain; the running maximum goes over the
+//     four lanes of a row (two lane swaps), the sum stays apart until the end.
+//   O^T += V^T P^T: B = P, hi + lo again, and already where the scores left it:
+//     the order of the 32 keys in the product is free, so lane group g takes keys
+//     4g..4g+3 of both pages.  A = V^T, read from the key-major rows in LDS with
+//     the transposing read (ds_read_b64_tr_b16).
+// The pair after the current one is in flight in registers meanwhile.  The waves'
+// states are merged through LDS; several segments' through memory, by the
+// workgroup that arrives last, in segment order.
+//
+// Masks: only pages that reach past base take the masked path.  There a score that
+// a row does not see becomes -inf (p = 0), and V of keys that no row of the tile
+// sees is cleared; a V that is not finite at a key that some rows see is taken out
+// of the product, which would multiply it by the others' zeros, and added to those
+// rows alone.
+//
+// Nothing in a row's arithmetic depends on the other rows: not its tile, not the
+// segments, not the wave that takes a page.
+#include <algorithm>
+
 #include "cdb_internal.h"
 
 namespace cdb {
 
-// One wave per (row, head), 64 positions at a time: lane = position for the
-// scores, lane = dim for the weighted sum of V.
-template <int HD>
-__global__ __launch_bounds__(64) void k_tree_attn(const float* __restrict__ q, KvTarget kv,
-                                                  const int32_t* __restrict__ seq, cdb_tree tree, int M, int H,
-                                                  uint16_t* __restrict__ out, int* err,
-                                                  const int32_t* __restrict__ dn) {
-    __shared__ float s_q[HD];
-    const int head = blockIdx.x, m = blockIdx.y, lane = threadIdx.x;
-    const int d = H * HD;
-    if (m >= live_rows(dn, M)) return;
-    const float qscale = 1.4426950408889634f / sqrtf((float)HD);
-    for (int k = lane; k < HD; k += 64) s_q[k] = q[(size_t)m * d + head * HD + k] * qscale;
-    __syncthreads();
-    const int sq = seq[m], base = tree.base[m];
-    const uint64_t mask = tree.mask[m];
-    const int plane = kv.c_row ? kv.c_row[m] + 1 : kv.plane_fixed;
-    const bool plane_ok = kv.c_row ? (plane >= 1 && plane <= kv.n_planes - 2) : (plane >= 0 && plane < kv.n_planes);
-    const int cap = kv.max_pages * kPage;
-    const int last = base + (mask ? 63 - __clzll((long long)mask) : -1);
-    if (sq < 0 || sq >= kv.max_seqs || !plane_ok || base < 0 || base > cap || last >= cap) {
-        if (lane == 0) set_err(err, CDB_DEV_UNMAPPED_PAGE);
-        return;
-    }
-    const int32_t* pt = kv.page_table + ((size_t)sq * kv.n_planes + plane) * kv.max_pages;
-    float mx = -1e30f, l = 0.f, acc[2] = {0.f, 0.f};
-    for (int p0 = 0; p0 <= last; p0 += 64) {
-        const int p = p0 + lane;
-        bool see = p <= last && (p < base || (mask >> (p - base) & 1));
-        const uint16_t* row = nullptr;
-        float s = -1e30f;
-        if (p <= last) {
-            const int pid = pt[p / kPage];
-            if (pid < 0 || pid >= kv.n_pages) {
-                set_err(err, CDB_DEV_UNMAPPED_PAGE);
-                see = false;
-            }
-            if (see) {
-                row = kv.pool + kv_offset(kv.layer, pid, kv.n_pages, 0, head, H, p % kPage, HD);
-                s = 0.f;
-                for (int k = 0; k < HD; ++k) s = fmaf(s_q[k], bf2f(row[k]), s);
-            }
-        }
-        float mn = s;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) mn = fmaxf(mn, __shfl_xor(mn, o, 64));
-        mn = fmaxf(mn, mx);
-        const float corr = exp2f(mx - mn), w = see ? exp2f(s - mn) : 0.f;
-        mx = mn;
-        l = l * corr + w;
-        acc[0] *= corr;
-        acc[1] *= corr;
-        const size_t vofs = (size_t)H * kPage * HD;
-        for (int j = 0; j < 64; ++j) {
-            const float wj = __shfl(w, j, 64);
-            const uint64_t rj = (uint64_t)__shfl((int)((uint64_t)row >> 32), j, 64) << 32 |
-                                (uint32_t)__shfl((int)(uint64_t)row, j, 64);
-            const uint16_t* vr = reinterpret_cast<const uint16_t*>(rj);
-            if (!vr) continue;
-            acc[0] = fmaf(wj, bf2f(vr[vofs + lane]), acc[0]);
-            if (lane + 64 < HD) acc[1] = fmaf(wj, bf2f(vr[vofs + lane + 64]), acc[1]);
-        }
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-        if (lane + 64 * u < HD)
-            out[frag_index(m, head * HD + lane + 64 * u, d)] = f2bf(l != 0.f ? acc[u] / l : 0.f);
+constexpr int kTreeWaves = 4;
+constexpr int kTreeSegs = 16;  // most segments of a context
+
+// Pages per segment of a context whose last committed position is on page npg - 1.
+__host__ __device__ __forceinline__ int tree_segment_pages(int npg) {
+    const int p = (npg + 8 * kTreeSegs - 1) / (8 * kTreeSegs) * 8;
+    return p < 32 ? 32 : p;
 }
 
-size_t tree_scratch_bytes(const cdb_model_desc&, int) { return 0; }
+struct TreeItem {
+    uint64_t seen;       // mask bits of any row of the tile
+    int row0, n;         // the tile's rows
+    int base;
+    int seq, plane;
+    int p0, p1;          // the segment's pages
+    int seg, nseg, tile;
+    int pad[4];
+};
 
-hipError_t launch_tree_attention(const float* q, const KvTarget& kv, const int32_t* seq, const cdb_tree& tree, int M,
-                                 int H, int hd, uint16_t* out, int* err, hipStream_t st, const int32_t* dn) {
+struct TreeScratch {
+    int* n_items;
+    TreeItem* items;  // [rows][kTreeSegs]
+    int* arrive;      // [rows][H], zero between launches
+    float* part;      // [rows][H][kTreeSegs][hd + 2]: sums, maximum, weight
+    size_t bytes;
+};
+static TreeScratch tree_scratch(void* at, int H, int hd, int rows) {
+    auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    unsigned char* p = static_cast<unsigned char*>(at);
+    size_t off = 256;
+    TreeScratch t{};
+    t.n_items = reinterpret_cast<int*>(p);
+    t.items = reinterpret_cast<TreeItem*>(p + off);
+    off = up(off + (size_t)rows * kTreeSegs * sizeof(TreeItem));
+    t.arrive = reinterpret_cast<int*>(p + off);
+    off = up(off + (size_t)rows * H * 4);
+    t.part = reinterpret_cast<float*>(p + off);
+    off = up(off + (size_t)rows * H * kTreeSegs * (hd + 2) * 4);
+    t.bytes = off;
+    return t;
+}
+size_t tree_scratch_bytes(const cdb_model_desc& d, int rows) {
+    return rows > 0 ? tree_scratch(nullptr, d.n_heads, d.head_dim, rows).bytes : 0;
+}
+
+// ------------------------------------------------------------------ plan
+// Thread = row.  cap = rows per tile.
+__global__ __launch_bounds__(256) void k_tree_plan(KvTarget kv, const int32_t* __restrict__ seq, cdb_tree tree, int M,
+                                                   int H, int cap, TreeScratch ts, int* err,
+                                                   const int32_t* __restrict__ dn) {
+    __shared__ int s_seq[256], s_plane[256], s_base[256];
+    __shared__ uint64_t s_mask[256];
+    __shared__ uint64_t s_run[4], s_tile[4], s_end[4];  // by row: a run starts; a tile starts; a tile or a skipped row starts
+    __shared__ int s_sum[4];
+    const int i = threadIdx.x, lane = i & 63, w = i >> 6;
+    const int n = live_rows(dn, M);
+    const int limit = kv.max_pages * kPage;
+    int sq = -1, plane = -1, base = 0;
+    uint64_t mask = 0;
+    bool ok = false;
+    if (i < n) {
+        sq = seq[i];
+        base = tree.base[i];
+        mask = tree.mask[i];
+        plane = kv.c_row ? kv.c_row[i] + 1 : kv.plane_fixed;
+        ok = sq >= 0 && sq < kv.max_seqs && base >= 0 && base <= limit &&
+             (kv.c_row ? plane >= 1 && plane <= kv.n_planes - 2 : plane >= 0 && plane < kv.n_planes);
+        ok = ok && (!mask || base + 63 - __clzll((long long)mask) < limit);
+        if (!ok) set_err(err, CDB_DEV_UNMAPPED_PAGE);
+    }
+    s_seq[i] = ok ? sq : -1;
+    s_plane[i] = plane;
+    s_base[i] = base;
+    s_mask[i] = mask;
+    __syncthreads();
+    const bool run = ok && !(i > 0 && s_seq[i - 1] == sq && s_plane[i - 1] == plane && s_base[i - 1] == base);
+    const uint64_t runs = __ballot(run);
+    if (lane == 0) s_run[w] = runs;
+    __syncthreads();
+    // the row at which i's run started
+    int start = i;
+    {
+        uint64_t b = runs & (~0ull >> (63 - lane));
+        int word = w;
+        while (!b && word > 0) b = s_run[--word];
+        if (b) start = word * 64 + 63 - __clzll((long long)b);
+    }
+    const bool first = ok && (i - start) % cap == 0;
+    const uint64_t firsts = __ballot(first), ends = __ballot(first || !ok);
+    if (lane == 0) {
+        s_tile[w] = firsts;
+        s_end[w] = ends;
+    }
+    __syncthreads();
+    int tile = __popcll(firsts & ((1ull << lane) - 1));
+    for (int k = 0; k < w; ++k) tile += __popcll(s_tile[k]);
+    int nseg = 0, rows = 0, npg = 0, sp = 0;
+    uint64_t seen = 0;
+    if (first) {
+        uint64_t b = lane == 63 ? 0 : ends & (~0ull << (lane + 1));
+        int word = w;
+        while (!b && word < 3) b = s_end[++word];
+        rows = (b ? word * 64 + __ffsll((unsigned long long)b) - 1 : 256) - i;
+        for (int k = 0; k < rows; ++k) seen |= s_mask[i + k];
+        const int last = seen ? base + 63 - __clzll((long long)seen) : base - 1;
+        npg = last < 0 ? 0 : last / kPage + 1;
+        sp = tree_segment_pages(base / kPage + 1);
+        nseg = (base / kPage + sp) / sp;
+    }
+    // items in tile order
+    int at = nseg;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(at, o, 64);
+        if (lane >= o) at += u;
+    }
+    if (lane == 63) s_sum[w] = at;
+    __syncthreads();
+    int total = 0;
+    for (int k = 0; k < 4; ++k) {
+        if (k < w) at += s_sum[k];
+        total += s_sum[k];
+    }
+    if (i == 0) *ts.n_items = total;
+    at -= nseg;
+    for (int sg = 0; sg < nseg; ++sg) {
+        TreeItem it{};
+        it.seen = seen;
+        it.row0 = i;
+        it.n = rows;
+        it.base = base;
+        it.seq = sq;
+        it.plane = plane;
+        it.p0 = sg * sp;
+        it.p1 = sg == nseg - 1 ? npg : (sg + 1) * sp;
+        it.seg = sg;
+        it.nseg = nseg;
+        it.tile = tile;
+        ts.items[at + sg] = it;
+    }
+    if (nseg > 1)
+        for (int h = 0; h < H; ++h) ts.arrive[tile * H + h] = 0;
+}
+
+// ------------------------------------------------------------------ attention
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float over_rows_max(float x) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float over_rows_sum(float x) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Bits 0..3: whether positions base + off .. base + off + 3 are visible, those
+// below base always.  (What follows from it is written as selects: out of
+// branches the compiler has lost the write of a vector's last element.)
+__device__ __forceinline__ uint32_t sees4(uint64_t mask, int off) {
+    const int up = off < 0 ? 0 : off > 63 ? 63 : off, below = off < -4 ? 4 : off < 0 ? -off : 0;
+    const uint32_t m = off > 63 ? 0 : (uint32_t)(mask >> up) & 15u;
+    return (m << below | ((1u << below) - 1)) & 15u;
+}
+
+// V of a page in LDS: key row r holds its 32-byte pieces b (16 dims) at place
+// vpiece(b, r), so that the 8 rows that half a wave reads at once lie on
+// different banks.
+template <int HD>
+__device__ __forceinline__ int vpiece(int b, int r) {
+    if constexpr (HD == 128) return b ^ (r & 7);
+    if constexpr (HD == 64) return b ^ ((r >> 1) & 3);
+    const int s = b + ((r >> 2) & 1);  // 96: rows are 6 pieces apart
+    return s == 6 ? 0 : s;
+}
+
+template <int HD, int NT>
+struct TreeState {
+    floatx4 o[NT][HD / 16];
+    float m[NT], l[NT];  // l: this lane's keys only
+};
+
+template <int HD, int NT>
+__global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
+    const float* __restrict__ q, KvTarget kv, cdb_tree tree, int H, TreeScratch ts, uint16_t* __restrict__ out, int* err) {
+    constexpr int NJ = HD / 32, NB = HD / 16, CPR = HD / 8;  // K steps, dim blocks, 16-byte pieces of a row
+    constexpr int PITCH = HD + 4;
+    constexpr int ROWS = 16 * NT;
+    constexpr int REC = HD + 2;
+    constexpr bool QLDS = NT > 1;
+    // V of the waves' pairs, then the q operands; the waves' states take their place
+    constexpr int VBYTES = kTreeWaves * 2 * kPage * HD * 2, QBYTES = QLDS ? NT * NJ * 2 * 1024 : 0;
+    constexpr int OBYTES = kTreeWaves * ROWS * PITCH * 4;
+    __shared__ __align__(16) unsigned char smem[VBYTES + QBYTES > OBYTES ? VBYTES + QBYTES : OBYTES];
+    __shared__ float s_m[kTreeWaves][ROWS], s_l[kTreeWaves][ROWS];
+    __shared__ int s_last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const int d = H * HD;
+    const float qscale = 1.4426950408889634f / sqrtf((float)HD);
+    const size_t vofs = (size_t)H * kPage * HD;
+    uint16_t* sv = reinterpret_cast<uint16_t*>(smem) + wave * 2 * kPage * HD;
+    const int n_work = *ts.n_items * H;
+
+    for (int work = blockIdx.x; work < n_work; work += gridDim.x) {
+        const int head = work % H;
+        const TreeItem it = ts.items[work / H];
+        const int32_t* pt = kv.page_table + ((size_t)it.seq * kv.n_planes + it.plane) * kv.max_pages;
+        const int nt = (it.n + 15) / 16;  // 16-row tiles in use
+        const uint16_t* pool = kv.pool + kv_offset(kv.layer, 0, kv.n_pages, 0, head, H, 0, HD);
+        const size_t page_elems = kv_offset(0, 1, 1, 0, 0, H, 0, HD);
+
+        // this wave's pages: pairs p, p + 8, ...; lane l holds the id of page l % 2 of its pair l / 2
+        int p = it.p0 + 2 * wave;
+        const int mine = it.p1 > p ? (it.p1 - p + 7) / 8 : 0;
+        auto page_ids = [&](int from) {
+            const int pg = from + (lane >> 1) * 8 + (lane & 1);
+            return pg < it.p1 ? pt[pg] : -2;  // -2: past the context
+        };
+        int ids = page_ids(p);
+
+        // q operands: row c of tile t, dims 32j + 8g .. + 7, scaled, hi + lo.  One tile's
+        // stay in each wave's registers; more would cost the loop its second wave per
+        // SIMD (or spill, at four), so all waves read them from LDS.
+        auto q_operand = [&](int t, int j, bf16x8& hi, bf16x8& lo) {
+            const int row = it.row0 + min(t * 16 + c, it.n - 1);  // rows past the tile repeat its last one
+            const float* src = q + (size_t)row * d + head * HD + 32 * j + 8 * g;
+            floatx4 a, b;
+            __builtin_memcpy(&a, src, 16);
+            __builtin_memcpy(&b, src + 4, 16);
+            const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+            uint32_t hw[4], lw[4];
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const float x0 = x[e] * qscale, x1 = x[e + 1] * qscale;
+                const uint32_t h = pack_bf16(x0, x1);
+                hw[e / 2] = h;
+                lw[e / 2] = pack_bf16(x0 - bflo(h), x1 - bfhi(h));
+            }
+            hi = __builtin_bit_cast(bf16x8, u32x4{hw[0], hw[1], hw[2], hw[3]});
+            lo = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], lw[2], lw[3]});
+        };
+        u32x4* sq = reinterpret_cast<u32x4*>(smem + VBYTES) + lane;
+        bf16x8 qr[2][QLDS ? 1 : NJ];  // hi, lo
+        if constexpr (QLDS) {
+            for (int f = wave; f < nt * NJ; f += kTreeWaves) {
+                bf16x8 hi, lo;
+                q_operand(f / NJ, f % NJ, hi, lo);
+                sq[f * 128] = __builtin_bit_cast(u32x4, hi);
+                sq[f * 128 + 64] = __builtin_bit_cast(u32x4, lo);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) q_operand(0, j, qr[0][j], qr[1][j]);
+        }
+        TreeState<HD, NT> st;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            st.m[t] = -1e30f;
+            st.l[t] = 0.f;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) st.o[t][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        // The wave's pair i.  K comes as operands (lane = key c, dims 32j + 8g ..), V in
+        // 16-byte pieces as stored.  Where a page is missing (bit h of the pair's
+        // flags clear) the registers are zeros.
+        u32x4 kr[2][NJ], vr[2][NJ];
+        auto page_base = [&](int i, int h) -> const uint16_t* {
+            const int pid = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + h);
+            if (pid < 0 || pid >= kv.n_pages) return nullptr;
+            return pool + (size_t)pid * page_elems;
+        };
+        auto flags = [&](int i) -> int {
+            int there = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int pid = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + h);
+                if (pid >= 0 && pid < kv.n_pages)
+                    there |= 1 << h;
+                else if (pid != -2 && lane == 0)
+                    set_err(err, CDB_DEV_UNMAPPED_PAGE);
+            }
+            return there;
+        };
+        auto fetch_k = [&](int i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint16_t* b = page_base(i, h);
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+                    kr[h][j] = b ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(b + c * HD + 32 * j + 8 * g))
+                                 : u32x4{0, 0, 0, 0};
+            }
+        };
+        auto fetch_v = [&](int i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint16_t* b = page_base(i, h);
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+                    vr[h][j] = b ? __builtin_nontemporal_load(
+                                       reinterpret_cast<const u32x4*>(b + vofs + (j * 64 + lane) * 8))
+                                 : u32x4{0, 0, 0, 0};
+            }
+        };
+
+        if (mine > 0) {
+            fetch_v(0);
+            fetch_k(0);
+        }
+        if constexpr (QLDS) __syncthreads();
+        for (int i = 0; i < mine; ++i, p += 8) {
+            const int there = flags(i);
+            const bool masked = there != 3 || p * kPage + 2 * kPage > it.base;  // wave-uniform
+            bool odd = false;  // a V that is not finite where only some rows may see it
+            if (masked) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) {
+                        const int off = (p + h) * kPage + (j * 64 + lane) / CPR - it.base;
+                        const uint32_t keep = sees4(it.seen, off) & 1 ? ~0u : 0u;
+                        const uint32_t part = off < 0 ? 0u : ~0u;  // committed positions: every row sees them
+                        u32x4 x = vr[h][j] & keep;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t bad = ((x[e] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) |
+                                                 ((x[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+                            odd |= (bad & part) != 0;
+                            x[e] &= ~(bad & part);
+                        }
+                        vr[h][j] = x;
+                    }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    const int f = j * 64 + lane, r = f / CPR, ch = f - r * CPR;
+                    *reinterpret_cast<u32x4*>(sv + (h * kPage + r) * HD + vpiece<HD>(ch >> 1, r) * 16 + (ch & 1) * 8) =
+                        vr[h][j];
+                }
+            const bool more = i + 1 < mine;
+            if (more) {
+                if (((i + 1) & 31) == 0) ids = page_ids(p + 8);
+                fetch_v(i + 1);
+            }
+            floatx4 s[NT][2];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                if (t >= nt) continue;
+                s[t][0] = s[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int part = 1; part >= 0; --part)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) {
+                        bf16x8 b;
+                        if constexpr (QLDS)
+                            b = __builtin_bit_cast(bf16x8, sq[(t * NJ + j) * 128 + part * 64]);
+                        else
+                            b = qr[part][j];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][j]), b,
+                                                                              s[t][h], 0, 0, 0);
+                    }
+            }
+            if (more) fetch_k(i + 1);
+            bf16x8 ph[NT], pl[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                if (t >= nt) continue;
+                if (masked) {
+                    const uint64_t mask = tree.mask[it.row0 + min(t * 16 + c, it.n - 1)];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t see =
+                            sees4(mask, (p + h) * kPage + 4 * g - it.base) & (there >> h & 1 ? 15u : 0u);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[t][h][e] = see >> e & 1 ? s[t][h][e] : -INFINITY;
+                    }
+                }
+                float mx = st.m[t];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) mx = fmaxf(mx, s[t][e >> 2][e & 3]);
+                mx = over_rows_max(mx);
+                if (__any(mx > st.m[t])) {
+                    const float corr = exp2f(st.m[t] - mx);
+                    st.l[t] *= corr;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) st.o[t][b] *= corr;
+                    st.m[t] = mx;
+                }
+                uint32_t hw[4], lw[4];
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float p0 = exp2f(s[t][e >> 2][e & 3] - mx), p1 = exp2f(s[t][e >> 2][(e & 3) + 1] - mx);
+                    st.l[t] += p0 + p1;
+                    const uint32_t hi = pack_bf16(p0, p1);
+                    hw[e / 2] = hi;
+                    lw[e / 2] = pack_bf16(p0 - bflo(hi), p1 - bfhi(hi));
+                }
+                ph[t] = __builtin_bit_cast(bf16x8, u32x4{hw[0], hw[1], hw[2], hw[3]});
+                pl[t] = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], lw[2], lw[3]});
+            }
+            // A = V^T: dim 16b + c, keys 4g..4g+3 of both pages; lane c of group g points at key 4g + c/4, dims 4(c%4)..
+            const int vk = 4 * g + (c >> 2);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const uint16_t* va = sv + vk * HD + vpiece<HD>(b, vk) * 16 + (c & 3) * 4;
+                const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4*)va);
+                const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4*)(va + kPage * HD));
+                const uint2 w0 = __builtin_bit_cast(uint2, v0), w1 = __builtin_bit_cast(uint2, v1);
+                const bf16x8 a = __builtin_bit_cast(bf16x8, u32x4{w0.x, w0.y, w1.x, w1.y});
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    if (t >= nt) continue;
+                    st.o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pl[t], st.o[t][b], 0, 0, 0);
+                    st.o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, ph[t], st.o[t][b], 0, 0, 0);
+                }
+            }
+            if (masked && __any(odd)) {  // rare: the values taken out above, to the rows that see them
+                for (int kk = 0; kk < 2 * kPage; ++kk) {
+                    const int off = p * kPage + kk - it.base;
+                    if (off < 0 || off >= 64 || !(it.seen >> off & 1) || !(there >> (kk >> 4) & 1)) continue;
+                    const uint16_t* row = pool + (size_t)pt[p + (kk >> 4)] * page_elems + vofs + (kk & 15) * HD;
+                    const int w = (kk >> 4) * 2 + ((kk & 3) >> 1);  // p of key kk: word w, half kk % 2, of lane group kk % 16 / 4
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        if (t >= nt) continue;
+                        const u32x4 h4 = __builtin_bit_cast(u32x4, ph[t]), l4 = __builtin_bit_cast(u32x4, pl[t]);
+                        uint32_t hw = 0, lw = 0;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (e == w) {
+                                hw = h4[e];
+                                lw = l4[e];
+                            }
+                        const int from = c + 16 * ((kk & 15) >> 2);
+                        hw = __shfl(hw, from, 64);
+                        lw = __shfl(lw, from, 64);
+                        const float pk = kk & 1 ? bfhi(hw) + bfhi(lw) : bflo(hw) + bflo(lw);
+                        const bool see = tree.mask[it.row0 + min(t * 16 + c, it.n - 1)] >> off & 1;
+#pragma unroll
+                        for (int b = 0; b < NB; ++b)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const uint32_t x = row[16 * b + 4 * g + e];
+                                const float o = st.o[t][b][e];
+                                st.o[t][b][e] = see && (x & 0x7f80u) == 0x7f80u ? fmaf(pk, bf2f((uint16_t)x), o) : o;
+                            }
+                    }
+                }
+            }
+        }
+
+        // the four waves' states: [wave][row][dim]
+        __syncthreads();  // every wave is done with its V
+        float* so = reinterpret_cast<float*>(smem);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if (t >= nt) continue;
+            const float l = over_rows_sum(st.l[t]);
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                *reinterpret_cast<floatx4*>(so + (wave * ROWS + t * 16 + c) * PITCH + 16 * b + 4 * g) = st.o[t][b];
+            if (g == 0) {
+                s_m[wave][t * 16 + c] = st.m[t];
+                s_l[wave][t * 16 + c] = l;
+            }
+        }
+        __syncthreads();
+        for (int e = tid; e < it.n * CPR; e += kTreeWaves * 64) {
+            const int r = e / CPR, c8 = e - r * CPR;
+            float mx = s_m[0][r];
+#pragma unroll
+            for (int w = 1; w < kTreeWaves; ++w) mx = fmaxf(mx, s_m[w][r]);
+            float den = 0.f, num[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < kTreeWaves; ++w) {
+                const float f = exp2f(s_m[w][r] - mx);
+                den = fmaf(f, s_l[w][r], den);
+                const float* src = so + (w * ROWS + r) * PITCH + c8 * 8;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) num[k] = fmaf(f, src[k], num[k]);
+            }
+            const int row = it.row0 + r;
+            if (it.nseg == 1) {
+                uint32_t pk[4];
+#pragma unroll
+                for (int k = 0; k < 8; k += 2)
+                    pk[k / 2] = pack_bf16(den != 0.f ? num[k] / den : 0.f, den != 0.f ? num[k + 1] / den : 0.f);
+                *reinterpret_cast<u32x4*>(out + frag_index(row, head * HD + c8 * 8, d)) = u32x4{pk[0], pk[1], pk[2], pk[3]};
+            } else {  // written through to memory: another XCD's workgroup may read it
+                float* rec = ts.part + (((size_t)row * H + head) * kTreeSegs + it.seg) * REC;
+                auto put = [&](float* at, float a, float b) {
+                    __hip_atomic_store(reinterpret_cast<uint64_t*>(at),
+                                       (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a), __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+                };
+#pragma unroll
+                for (int k = 0; k < 8; k += 2) put(rec + c8 * 8 + k, num[k], num[k + 1]);
+                if (c8 == 0) put(rec + HD, mx, den);
+            }
+        }
+        if (it.nseg > 1) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the wave's records have reached memory
+            __syncthreads();
+            if (tid == 0) {
+                int* a = ts.arrive + it.tile * H + head;
+                s_last = __hip_atomic_fetch_add(a, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == it.nseg - 1;
+                if (s_last) __hip_atomic_store(a, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            __syncthreads();
+            if (s_last) {
+                for (int e = tid; e < it.n * CPR; e += kTreeWaves * 64) {
+                    const int r = e / CPR, c8 = e - r * CPR;
+                    const int row = it.row0 + r;
+                    const float* rec0 = ts.part + ((size_t)row * H + head) * kTreeSegs * REC;
+                    auto get = [&](const float* at, float& a, float& b) {
+                        const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(at), __ATOMIC_RELAXED,
+                                                             __HIP_MEMORY_SCOPE_AGENT);
+                        a = __uint_as_float((uint32_t)v);
+                        b = __uint_as_float((uint32_t)(v >> 32));
+                    };
+                    float sm[kTreeSegs], sl[kTreeSegs], mx = -1e30f;
+#pragma unroll
+                    for (int sg = 0; sg < kTreeSegs; ++sg)
+                        if (sg < it.nseg) get(rec0 + sg * REC + HD, sm[sg], sl[sg]);
+                    float den = 0.f, num[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int sg = 0; sg < kTreeSegs; ++sg)
+                        if (sg < it.nseg) mx = fmaxf(mx, sm[sg]);
+#pragma unroll
+                    for (int sg = 0; sg < kTreeSegs; ++sg)
+                        if (sg < it.nseg) {
+                            const float f = exp2f(sm[sg] - mx);
+                            den = fmaf(f, sl[sg], den);
+#pragma unroll
+                            for (int k = 0; k < 8; k += 2) {
+                                float a, b;
+                                get(rec0 + sg * REC + c8 * 8 + k, a, b);
+                                num[k] = fmaf(f, a, num[k]);
+                                num[k + 1] = fmaf(f, b, num[k + 1]);
+                            }
+                        }
+                    uint32_t pk[4];
+#pragma unroll
+                    for (int k = 0; k < 8; k += 2)
+                        pk[k / 2] = pack_bf16(den != 0.f ? num[k] / den : 0.f, den != 0.f ? num[k + 1] / den : 0.f);
+                    *reinterpret_cast<u32x4*>(out + frag_index(row, head * HD + c8 * 8, d)) =
+                        u32x4{pk[0], pk[1], pk[2], pk[3]};
+                }
+            }
+        }
+        __syncthreads();  // the next item's V takes the place of the states
+    }
+}
+
+// 16-row tiles per workgroup
+static int tree_tiles(int max_nodes) { return max_nodes <= 16 ? 1 : max_nodes <= 32 ? 2 : 4; }
+
+hipError_t launch_tree_plan(const KvTarget& kv, const int32_t* seq, const cdb_tree& tree, int M, int H, int hd,
+                            void* scratch, int* err, hipStream_t st, const int32_t* dn) {
     if (M <= 0) return hipSuccess;
-    const dim3 grid(H, M);
+    if (M > kMaxRows) return hipErrorInvalidValue;
+    k_tree_plan<<<1, 256, 0, st>>>(kv, seq, tree, M, H, 16 * tree_tiles(tree.max_nodes),
+                                   tree_scratch(scratch, H, hd, M), err, dn);
+    return hipGetLastError();
+}
+
+template <int HD>
+static void run_tree_attn(int nt, dim3 grid, const float* q, const KvTarget& kv, const cdb_tree& tree, int H,
+                          const TreeScratch& ts, uint16_t* out, int* err, hipStream_t st) {
+    if (nt == 1)
+        k_tree_attn<HD, 1><<<grid, kTreeWaves * 64, 0, st>>>(q, kv, tree, H, ts, out, err);
+    else if (nt == 2)
+        k_tree_attn<HD, 2><<<grid, kTreeWaves * 64, 0, st>>>(q, kv, tree, H, ts, out, err);
+    else
+        k_tree_attn<HD, 4><<<grid, kTreeWaves * 64, 0, st>>>(q, kv, tree, H, ts, out, err);
+}
+
+hipError_t launch_tree_attention(const float* q, const KvTarget& kv, const cdb_tree& tree, int M, int H, int hd,
+                                 void* scratch, uint16_t* out, int* err, hipStream_t st) {
+    if (M <= 0) return hipSuccess;
+    const TreeScratch ts = tree_scratch(scratch, H, hd, M);
+    const int nt = tree_tiles(tree.max_nodes);
+    // as many workgroups as there can be items, up to what is resident at once
+    const int most = kv.max_pages <= 32 ? 1 : std::min(kTreeSegs, (kv.max_pages + 31) / 32);
+    const dim3 grid(std::min(M * H * most, 256 * (nt == 1 ? 2 : 1)));
     switch (hd) {
-        case 64: k_tree_attn<64><<<grid, 64, 0, st>>>(q, kv, seq, tree, M, H, out, err, dn); break;
-        case 96: k_tree_attn<96><<<grid, 64, 0, st>>>(q, kv, seq, tree, M, H, out, err, dn); break;
-        case 128: k_tree_attn<128><<<grid, 64, 0, st>>>(q, kv, seq, tree, M, H, out, err, dn); break;
+        case 64: run_tree_attn<64>(nt, grid, q, kv, tree, H, ts, out, err, st); break;
+        case 96: run_tree_attn<96>(nt, grid, q, kv, tree, H, ts, out, err, st); break;
+        case 128: run_tree_attn<128>(nt, grid, q, kv, tree, H, ts, out, err, st); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
