@@ -8,7 +8,7 @@
 //
 // k_tree_plan (one workgroup, once per stage call) cuts the rows into tiles:
 // adjacent rows of one sequence, plane and base, at most 16 NT of them.  A tile's
-// context is cut into segments (tree_segment_pages, by its base alone), and a
+// context is cut into segments (tree_segments, by its base alone), and a
 // work item is one segment of one tile, for each head.
 //
 // k_tree_attn: a workgroup takes items in turn; its 4 waves deal the segment's
@@ -44,10 +44,15 @@ namespace cdb {
 constexpr int kTreeWaves = 4;
 constexpr int kTreeSegs = 16;  // most segments of a context
 
-// Pages per segment of a context whose last committed position is on page npg - 1.
-__host__ __device__ __forceinline__ int tree_segment_pages(int npg) {
-    const int p = (npg + 8 * kTreeSegs - 1) / (8 * kTreeSegs) * 8;
-    return p < 32 ? 32 : p;
+constexpr int kTreeSegPages = 64;  // pages of a segment, unless that makes too many
+
+// Segments of a context whose last committed position is on page npg - 1, and the
+// pages of each (the last one has the rest).
+__host__ __device__ __forceinline__ int tree_segments(int npg, int* pages) {
+    int n = (npg + kTreeSegPages - 1) / kTreeSegPages;
+    n = n > kTreeSegs ? kTreeSegs : n;
+    *pages = (npg + 8 * n - 1) / (8 * n) * 8;
+    return (npg + *pages - 1) / *pages;
 }
 
 struct TreeItem {
@@ -147,8 +152,7 @@ __global__ __launch_bounds__(256) void k_tree_plan(KvTarget kv, const int32_t* _
         for (int k = 0; k < rows; ++k) seen |= s_mask[i + k];
         const int last = seen ? base + 63 - __clzll((long long)seen) : base - 1;
         npg = last < 0 ? 0 : last / kPage + 1;
-        sp = tree_segment_pages(base / kPage + 1);
-        nseg = (base / kPage + sp) / sp;
+        nseg = tree_segments(base / kPage + 1, &sp);
     }
     // items in tile order
     int at = nseg;
@@ -239,7 +243,8 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
     constexpr int VBYTES = kTreeWaves * 2 * kPage * HD * 2, QBYTES = QLDS ? NT * NJ * 2 * 1024 : 0;
     constexpr int OBYTES = kTreeWaves * ROWS * PITCH * 4;
     __shared__ __align__(16) unsigned char smem[VBYTES + QBYTES > OBYTES ? VBYTES + QBYTES : OBYTES];
-    __shared__ float s_m[kTreeWaves][ROWS], s_l[kTreeWaves][ROWS];
+    __shared__ float s_m[kTreeWaves][ROWS], s_l[kTreeWaves][ROWS], s_f[kTreeWaves][ROWS], s_den[ROWS];
+    __shared__ float s_fs[kTreeSegs][ROWS];
     __shared__ int s_last;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
@@ -254,6 +259,25 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
         const TreeItem it = ts.items[work / H];
         const int32_t* pt = kv.page_table + ((size_t)it.seq * kv.n_planes + it.plane) * kv.max_pages;
         const int nt = (it.n + 15) / 16;  // 16-row tiles in use
+        // A segment's record of a row: sums, maximum, weight.  Written through to memory
+        // and read past the caches: the workgroups run on XCDs with L2s of their own.
+        auto rec = [&](int row, int sg) {
+            return ts.part + (((size_t)row * H + head) * kTreeSegs + sg) * REC;
+        };
+        auto put2 = [](float* at, float a, float b) {
+            __hip_atomic_store(reinterpret_cast<uint64_t*>(at), (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a),
+                               __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        };
+        auto get2 = [](const float* at, float& a, float& b) {
+            const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(at), __ATOMIC_RELAXED,
+                                                 __HIP_MEMORY_SCOPE_AGENT);
+            a = __uint_as_float((uint32_t)v);
+            b = __uint_as_float((uint32_t)(v >> 32));
+        };
+        auto finish = [&](int row, int k, float a, float b, float den) {  // den 0: the row sees nothing
+            *reinterpret_cast<uint32_t*>(out + frag_index(row, head * HD + k, d)) =
+                den != 0.f ? pack_bf16(a / den, b / den) : 0u;
+        };
         const uint16_t* pool = kv.pool + kv_offset(kv.layer, 0, kv.n_pages, 0, head, H, 0, HD);
         const size_t page_elems = kv_offset(0, 1, 1, 0, 0, H, 0, HD);
 
@@ -520,38 +544,35 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
             }
         }
         __syncthreads();
-        for (int e = tid; e < it.n * CPR; e += kTreeWaves * 64) {
-            const int r = e / CPR, c8 = e - r * CPR;
-            float mx = s_m[0][r];
+        // row factors: waves of this segment
+        if (tid < it.n) {
+            float mx = s_m[0][tid], den = 0.f;
 #pragma unroll
-            for (int w = 1; w < kTreeWaves; ++w) mx = fmaxf(mx, s_m[w][r]);
-            float den = 0.f, num[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            for (int w = 1; w < kTreeWaves; ++w) mx = fmaxf(mx, s_m[w][tid]);
 #pragma unroll
             for (int w = 0; w < kTreeWaves; ++w) {
-                const float f = exp2f(s_m[w][r] - mx);
-                den = fmaf(f, s_l[w][r], den);
-                const float* src = so + (w * ROWS + r) * PITCH + c8 * 8;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) num[k] = fmaf(f, src[k], num[k]);
+                const float f = exp2f(s_m[w][tid] - mx);
+                s_f[w][tid] = f;
+                den = fmaf(f, s_l[w][tid], den);
             }
-            const int row = it.row0 + r;
-            if (it.nseg == 1) {
-                uint32_t pk[4];
+            s_den[tid] = den;
+            if (it.nseg > 1) put2(rec(it.row0 + tid, it.seg) + HD, mx, den);
+        }
+        __syncthreads();
+        // thread = two dims of a row, so that a wave's stores are one run
+        for (int e = tid; e < it.n * (HD / 2); e += kTreeWaves * 64) {
+            const int r = e / (HD / 2), k = 2 * (e - r * (HD / 2));
+            float a = 0.f, b = 0.f;
 #pragma unroll
-                for (int k = 0; k < 8; k += 2)
-                    pk[k / 2] = pack_bf16(den != 0.f ? num[k] / den : 0.f, den != 0.f ? num[k + 1] / den : 0.f);
-                *reinterpret_cast<u32x4*>(out + frag_index(row, head * HD + c8 * 8, d)) = u32x4{pk[0], pk[1], pk[2], pk[3]};
-            } else {  // written through to memory: another XCD's workgroup may read it
-                float* rec = ts.part + (((size_t)row * H + head) * kTreeSegs + it.seg) * REC;
-                auto put = [&](float* at, float a, float b) {
-                    __hip_atomic_store(reinterpret_cast<uint64_t*>(at),
-                                       (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a), __ATOMIC_RELAXED,
-                                       __HIP_MEMORY_SCOPE_AGENT);
-                };
-#pragma unroll
-                for (int k = 0; k < 8; k += 2) put(rec + c8 * 8 + k, num[k], num[k + 1]);
-                if (c8 == 0) put(rec + HD, mx, den);
+            for (int w = 0; w < kTreeWaves; ++w) {
+                const float2 o2 = *reinterpret_cast<const float2*>(so + (w * ROWS + r) * PITCH + k);
+                a = fmaf(s_f[w][r], o2.x, a);
+                b = fmaf(s_f[w][r], o2.y, b);
             }
+            if (it.nseg == 1)
+                finish(it.row0 + r, k, a, b, s_den[r]);
+            else
+                put2(rec(it.row0 + r, it.seg) + k, a, b);
         }
         if (it.nseg > 1) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the wave's records have reached memory
@@ -563,43 +584,39 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
             }
             __syncthreads();
             if (s_last) {
-                for (int e = tid; e < it.n * CPR; e += kTreeWaves * 64) {
-                    const int r = e / CPR, c8 = e - r * CPR;
-                    const int row = it.row0 + r;
-                    const float* rec0 = ts.part + ((size_t)row * H + head) * kTreeSegs * REC;
-                    auto get = [&](const float* at, float& a, float& b) {
-                        const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(at), __ATOMIC_RELAXED,
-                                                             __HIP_MEMORY_SCOPE_AGENT);
-                        a = __uint_as_float((uint32_t)v);
-                        b = __uint_as_float((uint32_t)(v >> 32));
-                    };
-                    float sm[kTreeSegs], sl[kTreeSegs], mx = -1e30f;
+                if (tid < it.n) {
+                    float sm[kTreeSegs], sl[kTreeSegs], mx = -1e30f, den = 0.f;
 #pragma unroll
-                    for (int sg = 0; sg < kTreeSegs; ++sg)
-                        if (sg < it.nseg) get(rec0 + sg * REC + HD, sm[sg], sl[sg]);
-                    float den = 0.f, num[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    for (int sg = 0; sg < kTreeSegs; ++sg)  // past the last: the last again, with weight 0
+                        get2(rec(it.row0 + tid, min(sg, it.nseg - 1)) + HD, sm[sg], sl[sg]);
 #pragma unroll
-                    for (int sg = 0; sg < kTreeSegs; ++sg)
-                        if (sg < it.nseg) mx = fmaxf(mx, sm[sg]);
+                    for (int sg = 0; sg < kTreeSegs; ++sg) mx = fmaxf(mx, sm[sg]);
 #pragma unroll
-                    for (int sg = 0; sg < kTreeSegs; ++sg)
-                        if (sg < it.nseg) {
-                            const float f = exp2f(sm[sg] - mx);
-                            den = fmaf(f, sl[sg], den);
+                    for (int sg = 0; sg < kTreeSegs; ++sg) {
+                        const float f = exp2f(sm[sg] - mx);
+                        s_fs[sg][tid] = f;
+                        den = sg < it.nseg ? fmaf(f, sl[sg], den) : den;
+                    }
+                    s_den[tid] = den;
+                }
+                __syncthreads();
+                for (int e = tid; e < it.n * (HD / 2); e += kTreeWaves * 64) {
+                    const int r = e / (HD / 2), k = 2 * (e - r * (HD / 2));
+                    const float* at = rec(it.row0 + r, 0) + k;
+                    float a = 0.f, b = 0.f;
+                    for (int s0 = 0; s0 < it.nseg; s0 += 8) {
+                        float x[8], y[8];
 #pragma unroll
-                            for (int k = 0; k < 8; k += 2) {
-                                float a, b;
-                                get(rec0 + sg * REC + c8 * 8 + k, a, b);
-                                num[k] = fmaf(f, a, num[k]);
-                                num[k + 1] = fmaf(f, b, num[k + 1]);
-                            }
+                        for (int u = 0; u < 8; ++u) get2(at + min(s0 + u, it.nseg - 1) * REC, x[u], y[u]);
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            const bool in = s0 + u < it.nseg;
+                            const float f = s_fs[min(s0 + u, it.nseg - 1)][r];
+                            a = in ? fmaf(f, x[u], a) : a;
+                            b = in ? fmaf(f, y[u], b) : b;
                         }
-                    uint32_t pk[4];
-#pragma unroll
-                    for (int k = 0; k < 8; k += 2)
-                        pk[k / 2] = pack_bf16(den != 0.f ? num[k] / den : 0.f, den != 0.f ? num[k + 1] / den : 0.f);
-                    *reinterpret_cast<u32x4*>(out + frag_index(row, head * HD + c8 * 8, d)) =
-                        u32x4{pk[0], pk[1], pk[2], pk[3]};
+                    }
+                    finish(it.row0 + r, k, a, b, s_den[r]);
                 }
             }
         }
@@ -636,7 +653,7 @@ hipError_t launch_tree_attention(const float* q, const KvTarget& kv, const cdb_t
     const TreeScratch ts = tree_scratch(scratch, H, hd, M);
     const int nt = tree_tiles(tree.max_nodes);
     // as many workgroups as there can be items, up to what is resident at once
-    const int most = kv.max_pages <= 32 ? 1 : std::min(kTreeSegs, (kv.max_pages + 31) / 32);
+    const int most = std::min(kTreeSegs, std::max(1, (kv.max_pages + 1 + kTreeSegPages - 1) / kTreeSegPages));
     const dim3 grid(std::min(M * H * most, 256 * (nt == 1 ? 2 : 1)));
     switch (hd) {
         case 64: run_tree_attn<64>(nt, grid, q, kv, tree, H, ts, out, err, st); break;
