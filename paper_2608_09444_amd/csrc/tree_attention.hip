@@ -214,6 +214,10 @@ __device__ __forceinline__ uint32_t sees4(uint64_t mask, int off) {
     return (m << below | ((1u << below) - 1)) & 15u;
 }
 
+// 2^x by the hardware instruction: within an ulp, results below the smallest normal
+// number are 0 (weights that far below the largest do not show in 32-bit sums).
+__device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
+
 // V of a page in LDS: key row r holds its 32-byte pieces b (16 dims) at place
 // vpiece(b, r), so that the 8 rows that half a wave reads at once lie on
 // different banks.
@@ -239,6 +243,7 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
     constexpr int ROWS = 16 * NT;
     constexpr int REC = HD + 2;
     constexpr bool QLDS = NT > 1;
+    constexpr int GT = NT > 1 ? 2 : 1;
     // V of the waves' pairs, then the q operands; the waves' states take their place
     constexpr int VBYTES = kTreeWaves * 2 * kPage * HD * 2, QBYTES = QLDS ? NT * NJ * 2 * 1024 : 0;
     constexpr int OBYTES = kTreeWaves * ROWS * PITCH * 4;
@@ -314,7 +319,7 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
         u32x4* sq = reinterpret_cast<u32x4*>(smem + VBYTES) + lane;
         bf16x8 qr[2][QLDS ? 1 : NJ];  // hi, lo
         if constexpr (QLDS) {
-            for (int f = wave; f < nt * NJ; f += kTreeWaves) {
+            for (int f = wave; f < (nt + GT - 1) / GT * GT * NJ; f += kTreeWaves) {
                 bf16x8 hi, lo;
                 q_operand(f / NJ, f % NJ, hi, lo);
                 sq[f * 128] = __builtin_bit_cast(u32x4, hi);
@@ -417,81 +422,104 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
                 if (((i + 1) & 31) == 0) ids = page_ids(p + 8);
                 fetch_v(i + 1);
             }
+            // Tiles go in groups of GT, skipped whole past the last used one: a group's
+            // products are independent chains that the matrix cores interleave.
             floatx4 s[NT][2];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                if (t >= nt) continue;
-                s[t][0] = s[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+            for (int t0 = 0; t0 < NT; t0 += GT) {
+                if (t0 >= nt) continue;
+#pragma unroll
+                for (int t = t0; t < t0 + GT; ++t) s[t][0] = s[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int part = 1; part >= 0; --part)
 #pragma unroll
-                    for (int j = 0; j < NJ; ++j) {
-                        bf16x8 b;
-                        if constexpr (QLDS)
-                            b = __builtin_bit_cast(bf16x8, sq[(t * NJ + j) * 128 + part * 64]);
-                        else
-                            b = qr[part][j];
+                    for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][j]), b,
-                                                                              s[t][h], 0, 0, 0);
-                    }
+                        for (int t = t0; t < t0 + GT; ++t) {
+                            bf16x8 b;
+                            if constexpr (QLDS)
+                                b = __builtin_bit_cast(bf16x8, sq[(t * NJ + j) * 128 + part * 64]);
+                            else
+                                b = qr[part][j];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][j]), b,
+                                                                                  s[t][h], 0, 0, 0);
+                        }
             }
             if (more) fetch_k(i + 1);
-            bf16x8 ph[NT], pl[NT];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                if (t >= nt) continue;
-                if (masked) {
-                    const uint64_t mask = tree.mask[it.row0 + min(t * 16 + c, it.n - 1)];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t see =
-                            sees4(mask, (p + h) * kPage + 4 * g - it.base) & (there >> h & 1 ? 15u : 0u);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s[t][h][e] = see >> e & 1 ? s[t][h][e] : -INFINITY;
-                    }
-                }
-                float mx = st.m[t];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) mx = fmaxf(mx, s[t][e >> 2][e & 3]);
-                mx = over_rows_max(mx);
-                if (__any(mx > st.m[t])) {
-                    const float corr = exp2f(st.m[t] - mx);
-                    st.l[t] *= corr;
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) st.o[t][b] *= corr;
-                    st.m[t] = mx;
-                }
-                uint32_t hw[4], lw[4];
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float p0 = exp2f(s[t][e >> 2][e & 3] - mx), p1 = exp2f(s[t][e >> 2][(e & 3) + 1] - mx);
-                    st.l[t] += p0 + p1;
-                    const uint32_t hi = pack_bf16(p0, p1);
-                    hw[e / 2] = hi;
-                    lw[e / 2] = pack_bf16(p0 - bflo(hi), p1 - bfhi(hi));
-                }
-                ph[t] = __builtin_bit_cast(bf16x8, u32x4{hw[0], hw[1], hw[2], hw[3]});
-                pl[t] = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], lw[2], lw[3]});
-            }
             // A = V^T: dim 16b + c, keys 4g..4g+3 of both pages; lane c of group g points at key 4g + c/4, dims 4(c%4)..
             const int vk = 4 * g + (c >> 2);
+            bf16x8 va[NB];
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                const uint16_t* va = sv + vk * HD + vpiece<HD>(b, vk) * 16 + (c & 3) * 4;
-                const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4*)va);
-                const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4*)(va + kPage * HD));
-                const uint2 w0 = __builtin_bit_cast(uint2, v0), w1 = __builtin_bit_cast(uint2, v1);
-                const bf16x8 a = __builtin_bit_cast(bf16x8, u32x4{w0.x, w0.y, w1.x, w1.y});
+                const uint16_t* at = sv + vk * HD + vpiece<HD>(b, vk) * 16 + (c & 3) * 4;
+                const uint2 w0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                               (__attribute__((address_space(3))) s16x4*)at));
+                const uint2 w1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                               (__attribute__((address_space(3))) s16x4*)(at + kPage * HD)));
+                va[b] = __builtin_bit_cast(bf16x8, u32x4{w0.x, w0.y, w1.x, w1.y});
+            }
+            bf16x8 ph[NT], pl[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    if (t >= nt) continue;
-                    st.o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pl[t], st.o[t][b], 0, 0, 0);
-                    st.o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, ph[t], st.o[t][b], 0, 0, 0);
+            for (int t0 = 0; t0 < NT; t0 += GT) {
+                if (t0 >= nt) continue;
+                float mx[GT];
+                bool up = false;
+#pragma unroll
+                for (int u = 0; u < GT; ++u) {
+                    const int t = t0 + u;
+                    if (masked) {
+                        const uint64_t mask = tree.mask[it.row0 + min(t * 16 + c, it.n - 1)];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t see =
+                                sees4(mask, (p + h) * kPage + 4 * g - it.base) & (there >> h & 1 ? 15u : 0u);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[t][h][e] = see >> e & 1 ? s[t][h][e] : -INFINITY;
+                        }
+                    }
+                    mx[u] = st.m[t];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) mx[u] = fmaxf(mx[u], s[t][e >> 2][e & 3]);
+                    mx[u] = over_rows_max(mx[u]);
+                    up |= mx[u] > st.m[t];
                 }
+                if (__any(up)) {
+#pragma unroll
+                    for (int u = 0; u < GT; ++u) {
+                        const int t = t0 + u;
+                        const float corr = exp2_raw(st.m[t] - mx[u]);
+                        st.l[t] *= corr;
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) st.o[t][b] *= corr;
+                        st.m[t] = mx[u];
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < GT; ++u) {
+                    const int t = t0 + u;
+                    uint32_t hw[4], lw[4];
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const float p0 = exp2_raw(s[t][e >> 2][e & 3] - mx[u]);
+                        const float p1 = exp2_raw(s[t][e >> 2][(e & 3) + 1] - mx[u]);
+                        st.l[t] += p0 + p1;
+                        const uint32_t hi = pack_bf16(p0, p1);
+                        hw[e / 2] = hi;
+                        lw[e / 2] = pack_bf16(p0 - bflo(hi), p1 - bfhi(hi));
+                    }
+                    ph[t] = __builtin_bit_cast(bf16x8, u32x4{hw[0], hw[1], hw[2], hw[3]});
+                    pl[t] = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], lw[2], lw[3]});
+                }
+#pragma unroll
+                for (int part = 1; part >= 0; --part)
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int t = t0; t < t0 + GT; ++t)
+                            st.o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[b], part ? pl[t] : ph[t], st.o[t][b], 0,
+                                                                                 0, 0);
             }
             if (masked && __any(odd)) {  // rare: the values taken out above, to the rows that see them
                 for (int kk = 0; kk < 2 * kPage; ++kk) {
@@ -551,7 +579,7 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
             for (int w = 1; w < kTreeWaves; ++w) mx = fmaxf(mx, s_m[w][tid]);
 #pragma unroll
             for (int w = 0; w < kTreeWaves; ++w) {
-                const float f = exp2f(s_m[w][tid] - mx);
+                const float f = exp2_raw(s_m[w][tid] - mx);
                 s_f[w][tid] = f;
                 den = fmaf(f, s_l[w][tid], den);
             }
@@ -593,7 +621,7 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
                     for (int sg = 0; sg < kTreeSegs; ++sg) mx = fmaxf(mx, sm[sg]);
 #pragma unroll
                     for (int sg = 0; sg < kTreeSegs; ++sg) {
-                        const float f = exp2f(sm[sg] - mx);
+                        const float f = exp2_raw(sm[sg] - mx);
                         s_fs[sg][tid] = f;
                         den = sg < it.nseg ? fmaf(f, sl[sg], den) : den;
                     }
