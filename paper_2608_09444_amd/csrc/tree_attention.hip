@@ -229,41 +229,117 @@ __device__ __forceinline__ int vpiece(int b, int r) {
     return s == 6 ? 0 : s;
 }
 
+struct Work {
+    TreeItem it;
+    int head;
+    int p, mine, nt;
+};
+
 template <int HD, int NT>
 struct TreeState {
     floatx4 o[NT][HD / 16];
     float m[NT], l[NT];  // l: this lane's keys only
 };
 
-template <int HD, int NT>
-__global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
+template <int HD, int NT, int HV>
+__global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
     const float* __restrict__ q, KvTarget kv, cdb_tree tree, int H, TreeScratch ts, uint16_t* __restrict__ out, int* err) {
     constexpr int NJ = HD / 32, NB = HD / 16, CPR = HD / 8;  // K steps, dim blocks, 16-byte pieces of a row
     constexpr int PITCH = HD + 4;
-    constexpr int ROWS = 16 * NT;
+    constexpr int ROWS = 16 * NT * HV, THREADS = kTreeWaves * 64 * HV;
     constexpr int REC = HD + 2;
     constexpr bool QLDS = NT > 1;
     constexpr int GT = NT > 1 ? 2 : 1;
     // V of the waves' pairs, then the q operands; the waves' states take their place
-    constexpr int VBYTES = kTreeWaves * 2 * kPage * HD * 2, QBYTES = QLDS ? NT * NJ * 2 * 1024 : 0;
+    constexpr int VBYTES = kTreeWaves * HV * 2 * kPage * HD * 2, QBYTES = QLDS ? NT * HV * NJ * 2 * 1024 : 0;
     constexpr int OBYTES = kTreeWaves * ROWS * PITCH * 4;
     __shared__ __align__(16) unsigned char smem[VBYTES + QBYTES > OBYTES ? VBYTES + QBYTES : OBYTES];
     __shared__ float s_m[kTreeWaves][ROWS], s_l[kTreeWaves][ROWS], s_f[kTreeWaves][ROWS], s_den[ROWS];
     __shared__ float s_fs[kTreeSegs][ROWS];
     __shared__ int s_last;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int cls = wave % kTreeWaves, half = wave / kTreeWaves;
     const int c = lane & 15, g = lane >> 4;
     const int d = H * HD;
     const float qscale = 1.4426950408889634f / sqrtf((float)HD);
-    const size_t vofs = (size_t)H * kPage * HD;
+    const size_t vofs = (size_t)H * kPage * HD, page_elems = 2 * vofs;
     uint16_t* sv = reinterpret_cast<uint16_t*>(smem) + wave * 2 * kPage * HD;
-    const int n_work = *ts.n_items * H;
 
-    for (int work = blockIdx.x; work < n_work; work += gridDim.x) {
-        const int head = work % H;
-        const TreeItem it = ts.items[work / H];
-        const int32_t* pt = kv.page_table + ((size_t)it.seq * kv.n_planes + it.plane) * kv.max_pages;
-        const int nt = (it.n + 15) / 16;  // 16-row tiles in use
+    auto load_work = [&](int w) {
+        Work x;
+        x.it = ts.items[w / H];
+        x.head = w % H;
+        x.p = x.it.p0 + 2 * cls;
+        // 16-row tiles of this wave's half in use, and its pages: pairs p, p + 8, ...
+        x.nt = min(max((x.it.n + 15) / 16 - half * NT, 0), NT);
+        x.mine = x.nt > 0 && x.it.p1 > x.p ? (x.it.p1 - x.p + 7) / 8 : 0;
+        return x;
+    };
+    // lane l: the id of page l % 2 of pair l / 2 from page `from` on
+    auto page_ids = [&](const Work& x, int from) {
+        const int pg = from + (lane >> 1) * 8 + (lane & 1);
+        return pg < x.it.p1 ? kv.page_table[((size_t)x.it.seq * kv.n_planes + x.it.plane) * kv.max_pages + pg]
+                            : -2;  // past the context
+    };
+    // The wave's pair i.  K comes as operands (lane = key c, dims 32j + 8g ..), V in
+    // 16-byte pieces as stored.  Where a page is missing (bit h of the pair's
+    // flags clear) the registers are zeros.
+    u32x4 kr[2][NJ], vr[2][NJ];
+    auto page_base = [&](const Work& x, int ids, int i, int h) -> const uint16_t* {
+        const int pid = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + h);
+        if (pid < 0 || pid >= kv.n_pages) return nullptr;
+        return kv.pool + kv_offset(kv.layer, pid, kv.n_pages, 0, x.head, H, 0, HD);
+    };
+    auto flags = [&](int ids, int i) -> int {
+        int there = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int pid = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + h);
+            if (pid >= 0 && pid < kv.n_pages)
+                there |= 1 << h;
+            else if (pid != -2 && lane == 0)
+                set_err(err, CDB_DEV_UNMAPPED_PAGE);
+        }
+        return there;
+    };
+    auto fetch_k = [&](const Work& x, int ids, int i) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint16_t* b = page_base(x, ids, i, h);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+                kr[h][j] = b ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(b + c * HD + 32 * j + 8 * g))
+                             : u32x4{0, 0, 0, 0};
+        }
+    };
+    auto fetch_v = [&](const Work& x, int ids, int i) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint16_t* b = page_base(x, ids, i, h);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+                vr[h][j] = b ? __builtin_nontemporal_load(
+                                   reinterpret_cast<const u32x4*>(b + vofs + (j * 64 + lane) * 8))
+                             : u32x4{0, 0, 0, 0};
+        }
+    };
+
+    // Each item's first pair is on its way before the item before it is written out.
+    const int n_work = *ts.n_items * H;
+    int work = blockIdx.x;  // the grid has no more workgroups than `items` has room for
+    Work x = load_work(work);
+    if (work >= n_work) return;
+    int ids = page_ids(x, x.p);
+    if (x.mine > 0) {
+        fetch_v(x, ids, 0);
+        fetch_k(x, ids, 0);
+    }
+    while (true) {
+        const int next = work + gridDim.x;
+        const Work x2 = load_work(next < n_work ? next : work);
+        const int ids2 = page_ids(x2, x2.p);
+        const TreeItem& it = x.it;
+        const int head = x.head, nt = x.nt;
         // A segment's record of a row: sums, maximum, weight.  Written through to memory
         // and read past the caches: the workgroups run on XCDs with L2s of their own.
         auto rec = [&](int row, int sg) {
@@ -283,21 +359,9 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
             *reinterpret_cast<uint32_t*>(out + frag_index(row, head * HD + k, d)) =
                 den != 0.f ? pack_bf16(a / den, b / den) : 0u;
         };
-        const uint16_t* pool = kv.pool + kv_offset(kv.layer, 0, kv.n_pages, 0, head, H, 0, HD);
-        const size_t page_elems = kv_offset(0, 1, 1, 0, 0, H, 0, HD);
-
-        // this wave's pages: pairs p, p + 8, ...; lane l holds the id of page l % 2 of its pair l / 2
-        int p = it.p0 + 2 * wave;
-        const int mine = it.p1 > p ? (it.p1 - p + 7) / 8 : 0;
-        auto page_ids = [&](int from) {
-            const int pg = from + (lane >> 1) * 8 + (lane & 1);
-            return pg < it.p1 ? pt[pg] : -2;  // -2: past the context
-        };
-        int ids = page_ids(p);
-
         // q operands: row c of tile t, dims 32j + 8g .. + 7, scaled, hi + lo.  One tile's
-        // stay in each wave's registers; more would cost the loop its second wave per
-        // SIMD (or spill, at four), so all waves read them from LDS.
+        // stay in each wave's registers; two would cost the loop its second wave per
+        // SIMD, so all waves read them from LDS.
         auto q_operand = [&](int t, int j, bf16x8& hi, bf16x8& lo) {
             const int row = it.row0 + min(t * 16 + c, it.n - 1);  // rows past the tile repeat its last one
             const float* src = q + (size_t)row * d + head * HD + 32 * j + 8 * g;
@@ -317,9 +381,10 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
             lo = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], lw[2], lw[3]});
         };
         u32x4* sq = reinterpret_cast<u32x4*>(smem + VBYTES) + lane;
+        const u32x4* sqh = sq + half * NT * NJ * 128;
         bf16x8 qr[2][QLDS ? 1 : NJ];  // hi, lo
         if constexpr (QLDS) {
-            for (int f = wave; f < (nt + GT - 1) / GT * GT * NJ; f += kTreeWaves) {
+            for (int f = wave; f < ROWS / 16 * NJ; f += kTreeWaves * HV) {
                 bf16x8 hi, lo;
                 q_operand(f / NJ, f % NJ, hi, lo);
                 sq[f * 128] = __builtin_bit_cast(u32x4, hi);
@@ -338,56 +403,10 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
             for (int b = 0; b < NB; ++b) st.o[t][b] = floatx4{0.f, 0.f, 0.f, 0.f};
         }
 
-        // The wave's pair i.  K comes as operands (lane = key c, dims 32j + 8g ..), V in
-        // 16-byte pieces as stored.  Where a page is missing (bit h of the pair's
-        // flags clear) the registers are zeros.
-        u32x4 kr[2][NJ], vr[2][NJ];
-        auto page_base = [&](int i, int h) -> const uint16_t* {
-            const int pid = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + h);
-            if (pid < 0 || pid >= kv.n_pages) return nullptr;
-            return pool + (size_t)pid * page_elems;
-        };
-        auto flags = [&](int i) -> int {
-            int there = 0;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int pid = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + h);
-                if (pid >= 0 && pid < kv.n_pages)
-                    there |= 1 << h;
-                else if (pid != -2 && lane == 0)
-                    set_err(err, CDB_DEV_UNMAPPED_PAGE);
-            }
-            return there;
-        };
-        auto fetch_k = [&](int i) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint16_t* b = page_base(i, h);
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-                    kr[h][j] = b ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(b + c * HD + 32 * j + 8 * g))
-                                 : u32x4{0, 0, 0, 0};
-            }
-        };
-        auto fetch_v = [&](int i) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint16_t* b = page_base(i, h);
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-                    vr[h][j] = b ? __builtin_nontemporal_load(
-                                       reinterpret_cast<const u32x4*>(b + vofs + (j * 64 + lane) * 8))
-                                 : u32x4{0, 0, 0, 0};
-            }
-        };
-
-        if (mine > 0) {
-            fetch_v(0);
-            fetch_k(0);
-        }
         if constexpr (QLDS) __syncthreads();
-        for (int i = 0; i < mine; ++i, p += 8) {
-            const int there = flags(i);
+        int p = x.p;
+        for (int i = 0; i < x.mine; ++i, p += 8) {
+            const int ids_i = ids, there = flags(ids, i);
             const bool masked = there != 3 || p * kPage + 2 * kPage > it.base;  // wave-uniform
             bool odd = false;  // a V that is not finite where only some rows may see it
             if (masked) {
@@ -417,10 +436,10 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
                     *reinterpret_cast<u32x4*>(sv + (h * kPage + r) * HD + vpiece<HD>(ch >> 1, r) * 16 + (ch & 1) * 8) =
                         vr[h][j];
                 }
-            const bool more = i + 1 < mine;
+            const bool more = i + 1 < x.mine;
             if (more) {
-                if (((i + 1) & 31) == 0) ids = page_ids(p + 8);
-                fetch_v(i + 1);
+                if (((i + 1) & 31) == 0) ids = page_ids(x, p + 8);
+                fetch_v(x, ids, i + 1);
             }
             // Tiles go in groups of GT, skipped whole past the last used one: a group's
             // products are independent chains that the matrix cores interleave.
@@ -438,7 +457,7 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
                         for (int t = t0; t < t0 + GT; ++t) {
                             bf16x8 b;
                             if constexpr (QLDS)
-                                b = __builtin_bit_cast(bf16x8, sq[(t * NJ + j) * 128 + part * 64]);
+                                b = __builtin_bit_cast(bf16x8, sqh[(t * NJ + j) * 128 + part * 64]);
                             else
                                 b = qr[part][j];
 #pragma unroll
@@ -447,7 +466,7 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
                                                                                   s[t][h], 0, 0, 0);
                         }
             }
-            if (more) fetch_k(i + 1);
+            if (more) fetch_k(x, ids, i + 1);
             // A = V^T: dim 16b + c, keys 4g..4g+3 of both pages; lane c of group g points at key 4g + c/4, dims 4(c%4)..
             const int vk = 4 * g + (c >> 2);
             bf16x8 va[NB];
@@ -470,7 +489,7 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
                 for (int u = 0; u < GT; ++u) {
                     const int t = t0 + u;
                     if (masked) {
-                        const uint64_t mask = tree.mask[it.row0 + min(t * 16 + c, it.n - 1)];
+                        const uint64_t mask = tree.mask[it.row0 + min((half * NT + t) * 16 + c, it.n - 1)];
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const uint32_t see =
@@ -525,7 +544,7 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
                 for (int kk = 0; kk < 2 * kPage; ++kk) {
                     const int off = p * kPage + kk - it.base;
                     if (off < 0 || off >= 64 || !(it.seen >> off & 1) || !(there >> (kk >> 4) & 1)) continue;
-                    const uint16_t* row = pool + (size_t)pt[p + (kk >> 4)] * page_elems + vofs + (kk & 15) * HD;
+                    const uint16_t* row = page_base(x, ids_i, i, kk >> 4) + vofs + (kk & 15) * HD;
                     const int w = (kk >> 4) * 2 + ((kk & 3) >> 1);  // p of key kk: word w, half kk % 2, of lane group kk % 16 / 4
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
@@ -542,7 +561,7 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
                         hw = __shfl(hw, from, 64);
                         lw = __shfl(lw, from, 64);
                         const float pk = kk & 1 ? bfhi(hw) + bfhi(lw) : bflo(hw) + bflo(lw);
-                        const bool see = tree.mask[it.row0 + min(t * 16 + c, it.n - 1)] >> off & 1;
+                        const bool see = tree.mask[it.row0 + min((half * NT + t) * 16 + c, it.n - 1)] >> off & 1;
 #pragma unroll
                         for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -556,8 +575,13 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
             }
         }
 
-        // the four waves' states: [wave][row][dim]
-        __syncthreads();  // every wave is done with its V
+        if (next < n_work && x2.mine > 0) {
+            fetch_v(x2, ids2, 0);
+            fetch_k(x2, ids2, 0);
+        }
+
+        // the waves' states: [page class][row][dim]
+        __syncthreads();  // every wave is done with its V and q
         float* so = reinterpret_cast<float*>(smem);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -565,10 +589,10 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
             const float l = over_rows_sum(st.l[t]);
 #pragma unroll
             for (int b = 0; b < NB; ++b)
-                *reinterpret_cast<floatx4*>(so + (wave * ROWS + t * 16 + c) * PITCH + 16 * b + 4 * g) = st.o[t][b];
+                *reinterpret_cast<floatx4*>(so + (cls * ROWS + (half * NT + t) * 16 + c) * PITCH + 16 * b + 4 * g) = st.o[t][b];
             if (g == 0) {
-                s_m[wave][t * 16 + c] = st.m[t];
-                s_l[wave][t * 16 + c] = l;
+                s_m[cls][(half * NT + t) * 16 + c] = st.m[t];
+                s_l[cls][(half * NT + t) * 16 + c] = l;
             }
         }
         __syncthreads();
@@ -588,7 +612,7 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
         }
         __syncthreads();
         // thread = two dims of a row, so that a wave's stores are one run
-        for (int e = tid; e < it.n * (HD / 2); e += kTreeWaves * 64) {
+        for (int e = tid; e < it.n * (HD / 2); e += THREADS) {
             const int r = e / (HD / 2), k = 2 * (e - r * (HD / 2));
             float a = 0.f, b = 0.f;
 #pragma unroll
@@ -628,7 +652,7 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
                     s_den[tid] = den;
                 }
                 __syncthreads();
-                for (int e = tid; e < it.n * (HD / 2); e += kTreeWaves * 64) {
+                for (int e = tid; e < it.n * (HD / 2); e += THREADS) {
                     const int r = e / (HD / 2), k = 2 * (e - r * (HD / 2));
                     const float* at = rec(it.row0 + r, 0) + k;
                     float a = 0.f, b = 0.f;
@@ -648,45 +672,50 @@ __global__ __launch_bounds__(kTreeWaves * 64, NT == 1 ? 2 : 1) void k_tree_attn(
                 }
             }
         }
+        if (next >= n_work) break;
+        x = x2;
+        ids = ids2;
+        work = next;
         __syncthreads();  // the next item's V takes the place of the states
     }
 }
 
-// 16-row tiles per workgroup
-static int tree_tiles(int max_nodes) { return max_nodes <= 16 ? 1 : max_nodes <= 32 ? 2 : 4; }
+// rows per tile
+static int tree_rows_per_tile(int max_nodes) { return max_nodes <= 16 ? 16 : max_nodes <= 32 ? 32 : 64; }
 
 hipError_t launch_tree_plan(const KvTarget& kv, const int32_t* seq, const cdb_tree& tree, int M, int H, int hd,
                             void* scratch, int* err, hipStream_t st, const int32_t* dn) {
     if (M <= 0) return hipSuccess;
     if (M > kMaxRows) return hipErrorInvalidValue;
-    k_tree_plan<<<1, 256, 0, st>>>(kv, seq, tree, M, H, 16 * tree_tiles(tree.max_nodes),
+    k_tree_plan<<<1, 256, 0, st>>>(kv, seq, tree, M, H, tree_rows_per_tile(tree.max_nodes),
                                    tree_scratch(scratch, H, hd, M), err, dn);
     return hipGetLastError();
 }
 
 template <int HD>
-static void run_tree_attn(int nt, dim3 grid, const float* q, const KvTarget& kv, const cdb_tree& tree, int H,
+static void run_tree_attn(int rows, int most, const float* q, const KvTarget& kv, const cdb_tree& tree, int H,
                           const TreeScratch& ts, uint16_t* out, int* err, hipStream_t st) {
-    if (nt == 1)
-        k_tree_attn<HD, 1><<<grid, kTreeWaves * 64, 0, st>>>(q, kv, tree, H, ts, out, err);
-    else if (nt == 2)
-        k_tree_attn<HD, 2><<<grid, kTreeWaves * 64, 0, st>>>(q, kv, tree, H, ts, out, err);
+    // resident workgroups: two of 4 waves per CU, or one of 8
+    if (rows == 16)
+        k_tree_attn<HD, 1, 1><<<std::min(most, 512), 256, 0, st>>>(q, kv, tree, H, ts, out, err);
+    else if (rows == 32)
+        k_tree_attn<HD, 2, 1><<<std::min(most, 512), 256, 0, st>>>(q, kv, tree, H, ts, out, err);
     else
-        k_tree_attn<HD, 4><<<grid, kTreeWaves * 64, 0, st>>>(q, kv, tree, H, ts, out, err);
+        k_tree_attn<HD, 2, 2><<<std::min(most, 256), 512, 0, st>>>(q, kv, tree, H, ts, out, err);
 }
 
 hipError_t launch_tree_attention(const float* q, const KvTarget& kv, const cdb_tree& tree, int M, int H, int hd,
                                  void* scratch, uint16_t* out, int* err, hipStream_t st) {
     if (M <= 0) return hipSuccess;
     const TreeScratch ts = tree_scratch(scratch, H, hd, M);
-    const int nt = tree_tiles(tree.max_nodes);
-    // as many workgroups as there can be items, up to what is resident at once
-    const int most = std::min(kTreeSegs, std::max(1, (kv.max_pages + 1 + kTreeSegPages - 1) / kTreeSegPages));
-    const dim3 grid(std::min(M * H * most, 256 * (nt == 1 ? 2 : 1)));
+    const int rows = tree_rows_per_tile(tree.max_nodes);
+    // no more workgroups than there can be items
+    const int segs = std::min(kTreeSegs, kv.max_pages / kTreeSegPages + 1);
+    const int most = M * H * segs;
     switch (hd) {
-        case 64: run_tree_attn<64>(nt, grid, q, kv, tree, H, ts, out, err, st); break;
-        case 96: run_tree_attn<96>(nt, grid, q, kv, tree, H, ts, out, err, st); break;
-        case 128: run_tree_attn<128>(nt, grid, q, kv, tree, H, ts, out, err, st); break;
+        case 64: run_tree_attn<64>(rows, most, q, kv, tree, H, ts, out, err, st); break;
+        case 96: run_tree_attn<96>(rows, most, q, kv, tree, H, ts, out, err, st); break;
+        case 128: run_tree_attn<128>(rows, most, q, kv, tree, H, ts, out, err, st); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
