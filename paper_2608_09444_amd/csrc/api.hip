@@ -298,11 +298,13 @@ constexpr int kMaxTablePages = (0x7fffffff - CDB_TREE_MAX_NODES) / kPage;
 
 // tree: NULL for the plain stage calls
 static cdb_status check_tree(const cdb_model* model, const cdb_kv* kv, const cdb_rows* rows, const cdb_tree* tree,
-                             size_t ws_bytes) {
+                             size_t ws_bytes, int stage) {
     if (!tree) return CDB_OK;
     if (tree->max_nodes < 1 || tree->max_nodes > CDB_TREE_MAX_NODES) return CDB_ERR_INVALID_ARG;
     if (rows->n_rows > 0 && (!tree->base || !tree->mask || !tree->rope_pos)) return CDB_ERR_INVALID_ARG;
     if (kv->max_pages > kMaxTablePages) return CDB_ERR_CAPACITY;
+    const KvTarget t = stage_target(model->desc, *kv, stage);
+    if (rows->n_rows > 0 && t.n_layers > 0 && t.n_pages < 1) return CDB_ERR_INVALID_ARG;
     const size_t own = ws_layout(model->desc, rows->n_rows, false).total;
     if (ws_bytes < own + tree_scratch_bytes(model->desc, rows->n_rows)) return CDB_ERR_CAPACITY;
     return CDB_OK;
@@ -376,7 +378,7 @@ cdb_status cdb_workspace_init(void* ws, size_t ws_bytes, hipStream_t st) {
 static cdb_status prelude(const cdb_model* model, const cdb_kv* kv, const cdb_state* state, const cdb_rows* rows,
                           const cdb_tree* tree, const int32_t* tokens, void* ws, size_t ws_bytes, hipStream_t st) {
     cdb_status s = check_common(model, kv, state, rows, ws, ws_bytes, 0);
-    if (s == CDB_OK) s = check_tree(model, kv, rows, tree, ws_bytes);
+    if (s == CDB_OK) s = check_tree(model, kv, rows, tree, ws_bytes, 0);
     if (s != CDB_OK) return s;
     const cdb_model_desc& d = model->desc;
     if (rows->n_rows > 0 && !tokens) return CDB_ERR_INVALID_ARG;
@@ -403,7 +405,7 @@ static cdb_status loop_step(const cdb_model* model, const cdb_kv* kv, const cdb_
                             const cdb_gate* gate, const cdb_step_out* out, void* ws, size_t ws_bytes, hipStream_t st,
                             int* err = nullptr, const cdb_tree* tree = nullptr) {
     cdb_status s = check_common(model, kv, state, rows, ws, ws_bytes, 1);
-    if (s == CDB_OK) s = check_tree(model, kv, rows, tree, ws_bytes);
+    if (s == CDB_OK) s = check_tree(model, kv, rows, tree, ws_bytes, 1);
     if (s != CDB_OK) return s;
     const cdb_model_desc& d = model->desc;
     if (!out || !out->exit_score || !out->exit_mask || !out->cont || !out->exited || !out->counts)
@@ -508,7 +510,7 @@ static cdb_status coda(const cdb_model* model, const cdb_kv* kv, const cdb_state
                        const cdb_tree* tree, float* logits, int32_t* next_ids, void* ws, size_t ws_bytes,
                        hipStream_t st) {
     cdb_status s = check_common(model, kv, state, rows, ws, ws_bytes, 2);
-    if (s == CDB_OK) s = check_tree(model, kv, rows, tree, ws_bytes);
+    if (s == CDB_OK) s = check_tree(model, kv, rows, tree, ws_bytes, 2);
     if (s != CDB_OK) return s;
     const cdb_model_desc& d = model->desc;
     if (!logits || !next_ids) return CDB_ERR_INVALID_ARG;
@@ -705,7 +707,7 @@ cdb_status cdb_tree_attention(const cdb_model_desc* desc, const cdb_kv* kv, cons
     const cdb_status s = check_attention(desc, kv, rows, stage, layer, q, out, ws, ws_bytes,
                                          256 + tree_scratch_bytes(*desc, rows->n_rows), &t);
     if (s != CDB_OK || rows->n_rows == 0) return s;
-    if (!tree->base || !tree->mask || kv->max_seqs < 0 || kv->max_pages < 0) return CDB_ERR_INVALID_ARG;
+    if (!tree->base || !tree->mask || kv->max_seqs < 0 || kv->max_pages < 0 || t.n_pages < 1) return CDB_ERR_INVALID_ARG;
     if (kv->max_pages > kMaxTablePages) return CDB_ERR_CAPACITY;
     void* scratch = static_cast<unsigned char*>(ws) + 256;
     int* err = static_cast<int*>(ws);

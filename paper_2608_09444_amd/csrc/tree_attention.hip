@@ -249,7 +249,6 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
     constexpr int ROWS = 16 * NT * HV, THREADS = kTreeWaves * 64 * HV;
     constexpr int REC = HD + 2;
     constexpr bool QLDS = NT > 1;
-    constexpr int GT = NT > 1 ? 2 : 1;
     // V of the waves' pairs, then the q operands; the waves' states take their place
     constexpr int VBYTES = kTreeWaves * HV * 2 * kPage * HD * 2, QBYTES = QLDS ? NT * HV * NJ * 2 * 1024 : 0;
     constexpr int OBYTES = kTreeWaves * ROWS * PITCH * 4;
@@ -262,7 +261,6 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
     const int c = lane & 15, g = lane >> 4;
     const int d = H * HD;
     const float qscale = 1.4426950408889634f / sqrtf((float)HD);
-    const size_t vofs = (size_t)H * kPage * HD, page_elems = 2 * vofs;
     uint16_t* sv = reinterpret_cast<uint16_t*>(smem) + wave * 2 * kPage * HD;
 
     auto load_work = [&](int w) {
@@ -281,47 +279,37 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
         return pg < x.it.p1 ? kv.page_table[((size_t)x.it.seq * kv.n_planes + x.it.plane) * kv.max_pages + pg]
                             : -2;  // past the context
     };
-    // The wave's pair i.  K comes as operands (lane = key c, dims 32j + 8g ..), V in
-    // 16-byte pieces as stored.  Where a page is missing (bit h of the pair's
-    // flags clear) the registers are zeros.
+    // The wave's pair i: whether its pages are there (bits 0, 1), and where they are.
+    // A missing page's loads go to one that exists; what they bring is masked.
+    struct Pair {
+        int there;
+        const uint16_t* at[2];
+    };
+    auto pair_of = [&](const Work& x, int ids, int i) {
+        const int p0 = __builtin_amdgcn_readlane(ids, 2 * (i & 31)), p1 = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + 1);
+        const bool ok0 = p0 >= 0 && p0 < kv.n_pages, ok1 = p1 >= 0 && p1 < kv.n_pages;
+        const int q0 = ok0 ? p0 : 0, q1 = ok1 ? p1 : q0;
+        if (((!ok0 && p0 != -2) || (!ok1 && p1 != -2)) && lane == 0) set_err(err, CDB_DEV_UNMAPPED_PAGE);
+        return Pair{(ok0 ? 1 : 0) | (ok1 ? 2 : 0),
+                    {kv.pool + kv_offset(kv.layer, q0, kv.n_pages, 0, x.head, H, 0, HD),
+                     kv.pool + kv_offset(kv.layer, q1, kv.n_pages, 0, x.head, H, 0, HD)}};
+    };
+    // K comes as operands (lane = key c, dims 32j + 8g ..), V in 16-byte pieces as stored
     u32x4 kr[2][NJ], vr[2][NJ];
-    auto page_base = [&](const Work& x, int ids, int i, int h) -> const uint16_t* {
-        const int pid = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + h);
-        if (pid < 0 || pid >= kv.n_pages) return nullptr;
-        return kv.pool + kv_offset(kv.layer, pid, kv.n_pages, 0, x.head, H, 0, HD);
-    };
-    auto flags = [&](int ids, int i) -> int {
-        int there = 0;
+    const int k_at = c * HD + 8 * g, v_at = H * kPage * HD + lane * 8;
+    auto fetch_k = [&](const Pair& x) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int pid = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + h);
-            if (pid >= 0 && pid < kv.n_pages)
-                there |= 1 << h;
-            else if (pid != -2 && lane == 0)
-                set_err(err, CDB_DEV_UNMAPPED_PAGE);
-        }
-        return there;
-    };
-    auto fetch_k = [&](const Work& x, int ids, int i) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint16_t* b = page_base(x, ids, i, h);
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
-                kr[h][j] = b ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(b + c * HD + 32 * j + 8 * g))
-                             : u32x4{0, 0, 0, 0};
-        }
+                kr[h][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x.at[h] + k_at + 32 * j));
     };
-    auto fetch_v = [&](const Work& x, int ids, int i) {
+    auto fetch_v = [&](const Pair& x) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint16_t* b = page_base(x, ids, i, h);
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
-                vr[h][j] = b ? __builtin_nontemporal_load(
-                                   reinterpret_cast<const u32x4*>(b + vofs + (j * 64 + lane) * 8))
-                             : u32x4{0, 0, 0, 0};
-        }
+                vr[h][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x.at[h] + v_at + 512 * j));
     };
 
     // Each item's first pair is on its way before the item before it is written out.
@@ -330,9 +318,11 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
     Work x = load_work(work);
     if (work >= n_work) return;
     int ids = page_ids(x, x.p);
+    Pair pair{};
     if (x.mine > 0) {
-        fetch_v(x, ids, 0);
-        fetch_k(x, ids, 0);
+        pair = pair_of(x, ids, 0);
+        fetch_v(pair);
+        fetch_k(pair);
     }
     while (true) {
         const int next = work + gridDim.x;
@@ -406,7 +396,8 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
         if constexpr (QLDS) __syncthreads();
         int p = x.p;
         for (int i = 0; i < x.mine; ++i, p += 8) {
-            const int ids_i = ids, there = flags(ids, i);
+            const Pair now = pair;
+            const int there = now.there;
             const bool masked = there != 3 || p * kPage + 2 * kPage > it.base;  // wave-uniform
             bool odd = false;  // a V that is not finite where only some rows may see it
             if (masked) {
@@ -415,7 +406,7 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
 #pragma unroll
                     for (int j = 0; j < NJ; ++j) {
                         const int off = (p + h) * kPage + (j * 64 + lane) / CPR - it.base;
-                        const uint32_t keep = sees4(it.seen, off) & 1 ? ~0u : 0u;
+                        const uint32_t keep = (there >> h & 1) && (sees4(it.seen, off) & 1) ? ~0u : 0u;
                         const uint32_t part = off < 0 ? 0u : ~0u;  // committed positions: every row sees them
                         u32x4 x = vr[h][j] & keep;
 #pragma unroll
@@ -439,34 +430,33 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
             const bool more = i + 1 < x.mine;
             if (more) {
                 if (((i + 1) & 31) == 0) ids = page_ids(x, p + 8);
-                fetch_v(x, ids, i + 1);
+                pair = pair_of(x, ids, i + 1);
+                fetch_v(pair);
             }
-            // Tiles go in groups of GT, skipped whole past the last used one: a group's
-            // products are independent chains that the matrix cores interleave.
             floatx4 s[NT][2];
 #pragma unroll
-            for (int t0 = 0; t0 < NT; t0 += GT) {
-                if (t0 >= nt) continue;
+            for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int t = t0; t < t0 + GT; ++t) s[t][0] = s[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+            for (int part = 1; part >= 0; --part) {
+                bf16x8 b[NT][NJ];
 #pragma unroll
-                for (int part = 1; part >= 0; --part)
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int j = 0; j < NJ; ++j)
+                        if constexpr (QLDS)
+                            b[t][j] = __builtin_bit_cast(bf16x8, sqh[(t * NJ + j) * 128 + part * 64]);
+                        else
+                            b[t][j] = qr[part][j];
 #pragma unroll
-                        for (int t = t0; t < t0 + GT; ++t) {
-                            bf16x8 b;
-                            if constexpr (QLDS)
-                                b = __builtin_bit_cast(bf16x8, sqh[(t * NJ + j) * 128 + part * 64]);
-                            else
-                                b = qr[part][j];
+                for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                            for (int h = 0; h < 2; ++h)
-                                s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][j]), b,
-                                                                                  s[t][h], 0, 0, 0);
-                        }
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][j]), b[t][j],
+                                                                              s[t][h], 0, 0, 0);
             }
-            if (more) fetch_k(x, ids, i + 1);
+            if (more) fetch_k(pair);
             // A = V^T: dim 16b + c, keys 4g..4g+3 of both pages; lane c of group g points at key 4g + c/4, dims 4(c%4)..
             const int vk = 4 * g + (c >> 2);
             bf16x8 va[NB];
@@ -479,72 +469,68 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
                                                                (__attribute__((address_space(3))) s16x4*)(at + kPage * HD)));
                 va[b] = __builtin_bit_cast(bf16x8, u32x4{w0.x, w0.y, w1.x, w1.y});
             }
+            // The maximum that weights are taken against follows the row's own once it has
+            // fallen 8 behind (weights stay below 2^8), so most pairs rescale nothing.
             bf16x8 ph[NT], pl[NT];
+            bool up[NT], any_up = false;
+            float mx[NT];
 #pragma unroll
-            for (int t0 = 0; t0 < NT; t0 += GT) {
-                if (t0 >= nt) continue;
-                float mx[GT];
-                bool up = false;
+            for (int t = 0; t < NT; ++t) {
+                if (masked) {
+                    const uint64_t mask = tree.mask[it.row0 + min((half * NT + t) * 16 + c, it.n - 1)];
 #pragma unroll
-                for (int u = 0; u < GT; ++u) {
-                    const int t = t0 + u;
-                    if (masked) {
-                        const uint64_t mask = tree.mask[it.row0 + min((half * NT + t) * 16 + c, it.n - 1)];
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t see = sees4(mask, (p + h) * kPage + 4 * g - it.base) & (there >> h & 1 ? 15u : 0u);
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const uint32_t see =
-                                sees4(mask, (p + h) * kPage + 4 * g - it.base) & (there >> h & 1 ? 15u : 0u);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) s[t][h][e] = see >> e & 1 ? s[t][h][e] : -INFINITY;
-                        }
-                    }
-                    mx[u] = st.m[t];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) mx[u] = fmaxf(mx[u], s[t][e >> 2][e & 3]);
-                    mx[u] = over_rows_max(mx[u]);
-                    up |= mx[u] > st.m[t];
-                }
-                if (__any(up)) {
-#pragma unroll
-                    for (int u = 0; u < GT; ++u) {
-                        const int t = t0 + u;
-                        const float corr = exp2_raw(st.m[t] - mx[u]);
-                        st.l[t] *= corr;
-#pragma unroll
-                        for (int b = 0; b < NB; ++b) st.o[t][b] *= corr;
-                        st.m[t] = mx[u];
+                        for (int e = 0; e < 4; ++e) s[t][h][e] = see >> e & 1 ? s[t][h][e] : -INFINITY;
                     }
                 }
+                mx[t] = fmaxf(s[t][0][0], s[t][0][1]);
 #pragma unroll
-                for (int u = 0; u < GT; ++u) {
-                    const int t = t0 + u;
-                    uint32_t hw[4], lw[4];
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const float p0 = exp2_raw(s[t][e >> 2][e & 3] - mx[u]);
-                        const float p1 = exp2_raw(s[t][e >> 2][(e & 3) + 1] - mx[u]);
-                        st.l[t] += p0 + p1;
-                        const uint32_t hi = pack_bf16(p0, p1);
-                        hw[e / 2] = hi;
-                        lw[e / 2] = pack_bf16(p0 - bflo(hi), p1 - bfhi(hi));
-                    }
-                    ph[t] = __builtin_bit_cast(bf16x8, u32x4{hw[0], hw[1], hw[2], hw[3]});
-                    pl[t] = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], lw[2], lw[3]});
-                }
-#pragma unroll
-                for (int part = 1; part >= 0; --part)
-#pragma unroll
-                    for (int b = 0; b < NB; ++b)
-#pragma unroll
-                        for (int t = t0; t < t0 + GT; ++t)
-                            st.o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[b], part ? pl[t] : ph[t], st.o[t][b], 0,
-                                                                                 0, 0);
+                for (int e = 2; e < 8; ++e) mx[t] = fmaxf(mx[t], s[t][e >> 2][e & 3]);
+                mx[t] = over_rows_max(mx[t]);
+                up[t] = mx[t] > st.m[t] + 8.f;
+                any_up |= up[t];
             }
+            if (__any(any_up)) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const float m = up[t] ? mx[t] : st.m[t];
+                    const float corr = up[t] ? exp2_raw(st.m[t] - m) : 1.f;
+                    st.l[t] *= corr;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) st.o[t][b] *= corr;
+                    st.m[t] = m;
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                uint32_t hw[4], lw[4];
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float p0 = exp2_raw(s[t][e >> 2][e & 3] - st.m[t]);
+                    const float p1 = exp2_raw(s[t][e >> 2][(e & 3) + 1] - st.m[t]);
+                    st.l[t] += p0 + p1;
+                    const uint32_t hi = pack_bf16(p0, p1);
+                    hw[e / 2] = hi;
+                    lw[e / 2] = pack_bf16(p0 - bflo(hi), p1 - bfhi(hi));
+                }
+                ph[t] = __builtin_bit_cast(bf16x8, u32x4{hw[0], hw[1], hw[2], hw[3]});
+                pl[t] = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], lw[2], lw[3]});
+            }
+#pragma unroll
+            for (int part = 1; part >= 0; --part)
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        st.o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[b], part ? pl[t] : ph[t], st.o[t][b], 0, 0,
+                                                                             0);
             if (masked && __any(odd)) {  // rare: the values taken out above, to the rows that see them
                 for (int kk = 0; kk < 2 * kPage; ++kk) {
                     const int off = p * kPage + kk - it.base;
                     if (off < 0 || off >= 64 || !(it.seen >> off & 1) || !(there >> (kk >> 4) & 1)) continue;
-                    const uint16_t* row = page_base(x, ids_i, i, kk >> 4) + vofs + (kk & 15) * HD;
+                    const uint16_t* row = (kk < kPage ? now.at[0] : now.at[1]) + H * kPage * HD + (kk & 15) * HD;
                     const int w = (kk >> 4) * 2 + ((kk & 3) >> 1);  // p of key kk: word w, half kk % 2, of lane group kk % 16 / 4
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
@@ -576,8 +562,9 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
         }
 
         if (next < n_work && x2.mine > 0) {
-            fetch_v(x2, ids2, 0);
-            fetch_k(x2, ids2, 0);
+            pair = pair_of(x2, ids2, 0);
+            fetch_v(pair);
+            fetch_k(pair);
         }
 
         // the waves' states: [page class][row][dim]

@@ -131,7 +131,8 @@ def test_tree_attention_refusals():
                {"t": tree.cdb_tree(8, 1, None, 1)}, {"stage": 3}, {"stage": -1}, {"layer": 2}, {"layer": -1},
                {"rows": cdb.cdb_rows(-1, 1, 1, 1, 1)}, {"rows": cdb.cdb_rows(8, 1, None, 1, 1)},
                {"rows": cdb.cdb_rows(8, 1, 1, 1, None)}, {"kv": cdb.cdb_kv(1, None, 1, 1, 1, 1, 1, 4, 8)},
-               {"kv": cdb.cdb_kv(1, 1, 1, 1, 1, 1, None, 4, 8)}, {"kv": cdb.cdb_kv(1, 1, 1, 1, 1, 1, 1, -4, 8)}):
+               {"kv": cdb.cdb_kv(1, 1, 1, 1, 1, 1, None, 4, 8)}, {"kv": cdb.cdb_kv(1, 1, 1, 1, 1, 1, 1, -4, 8)},
+               {"kv": cdb.cdb_kv(1, 1, 1, 1, 0, 1, 1, 4, 8)}):
         assert call(**kw) == INVALID, kw
     assert call(desc=BAD_DESC) == UNSUPPORTED
     assert call(rows=cdb.cdb_rows(cdb.MAX_ROWS + 1, 1, 1, 1, 1)) == CAPACITY
@@ -157,6 +158,7 @@ def test_tree_stage_refusals():
         assert calls(t) == [INVALID] * 3
     assert calls(good, nb=cdb.cdb_workspace_bytes(DESC, 1)) == [CAPACITY] * 3
     assert calls(good, kv=cdb.cdb_kv(1, 1, 1, 1, 1, 1, 1, 4, 1 << 28)) == [CAPACITY] * 3
+    assert calls(good, kv=cdb.cdb_kv(1, 1, 1, 0, 0, 0, 1, 4, 8)) == [INVALID] * 3
     bad = cdb.cdb_gate(0.5, 1, None)
     assert _status("cdb_tree_step", model, kv, state, rows, good, bad, out, 1, nb, None) == INVALID
 
