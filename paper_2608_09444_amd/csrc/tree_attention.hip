@@ -41,17 +41,19 @@
 
 namespace cdb {
 
-constexpr int kTreeWaves = 4;
+constexpr int kTreeWaves = 8;
 constexpr int kTreeSegs = 16;  // most segments of a context
+constexpr int kTreeRows = 32;  // most rows of a workgroup
 
-constexpr int kTreeSegPages = 64;  // pages of a segment, unless that makes too many
+constexpr int kTreeSegPages = 128;  // pages of a segment, unless that makes too many
 
 // Segments of a context whose last committed position is on page npg - 1, and the
 // pages of each (the last one has the rest).
 __host__ __device__ __forceinline__ int tree_segments(int npg, int* pages) {
     int n = (npg + kTreeSegPages - 1) / kTreeSegPages;
     n = n > kTreeSegs ? kTreeSegs : n;
-    *pages = (npg + 8 * n - 1) / (8 * n) * 8;
+    constexpr int round = 2 * kTreeWaves;  // the waves' pairs
+    *pages = (npg + round * n - 1) / (round * n) * round;
     return (npg + *pages - 1) / *pages;
 }
 
@@ -61,14 +63,14 @@ struct TreeItem {
     int base;
     int seq, plane;
     int p0, p1;          // the segment's pages
-    int seg, nseg, tile;
-    int pad[4];
+    int seg, nseg;
+    int pad[5];
 };
 
 struct TreeScratch {
     int* n_items;
     TreeItem* items;  // [rows][kTreeSegs]
-    int* arrive;      // [rows][H], zero between launches
+    int* arrive;      // [rows][H], by a workgroup's first row, zero between launches
     float* part;      // [rows][H][kTreeSegs][hd + 2]: sums, maximum, weight
     size_t bytes;
 };
@@ -79,7 +81,7 @@ static TreeScratch tree_scratch(void* at, int H, int hd, int rows) {
     TreeScratch t{};
     t.n_items = reinterpret_cast<int*>(p);
     t.items = reinterpret_cast<TreeItem*>(p + off);
-    off = up(off + (size_t)rows * kTreeSegs * sizeof(TreeItem));
+    off = up(off + ((size_t)rows * kTreeSegs + 8) * sizeof(TreeItem));  // 8: read, not used, past the last
     t.arrive = reinterpret_cast<int*>(p + off);
     off = up(off + (size_t)rows * H * 4);
     t.part = reinterpret_cast<float*>(p + off);
@@ -98,7 +100,7 @@ __global__ __launch_bounds__(256) void k_tree_plan(KvTarget kv, const int32_t* _
                                                    const int32_t* __restrict__ dn) {
     __shared__ int s_seq[256], s_plane[256], s_base[256];
     __shared__ uint64_t s_mask[256];
-    __shared__ uint64_t s_run[4], s_tile[4], s_end[4];  // by row: a run starts; a tile starts; a tile or a skipped row starts
+    __shared__ uint64_t s_run[4], s_end[4];  // by row: a run starts; a tile or a skipped row starts
     __shared__ int s_sum[4];
     const int i = threadIdx.x, lane = i & 63, w = i >> 6;
     const int n = live_rows(dn, M);
@@ -134,14 +136,9 @@ __global__ __launch_bounds__(256) void k_tree_plan(KvTarget kv, const int32_t* _
         if (b) start = word * 64 + 63 - __clzll((long long)b);
     }
     const bool first = ok && (i - start) % cap == 0;
-    const uint64_t firsts = __ballot(first), ends = __ballot(first || !ok);
-    if (lane == 0) {
-        s_tile[w] = firsts;
-        s_end[w] = ends;
-    }
+    const uint64_t ends = __ballot(first || !ok);
+    if (lane == 0) s_end[w] = ends;
     __syncthreads();
-    int tile = __popcll(firsts & ((1ull << lane) - 1));
-    for (int k = 0; k < w; ++k) tile += __popcll(s_tile[k]);
     int nseg = 0, rows = 0, npg = 0, sp = 0;
     uint64_t seen = 0;
     if (first) {
@@ -182,11 +179,11 @@ __global__ __launch_bounds__(256) void k_tree_plan(KvTarget kv, const int32_t* _
         it.p1 = sg == nseg - 1 ? npg : (sg + 1) * sp;
         it.seg = sg;
         it.nseg = nseg;
-        it.tile = tile;
         ts.items[at + sg] = it;
     }
     if (nseg > 1)
-        for (int h = 0; h < H; ++h) ts.arrive[tile * H + h] = 0;
+        for (int r = 0; r < rows; r += kTreeRows)
+            for (int h = 0; h < H; ++h) ts.arrive[(i + r) * H + h] = 0;
 }
 
 // ------------------------------------------------------------------ attention
@@ -229,10 +226,20 @@ __device__ __forceinline__ int vpiece(int b, int r) {
     return s == 6 ? 0 : s;
 }
 
+// K of a page in LDS: key row r holds its 16-byte piece ch at place kpiece(ch, r),
+// so that 16 rows read at one piece lie on different banks.
+template <int HD>
+__device__ __forceinline__ int kpiece(int ch, int r) {
+    if constexpr (HD == 128) return ch ^ r;
+    if constexpr (HD == 64) return ch ^ (r >> 1);
+    const int s = ch + (r >> 2);  // 96: 12 pieces a row
+    return s >= 12 ? s - 12 : s;
+}
+
 struct Work {
-    TreeItem it;
+    TreeItem it;     // row0, n: this workgroup's rows
     int head;
-    int p, mine, nt;
+    int p, mine;     // this wave's first page, and how many pairs of pages it has
 };
 
 template <int HD, int NT>
@@ -241,42 +248,48 @@ struct TreeState {
     float m[NT], l[NT];  // l: this lane's keys only
 };
 
-template <int HD, int NT, int HV>
-__global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
+template <int HD, int NT, bool HALVES>
+__global__ __launch_bounds__(kTreeWaves * 64) void k_tree_attn(
     const float* __restrict__ q, KvTarget kv, cdb_tree tree, int H, TreeScratch ts, uint16_t* __restrict__ out, int* err) {
     constexpr int NJ = HD / 32, NB = HD / 16, CPR = HD / 8;  // K steps, dim blocks, 16-byte pieces of a row
     constexpr int PITCH = HD + 4;
-    constexpr int ROWS = 16 * NT * HV, THREADS = kTreeWaves * 64 * HV;
+    constexpr int ROWS = 16 * NT, THREADS = kTreeWaves * 64;
     constexpr int REC = HD + 2;
     constexpr bool QLDS = NT > 1;
-    // V of the waves' pairs, then the q operands; the waves' states take their place
-    constexpr int VBYTES = kTreeWaves * HV * 2 * kPage * HD * 2, QBYTES = QLDS ? NT * HV * NJ * 2 * 1024 : 0;
+    // K and V of the waves' pairs, then the q operands; the waves' states take their place
+    constexpr int VBYTES = kTreeWaves * 4 * kPage * HD * 2, QBYTES = QLDS ? NT * NJ * 2 * 1024 : 0;
     constexpr int OBYTES = kTreeWaves * ROWS * PITCH * 4;
     __shared__ __align__(16) unsigned char smem[VBYTES + QBYTES > OBYTES ? VBYTES + QBYTES : OBYTES];
     __shared__ float s_m[kTreeWaves][ROWS], s_l[kTreeWaves][ROWS], s_f[kTreeWaves][ROWS], s_den[ROWS];
     __shared__ float s_fs[kTreeSegs][ROWS];
     __shared__ int s_last;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int cls = wave % kTreeWaves, half = wave / kTreeWaves;
     const int c = lane & 15, g = lane >> 4;
     const int d = H * HD;
     const float qscale = 1.4426950408889634f / sqrtf((float)HD);
-    uint16_t* sv = reinterpret_cast<uint16_t*>(smem) + wave * 2 * kPage * HD;
+    uint16_t* sk = reinterpret_cast<uint16_t*>(smem) + wave * 4 * kPage * HD;
+    uint16_t* sv = sk + 2 * kPage * HD;
 
+    // Work w: with two halves, workgroups 8 apart, which run on one XCD at one time,
+    // take the halves of a tile's rows, so that the second one's K and V come from
+    // that XCD's L2.
+    const int n_heads = *ts.n_items * H;  // items x heads
+    const int n_work = !HALVES ? n_heads : (n_heads + 7) / 8 * 16;
     auto load_work = [&](int w) {
+        const int ih = !HALVES ? w : w / 16 * 8 + w % 8, r = !HALVES ? 0 : w / 8 % 2 * kTreeRows;
         Work x;
-        x.it = ts.items[w / H];
-        x.head = w % H;
-        x.p = x.it.p0 + 2 * cls;
-        // 16-row tiles of this wave's half in use, and its pages: pairs p, p + 8, ...
-        x.nt = min(max((x.it.n + 15) / 16 - half * NT, 0), NT);
-        x.mine = x.nt > 0 && x.it.p1 > x.p ? (x.it.p1 - x.p + 7) / 8 : 0;
+        x.it = ts.items[ih / H];
+        x.head = ih % H;
+        x.it.row0 += r;
+        x.it.n = ih < n_heads ? min(x.it.n - r, ROWS) : 0;  // at most 0: no rows
+        x.p = x.it.p0 + 2 * wave;
+        x.mine = x.it.n > 0 && x.it.p1 > x.p ? (x.it.p1 - x.p + 2 * kTreeWaves - 1) / (2 * kTreeWaves) : 0;
         return x;
     };
     // lane l: the id of page l % 2 of pair l / 2 from page `from` on
     auto page_ids = [&](const Work& x, int from) {
-        const int pg = from + (lane >> 1) * 8 + (lane & 1);
-        return pg < x.it.p1 ? kv.page_table[((size_t)x.it.seq * kv.n_planes + x.it.plane) * kv.max_pages + pg]
+        const int pg = from + (lane >> 1) * (2 * kTreeWaves) + (lane & 1);
+        return x.mine > 0 && pg < x.it.p1 ? kv.page_table[((size_t)x.it.seq * kv.n_planes + x.it.plane) * kv.max_pages + pg]
                             : -2;  // past the context
     };
     // The wave's pair i: whether its pages are there (bits 0, 1), and where they are.
@@ -294,26 +307,27 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
                     {kv.pool + kv_offset(kv.layer, q0, kv.n_pages, 0, x.head, H, 0, HD),
                      kv.pool + kv_offset(kv.layer, q1, kv.n_pages, 0, x.head, H, 0, HD)}};
     };
-    // K comes as operands (lane = key c, dims 32j + 8g ..), V in 16-byte pieces as stored
-    u32x4 kr[2][NJ], vr[2][NJ];
-    const int k_at = c * HD + 8 * g, v_at = H * kPage * HD + lane * 8;
-    auto fetch_k = [&](const Pair& x) {
+    // A pair's K and V, in 16-byte pieces as stored.  Each is read once by one
+    // workgroup (past the caches' normal allocation), with halves by two.
+    typedef u32x4 PairRegs[2][NJ];
+    PairRegs kr, vr;
+    const int v_at = H * kPage * HD;
+    auto fetch = [&](const Pair& x) {
+        auto load = [](const uint16_t* at) {
+            const u32x4* a = reinterpret_cast<const u32x4*>(at);
+            return HALVES ? *a : __builtin_nontemporal_load(a);
+        };
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
-                kr[h][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x.at[h] + k_at + 32 * j));
-    };
-    auto fetch_v = [&](const Pair& x) {
+            for (int j = 0; j < NJ; ++j) kr[h][j] = load(x.at[h] + (j * 64 + lane) * 8);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
-                vr[h][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x.at[h] + v_at + 512 * j));
+            for (int j = 0; j < NJ; ++j) vr[h][j] = load(x.at[h] + v_at + (j * 64 + lane) * 8);
     };
 
     // Each item's first pair is on its way before the item before it is written out.
-    const int n_work = *ts.n_items * H;
     int work = blockIdx.x;  // the grid has no more workgroups than `items` has room for
     Work x = load_work(work);
     if (work >= n_work) return;
@@ -321,15 +335,14 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
     Pair pair{};
     if (x.mine > 0) {
         pair = pair_of(x, ids, 0);
-        fetch_v(pair);
-        fetch_k(pair);
+        fetch(pair);
     }
     while (true) {
         const int next = work + gridDim.x;
         const Work x2 = load_work(next < n_work ? next : work);
         const int ids2 = page_ids(x2, x2.p);
         const TreeItem& it = x.it;
-        const int head = x.head, nt = x.nt;
+        const int head = x.head;
         // A segment's record of a row: sums, maximum, weight.  Written through to memory
         // and read past the caches: the workgroups run on XCDs with L2s of their own.
         auto rec = [&](int row, int sg) {
@@ -371,10 +384,9 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
             lo = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], lw[2], lw[3]});
         };
         u32x4* sq = reinterpret_cast<u32x4*>(smem + VBYTES) + lane;
-        const u32x4* sqh = sq + half * NT * NJ * 128;
         bf16x8 qr[2][QLDS ? 1 : NJ];  // hi, lo
         if constexpr (QLDS) {
-            for (int f = wave; f < ROWS / 16 * NJ; f += kTreeWaves * HV) {
+            for (int f = wave; f < NT * NJ && it.n > 0; f += kTreeWaves) {
                 bf16x8 hi, lo;
                 q_operand(f / NJ, f % NJ, hi, lo);
                 sq[f * 128] = __builtin_bit_cast(u32x4, hi);
@@ -382,7 +394,8 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) q_operand(0, j, qr[0][j], qr[1][j]);
+            for (int j = 0; j < NJ; ++j)
+                if (it.n > 0) q_operand(0, j, qr[0][j], qr[1][j]);
         }
         TreeState<HD, NT> st;
 #pragma unroll
@@ -395,7 +408,7 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
 
         if constexpr (QLDS) __syncthreads();
         int p = x.p;
-        for (int i = 0; i < x.mine; ++i, p += 8) {
+        for (int i = 0; i < x.mine; ++i, p += 2 * kTreeWaves) {
             const Pair now = pair;
             const int there = now.there;
             const bool masked = there != 3 || p * kPage + 2 * kPage > it.base;  // wave-uniform
@@ -424,15 +437,23 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) {
                     const int f = j * 64 + lane, r = f / CPR, ch = f - r * CPR;
+                    *reinterpret_cast<u32x4*>(sk + (h * kPage + r) * HD + kpiece<HD>(ch, r) * 8) = kr[h][j];
                     *reinterpret_cast<u32x4*>(sv + (h * kPage + r) * HD + vpiece<HD>(ch >> 1, r) * 16 + (ch & 1) * 8) =
                         vr[h][j];
                 }
             const bool more = i + 1 < x.mine;
             if (more) {
-                if (((i + 1) & 31) == 0) ids = page_ids(x, p + 8);
+                if (((i + 1) & 31) == 0) ids = page_ids(x, p + 2 * kTreeWaves);
                 pair = pair_of(x, ids, i + 1);
-                fetch_v(pair);
+                fetch(pair);
             }
+            // A = K: key c of either page, dims 32j + 8g ..
+            bf16x8 ka[2][NJ];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+                    ka[h][j] = *reinterpret_cast<const bf16x8*>(sk + (h * kPage + c) * HD + kpiece<HD>(4 * j + g, c) * 8);
             floatx4 s[NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -444,7 +465,7 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
 #pragma unroll
                     for (int j = 0; j < NJ; ++j)
                         if constexpr (QLDS)
-                            b[t][j] = __builtin_bit_cast(bf16x8, sqh[(t * NJ + j) * 128 + part * 64]);
+                            b[t][j] = __builtin_bit_cast(bf16x8, sq[(t * NJ + j) * 128 + part * 64]);
                         else
                             b[t][j] = qr[part][j];
 #pragma unroll
@@ -453,10 +474,8 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
-                            s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][j]), b[t][j],
-                                                                              s[t][h], 0, 0, 0);
+                            s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[h][j], b[t][j], s[t][h], 0, 0, 0);
             }
-            if (more) fetch_k(pair);
             // A = V^T: dim 16b + c, keys 4g..4g+3 of both pages; lane c of group g points at key 4g + c/4, dims 4(c%4)..
             const int vk = 4 * g + (c >> 2);
             bf16x8 va[NB];
@@ -477,7 +496,7 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 if (masked) {
-                    const uint64_t mask = tree.mask[it.row0 + min((half * NT + t) * 16 + c, it.n - 1)];
+                    const uint64_t mask = tree.mask[it.row0 + min(t * 16 + c, it.n - 1)];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const uint32_t see = sees4(mask, (p + h) * kPage + 4 * g - it.base) & (there >> h & 1 ? 15u : 0u);
@@ -534,7 +553,6 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
                     const int w = (kk >> 4) * 2 + ((kk & 3) >> 1);  // p of key kk: word w, half kk % 2, of lane group kk % 16 / 4
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        if (t >= nt) continue;
                         const u32x4 h4 = __builtin_bit_cast(u32x4, ph[t]), l4 = __builtin_bit_cast(u32x4, pl[t]);
                         uint32_t hw = 0, lw = 0;
 #pragma unroll
@@ -547,7 +565,7 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
                         hw = __shfl(hw, from, 64);
                         lw = __shfl(lw, from, 64);
                         const float pk = kk & 1 ? bfhi(hw) + bfhi(lw) : bflo(hw) + bflo(lw);
-                        const bool see = tree.mask[it.row0 + min((half * NT + t) * 16 + c, it.n - 1)] >> off & 1;
+                        const bool see = tree.mask[it.row0 + min(t * 16 + c, it.n - 1)] >> off & 1;
 #pragma unroll
                         for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -560,11 +578,9 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
                 }
             }
         }
-
         if (next < n_work && x2.mine > 0) {
             pair = pair_of(x2, ids2, 0);
-            fetch_v(pair);
-            fetch_k(pair);
+            fetch(pair);
         }
 
         // the waves' states: [page class][row][dim]
@@ -572,14 +588,13 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
         float* so = reinterpret_cast<float*>(smem);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            if (t >= nt) continue;
             const float l = over_rows_sum(st.l[t]);
 #pragma unroll
             for (int b = 0; b < NB; ++b)
-                *reinterpret_cast<floatx4*>(so + (cls * ROWS + (half * NT + t) * 16 + c) * PITCH + 16 * b + 4 * g) = st.o[t][b];
+                *reinterpret_cast<floatx4*>(so + (wave * ROWS + t * 16 + c) * PITCH + 16 * b + 4 * g) = st.o[t][b];
             if (g == 0) {
-                s_m[cls][(half * NT + t) * 16 + c] = st.m[t];
-                s_l[cls][(half * NT + t) * 16 + c] = l;
+                s_m[wave][t * 16 + c] = st.m[t];
+                s_l[wave][t * 16 + c] = l;
             }
         }
         __syncthreads();
@@ -613,11 +628,11 @@ __global__ __launch_bounds__(kTreeWaves * 64 * HV, 2) void k_tree_attn(
             else
                 put2(rec(it.row0 + r, it.seg) + k, a, b);
         }
-        if (it.nseg > 1) {
+        if (it.nseg > 1 && it.n > 0) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the wave's records have reached memory
             __syncthreads();
             if (tid == 0) {
-                int* a = ts.arrive + it.tile * H + head;
+                int* a = ts.arrive + it.row0 * H + head;
                 s_last = __hip_atomic_fetch_add(a, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == it.nseg - 1;
                 if (s_last) __hip_atomic_store(a, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
@@ -682,13 +697,14 @@ hipError_t launch_tree_plan(const KvTarget& kv, const int32_t* seq, const cdb_tr
 template <int HD>
 static void run_tree_attn(int rows, int most, const float* q, const KvTarget& kv, const cdb_tree& tree, int H,
                           const TreeScratch& ts, uint16_t* out, int* err, hipStream_t st) {
-    // resident workgroups: two of 4 waves per CU, or one of 8
+    // one resident workgroup of 8 waves per CU
     if (rows == 16)
-        k_tree_attn<HD, 1, 1><<<std::min(most, 512), 256, 0, st>>>(q, kv, tree, H, ts, out, err);
+        k_tree_attn<HD, 1, false><<<std::min(most, 256), kTreeWaves * 64, 0, st>>>(q, kv, tree, H, ts, out, err);
     else if (rows == 32)
-        k_tree_attn<HD, 2, 1><<<std::min(most, 512), 256, 0, st>>>(q, kv, tree, H, ts, out, err);
-    else
-        k_tree_attn<HD, 2, 2><<<std::min(most, 256), 512, 0, st>>>(q, kv, tree, H, ts, out, err);
+        k_tree_attn<HD, 2, false><<<std::min(most, 256), kTreeWaves * 64, 0, st>>>(q, kv, tree, H, ts, out, err);
+    else  // most <= items x heads; whole groups of 16
+        k_tree_attn<HD, 2, true><<<std::min((most + 7) / 8 * 16, 256), kTreeWaves * 64, 0, st>>>(q, kv, tree, H, ts, out,
+                                                                                                  err);
 }
 
 hipError_t launch_tree_attention(const float* q, const KvTarget& kv, const cdb_tree& tree, int M, int H, int hd,
