@@ -215,26 +215,13 @@ __device__ __forceinline__ uint32_t sees4(uint64_t mask, int off) {
 // number are 0 (weights that far below the largest do not show in 32-bit sums).
 __device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// V of a page in LDS: key row r holds its 32-byte pieces b (16 dims) at place
-// vpiece(b, r), so that the 8 rows that half a wave reads at once lie on
-// different banks.
+// Rows of a page in LDS are padded so that what a read takes from several rows at
+// once lies on different banks: K 16 bytes (16 rows at one 16-byte piece), V 32
+// (8 rows at one 32-byte piece, by half a wave).
 template <int HD>
-__device__ __forceinline__ int vpiece(int b, int r) {
-    if constexpr (HD == 128) return b ^ (r & 7);
-    if constexpr (HD == 64) return b ^ ((r >> 1) & 3);
-    const int s = b + ((r >> 2) & 1);  // 96: rows are 6 pieces apart
-    return s == 6 ? 0 : s;
-}
-
-// K of a page in LDS: key row r holds its 16-byte piece ch at place kpiece(ch, r),
-// so that 16 rows read at one piece lie on different banks.
+constexpr int kKPitch = HD + 8;
 template <int HD>
-__device__ __forceinline__ int kpiece(int ch, int r) {
-    if constexpr (HD == 128) return ch ^ r;
-    if constexpr (HD == 64) return ch ^ (r >> 1);
-    const int s = ch + (r >> 2);  // 96: 12 pieces a row
-    return s >= 12 ? s - 12 : s;
-}
+constexpr int kVPitch = HD + 16;
 
 struct Work {
     TreeItem it;     // row0, n: this workgroup's rows
@@ -257,18 +244,22 @@ __global__ __launch_bounds__(kTreeWaves * 64) void k_tree_attn(
     constexpr int REC = HD + 2;
     constexpr bool QLDS = NT > 1;
     // K and V of the waves' pairs, then the q operands; the waves' states take their place
-    constexpr int VBYTES = kTreeWaves * 4 * kPage * HD * 2, QBYTES = QLDS ? NT * NJ * 2 * 1024 : 0;
+    constexpr int KP = kKPitch<HD>, VP = kVPitch<HD>, KROWS = 2 * kPage;
+    constexpr int VBYTES = kTreeWaves * KROWS * (KP + VP) * 2, QBYTES = QLDS ? NT * NJ * 2 * 1024 : 0;
     constexpr int OBYTES = kTreeWaves * ROWS * PITCH * 4;
-    __shared__ __align__(16) unsigned char smem[VBYTES + QBYTES > OBYTES ? VBYTES + QBYTES : OBYTES];
-    __shared__ float s_m[kTreeWaves][ROWS], s_l[kTreeWaves][ROWS], s_f[kTreeWaves][ROWS], s_den[ROWS];
-    __shared__ float s_fs[kTreeSegs][ROWS];
+    struct Factors {  // of the rows: the waves' maxima, weights and factors, the sum, the segments' factors
+        float m[kTreeWaves][ROWS], l[kTreeWaves][ROWS], f[kTreeWaves][ROWS], den[ROWS], seg[kTreeSegs][ROWS];
+    };
+    constexpr int ABYTES = VBYTES + QBYTES, BBYTES = OBYTES + (int)sizeof(Factors);
+    __shared__ __align__(16) unsigned char smem[ABYTES > BBYTES ? ABYTES : BBYTES];
     __shared__ int s_last;
+    Factors& sf = *reinterpret_cast<Factors*>(smem + OBYTES);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
     const int d = H * HD;
     const float qscale = 1.4426950408889634f / sqrtf((float)HD);
-    uint16_t* sk = reinterpret_cast<uint16_t*>(smem) + wave * 4 * kPage * HD;
-    uint16_t* sv = sk + 2 * kPage * HD;
+    uint16_t* sk = reinterpret_cast<uint16_t*>(smem) + wave * KROWS * (KP + VP);
+    uint16_t* sv = sk + KROWS * KP;
 
     // Work w: with two halves, workgroups 8 apart, which run on one XCD at one time,
     // take the halves of a tile's rows, so that the second one's K and V come from
@@ -296,35 +287,36 @@ __global__ __launch_bounds__(kTreeWaves * 64) void k_tree_attn(
     // A missing page's loads go to one that exists; what they bring is masked.
     struct Pair {
         int there;
-        const uint16_t* at[2];
+        const char* at[2];
     };
+    const size_t page_bytes = (size_t)2 * H * kPage * HD * 2;
+    const uint32_t v_at = (uint32_t)H * kPage * HD * 2;
     auto pair_of = [&](const Work& x, int ids, int i) {
         const int p0 = __builtin_amdgcn_readlane(ids, 2 * (i & 31)), p1 = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + 1);
         const bool ok0 = p0 >= 0 && p0 < kv.n_pages, ok1 = p1 >= 0 && p1 < kv.n_pages;
-        const int q0 = ok0 ? p0 : 0, q1 = ok1 ? p1 : q0;
         if (((!ok0 && p0 != -2) || (!ok1 && p1 != -2)) && lane == 0) set_err(err, CDB_DEV_UNMAPPED_PAGE);
-        return Pair{(ok0 ? 1 : 0) | (ok1 ? 2 : 0),
-                    {kv.pool + kv_offset(kv.layer, q0, kv.n_pages, 0, x.head, H, 0, HD),
-                     kv.pool + kv_offset(kv.layer, q1, kv.n_pages, 0, x.head, H, 0, HD)}};
+        const int q0 = ok0 ? p0 : 0, q1 = ok1 ? p1 : q0;
+        const char* pool = reinterpret_cast<const char*>(kv.pool + kv_offset(kv.layer, 0, kv.n_pages, 0, x.head, H, 0, HD));
+        return Pair{(ok0 ? 1 : 0) | (ok1 ? 2 : 0), {pool + q0 * page_bytes, pool + q1 * page_bytes}};
     };
     // A pair's K and V, in 16-byte pieces as stored.  Each is read once by one
     // workgroup (past the caches' normal allocation), with halves by two.
     typedef u32x4 PairRegs[2][NJ];
     PairRegs kr, vr;
-    const int v_at = H * kPage * HD;
+    const uint32_t lane16 = lane * 16;
     auto fetch = [&](const Pair& x) {
-        auto load = [](const uint16_t* at) {
-            const u32x4* a = reinterpret_cast<const u32x4*>(at);
+        auto load = [&](const char* page, int j) {  // uniform page + 32-bit lane offset + constant
+            const u32x4* a = reinterpret_cast<const u32x4*>(page + (size_t)lane16 + 1024 * j);
             return HALVES ? *a : __builtin_nontemporal_load(a);
         };
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) kr[h][j] = load(x.at[h] + (j * 64 + lane) * 8);
+            for (int j = 0; j < NJ; ++j) kr[h][j] = load(x.at[h], j);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) vr[h][j] = load(x.at[h] + v_at + (j * 64 + lane) * 8);
+            for (int j = 0; j < NJ; ++j) vr[h][j] = load(x.at[h] + v_at, j);
     };
 
     // Each item's first pair is on its way before the item before it is written out.
@@ -339,8 +331,11 @@ __global__ __launch_bounds__(kTreeWaves * 64) void k_tree_attn(
     }
     while (true) {
         const int next = work + gridDim.x;
-        const Work x2 = load_work(next < n_work ? next : work);
-        const int ids2 = page_ids(x2, x2.p);
+        int ids2;
+        {
+            const Work x2 = load_work(next < n_work ? next : work);
+            ids2 = page_ids(x2, x2.p);
+        }
         const TreeItem& it = x.it;
         const int head = x.head;
         // A segment's record of a row: sums, maximum, weight.  Written through to memory
@@ -437,9 +432,8 @@ __global__ __launch_bounds__(kTreeWaves * 64) void k_tree_attn(
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) {
                     const int f = j * 64 + lane, r = f / CPR, ch = f - r * CPR;
-                    *reinterpret_cast<u32x4*>(sk + (h * kPage + r) * HD + kpiece<HD>(ch, r) * 8) = kr[h][j];
-                    *reinterpret_cast<u32x4*>(sv + (h * kPage + r) * HD + vpiece<HD>(ch >> 1, r) * 16 + (ch & 1) * 8) =
-                        vr[h][j];
+                    *reinterpret_cast<u32x4*>(sk + (h * kPage + r) * KP + ch * 8) = kr[h][j];
+                    *reinterpret_cast<u32x4*>(sv + (h * kPage + r) * VP + ch * 8) = vr[h][j];
                 }
             const bool more = i + 1 < x.mine;
             if (more) {
@@ -453,7 +447,7 @@ __global__ __launch_bounds__(kTreeWaves * 64) void k_tree_attn(
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int j = 0; j < NJ; ++j)
-                    ka[h][j] = *reinterpret_cast<const bf16x8*>(sk + (h * kPage + c) * HD + kpiece<HD>(4 * j + g, c) * 8);
+                    ka[h][j] = *reinterpret_cast<const bf16x8*>(sk + (h * kPage + c) * KP + 32 * j + 8 * g);
             floatx4 s[NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -481,11 +475,11 @@ __global__ __launch_bounds__(kTreeWaves * 64) void k_tree_attn(
             bf16x8 va[NB];
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                const uint16_t* at = sv + vk * HD + vpiece<HD>(b, vk) * 16 + (c & 3) * 4;
+                const uint16_t* at = sv + vk * VP + b * 16 + (c & 3) * 4;
                 const uint2 w0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                                                (__attribute__((address_space(3))) s16x4*)at));
                 const uint2 w1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                                               (__attribute__((address_space(3))) s16x4*)(at + kPage * HD)));
+                                                               (__attribute__((address_space(3))) s16x4*)(at + kPage * VP)));
                 va[b] = __builtin_bit_cast(bf16x8, u32x4{w0.x, w0.y, w1.x, w1.y});
             }
             // The maximum that weights are taken against follows the row's own once it has
@@ -549,7 +543,8 @@ __global__ __launch_bounds__(kTreeWaves * 64) void k_tree_attn(
                 for (int kk = 0; kk < 2 * kPage; ++kk) {
                     const int off = p * kPage + kk - it.base;
                     if (off < 0 || off >= 64 || !(it.seen >> off & 1) || !(there >> (kk >> 4) & 1)) continue;
-                    const uint16_t* row = (kk < kPage ? now.at[0] : now.at[1]) + H * kPage * HD + (kk & 15) * HD;
+                    const uint16_t* row =
+                        reinterpret_cast<const uint16_t*>((kk < kPage ? now.at[0] : now.at[1]) + v_at) + (kk & 15) * HD;
                     const int w = (kk >> 4) * 2 + ((kk & 3) >> 1);  // p of key kk: word w, half kk % 2, of lane group kk % 16 / 4
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
@@ -578,6 +573,7 @@ __global__ __launch_bounds__(kTreeWaves * 64) void k_tree_attn(
                 }
             }
         }
+        const Work x2 = load_work(next < n_work ? next : work);  // again: kept, it would crowd the loop's scalars
         if (next < n_work && x2.mine > 0) {
             pair = pair_of(x2, ids2, 0);
             fetch(pair);
@@ -593,23 +589,23 @@ __global__ __launch_bounds__(kTreeWaves * 64) void k_tree_attn(
             for (int b = 0; b < NB; ++b)
                 *reinterpret_cast<floatx4*>(so + (wave * ROWS + t * 16 + c) * PITCH + 16 * b + 4 * g) = st.o[t][b];
             if (g == 0) {
-                s_m[wave][t * 16 + c] = st.m[t];
-                s_l[wave][t * 16 + c] = l;
+                sf.m[wave][t * 16 + c] = st.m[t];
+                sf.l[wave][t * 16 + c] = l;
             }
         }
         __syncthreads();
         // row factors: waves of this segment
         if (tid < it.n) {
-            float mx = s_m[0][tid], den = 0.f;
+            float mx = sf.m[0][tid], den = 0.f;
 #pragma unroll
-            for (int w = 1; w < kTreeWaves; ++w) mx = fmaxf(mx, s_m[w][tid]);
+            for (int w = 1; w < kTreeWaves; ++w) mx = fmaxf(mx, sf.m[w][tid]);
 #pragma unroll
             for (int w = 0; w < kTreeWaves; ++w) {
-                const float f = exp2_raw(s_m[w][tid] - mx);
-                s_f[w][tid] = f;
-                den = fmaf(f, s_l[w][tid], den);
+                const float f = exp2_raw(sf.m[w][tid] - mx);
+                sf.f[w][tid] = f;
+                den = fmaf(f, sf.l[w][tid], den);
             }
-            s_den[tid] = den;
+            sf.den[tid] = den;
             if (it.nseg > 1) put2(rec(it.row0 + tid, it.seg) + HD, mx, den);
         }
         __syncthreads();
@@ -620,11 +616,11 @@ __global__ __launch_bounds__(kTreeWaves * 64) void k_tree_attn(
 #pragma unroll
             for (int w = 0; w < kTreeWaves; ++w) {
                 const float2 o2 = *reinterpret_cast<const float2*>(so + (w * ROWS + r) * PITCH + k);
-                a = fmaf(s_f[w][r], o2.x, a);
-                b = fmaf(s_f[w][r], o2.y, b);
+                a = fmaf(sf.f[w][r], o2.x, a);
+                b = fmaf(sf.f[w][r], o2.y, b);
             }
             if (it.nseg == 1)
-                finish(it.row0 + r, k, a, b, s_den[r]);
+                finish(it.row0 + r, k, a, b, sf.den[r]);
             else
                 put2(rec(it.row0 + r, it.seg) + k, a, b);
         }
@@ -648,10 +644,10 @@ __global__ __launch_bounds__(kTreeWaves * 64) void k_tree_attn(
 #pragma unroll
                     for (int sg = 0; sg < kTreeSegs; ++sg) {
                         const float f = exp2_raw(sm[sg] - mx);
-                        s_fs[sg][tid] = f;
+                        sf.seg[sg][tid] = f;
                         den = sg < it.nseg ? fmaf(f, sl[sg], den) : den;
                     }
-                    s_den[tid] = den;
+                    sf.den[tid] = den;
                 }
                 __syncthreads();
                 for (int e = tid; e < it.n * (HD / 2); e += THREADS) {
@@ -665,12 +661,12 @@ __global__ __launch_bounds__(kTreeWaves * 64) void k_tree_attn(
 #pragma unroll
                         for (int u = 0; u < 8; ++u) {
                             const bool in = s0 + u < it.nseg;
-                            const float f = s_fs[min(s0 + u, it.nseg - 1)][r];
+                            const float f = sf.seg[min(s0 + u, it.nseg - 1)][r];
                             a = in ? fmaf(f, x[u], a) : a;
                             b = in ? fmaf(f, y[u], b) : b;
                         }
                     }
-                    finish(it.row0 + r, k, a, b, s_den[r]);
+                    finish(it.row0 + r, k, a, b, sf.den[r]);
                 }
             }
         }
