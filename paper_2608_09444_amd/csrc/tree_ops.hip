@@ -225,22 +225,36 @@ __device__ __forceinline__ uint64_t shfl64(uint64_t v, int src) {
 }
 
 __global__ __launch_bounds__(256) void k_tree_rows(cdb_drafts dr, cdb_row_map out, int* err) {
-    __shared__ int s_seq[CDB_TREE_MAX_TREES], s_len[CDB_TREE_MAX_TREES], s_n[CDB_TREE_MAX_TREES], s_end[CDB_TREE_MAX_TREES];
+    __shared__ __align__(16) int s_seq[CDB_TREE_MAX_TREES];
+    __shared__ int s_len[CDB_TREE_MAX_TREES], s_n[CDB_TREE_MAX_TREES], s_end[CDB_TREE_MAX_TREES];
     __shared__ int red[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool lead = blockIdx.x == 0;
+    // this wave's tree, before its node count is known
+    const int t = blockIdx.x * 4 + wave;
+    const bool inside = t < dr.n_trees && lane < dr.max_nodes;
+    int p = inside ? dr.parent[(size_t)t * dr.max_nodes + lane] : -1;
+    const int token = inside ? dr.tokens[(size_t)t * dr.max_nodes + lane] : 0;
     int n = 0;
     {
         const int q = tid < dr.n_trees ? dr.seq[tid] : -1;
         s_seq[tid] = q;
+        bool ok = q >= 0 && q < dr.max_seqs;
+        const int l = ok ? dr.len[q] : -1;
+        if (tid < dr.n_trees) n = dr.n_nodes[tid];
+        ok = ok && l >= 0 && l <= 0x7fffffff - CDB_TREE_MAX_NODES && n >= 0 && n <= dr.max_nodes;
         __syncthreads();
         if (tid < dr.n_trees) {
-            bool ok = q >= 0 && q < dr.max_seqs;
-            const int l = ok ? dr.len[q] : -1;
-            n = dr.n_nodes[tid];
-            ok = ok && l >= 0 && l <= 0x7fffffff - CDB_TREE_MAX_NODES && n >= 0 && n <= dr.max_nodes;
-            for (int t = 0; t < tid; ++t) ok = ok && s_seq[t] != q;
-            if (!ok) {
+            bool twice = false;  // an earlier tree of this sequence
+            for (int u = 0; u < dr.n_trees; u += 8) {
+                int4 a[2];
+                a[0] = *reinterpret_cast<const int4*>(s_seq + u);
+                a[1] = *reinterpret_cast<const int4*>(s_seq + u + 4);
+                const int b[8] = {a[0].x, a[0].y, a[0].z, a[0].w, a[1].x, a[1].y, a[1].z, a[1].w};
+#pragma unroll
+                for (int k = 0; k < 8; ++k) twice |= (u + k < tid) & (b[k] == q);
+            }
+            if (!ok || twice) {
                 if (lead) set_err(err, CDB_DEV_BAD_INDEX);
                 n = 0;
             }
@@ -261,11 +275,10 @@ __global__ __launch_bounds__(256) void k_tree_rows(cdb_drafts dr, cdb_row_map ou
         if (!fits && tid == 0) *out.n_rows = 0;
     }
     if (lead && tid == 0 && dr.n_trees == 0) *out.n_rows = 0;
-    const int t = blockIdx.x * 4 + wave;
     if (t >= dr.n_trees || s_end[t] > out.capacity) return;
     const int nt = s_n[t], row0 = s_end[t] - nt, base = s_len[t];
     const bool live = lane < nt;
-    int p = live ? dr.parent[(size_t)t * dr.max_nodes + lane] : -1;
+    if (!live) p = -1;
     if (live && (p < -1 || p >= lane)) {
         set_err(err, CDB_DEV_BAD_INDEX);
         p = -1;
@@ -286,7 +299,7 @@ __global__ __launch_bounds__(256) void k_tree_rows(cdb_drafts dr, cdb_row_map ou
         out.pos[r] = base + lane;
         out.base[r] = base;
         out.rope_pos[r] = base + __popcll(m) - 1;
-        out.tokens[r] = dr.tokens[(size_t)t * dr.max_nodes + lane];
+        out.tokens[r] = token;
         out.mask[r] = m;
     }
 }

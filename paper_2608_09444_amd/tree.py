@@ -9,7 +9,9 @@ from __future__ import annotations
 
 import ctypes as C
 
-from . import (CDB_ERR_CAPACITY, CDB_ERR_INVALID_ARG, MAX_ROWS, CdbError, _check, _ptr, _stream, cdb_kv, cdb_model,
+import torch
+
+from . import (CDB_ERR_CAPACITY, CDB_ERR_INVALID_ARG, MAX_ROWS, CdbError, _check, _ptr, cdb_kv, cdb_model,
                cdb_model_desc, cdb_rows, cdb_state, cdb_step_out, cdb_workspace_init, lib as _lib)
 
 EXPORTED = ("cdb_tree_workspace_bytes", "cdb_map_pages", "cdb_tree_rows", "cdb_tree_attention", "cdb_tree_prelude",
@@ -67,6 +69,14 @@ def lib() -> C.CDLL:
     return L
 
 
+def _stream(stream) -> int:
+    """The stream's handle.  The current one is looked up without making a Stream object, which would take longer than
+    the smaller of these calls run."""
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
 def _need(fn, ok):
     if not ok:
         raise CdbError(fn, CDB_ERR_INVALID_ARG)
@@ -74,10 +84,16 @@ def _need(fn, ok):
 
 def _tensor(fn, t, dtype, *shape):
     """A contiguous device tensor of this type; shape: its sizes (None: any)."""
-    import torch
-    _need(fn, isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == getattr(torch, dtype) and t.is_contiguous())
-    _need(fn, not shape or (t.dim() == len(shape) and all(w is None or n == w for n, w in zip(t.shape, shape))))
+    _need(fn, isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.is_contiguous() and
+          (not shape or (t.dim() == len(shape) and all(w is None or n == w for n, w in zip(t.shape, shape)))))
     return t
+
+
+def _flat(fn, t, dtype, least):
+    """The address of a contiguous device tensor of this type with at least so many values."""
+    if not (t.is_cuda and t.dtype is dtype and t.numel() >= least and t.is_contiguous()):
+        raise CdbError(fn, CDB_ERR_INVALID_ARG)
+    return t.data_ptr()
 
 
 # ---------------------------------------------------------------- C ABI, same names
@@ -93,12 +109,11 @@ def _ref(c):
 def cdb_map_pages(desc: cdb_model_desc, page_table, pre, core, coda, kv_layout: int, length, mapped, ws, stream=None):
     """page_table: device int32 [max_seqs][r_max + 2][max_pages]; pre, core, coda: cdb_page_pool, None for a stage
     without layers; length, mapped: device int32 [max_seqs]."""
-    _tensor("cdb_map_pages", page_table, "int32", None, desc.r_max + 2, None)
+    _tensor("cdb_map_pages", page_table, torch.int32, None, desc.r_max + 2, None)
     S, _, P = page_table.shape
-    _tensor("cdb_map_pages", length, "int32", S)
-    _tensor("cdb_map_pages", mapped, "int32", S)
-    _check("cdb_map_pages", lib().cdb_map_pages(C.byref(desc), _ptr(page_table), S, P, _ref(pre), _ref(core), _ref(coda),
-                                                kv_layout, _ptr(length), _ptr(mapped), _ptr(ws), ws.numel(),
+    lens, have = (_flat("cdb_map_pages", t, torch.int32, S) for t in (length, mapped))
+    _check("cdb_map_pages", lib().cdb_map_pages(C.byref(desc), page_table.data_ptr(), S, P, _ref(pre), _ref(core),
+                                                _ref(coda), kv_layout, lens, have, ws.data_ptr(), ws.numel(),
                                                 _stream(stream)))
 
 
@@ -120,14 +135,13 @@ def cdb_tree_rows(drafts: cdb_drafts, out: cdb_row_map, ws, stream=None):
 def cdb_tree_attention(desc: cdb_model_desc, kv: cdb_kv, rows: cdb_rows, tree: cdb_tree, stage: int, layer: int, q, out,
                        ws, stream=None):
     """q: device fp32 [n_rows][d]; out: device bf16 in fragment order (cdb_paged_attention)."""
-    _tensor("cdb_tree_attention", q, "float32")
-    _tensor("cdb_tree_attention", out, "bfloat16")
-    padded = next(p for p in (32, 64, 128, 256, rows.n_rows) if p >= rows.n_rows)
+    n = rows.n_rows
+    padded = 32 if n <= 32 else 64 if n <= 64 else 128 if n <= 128 else max(n, 256)
     _rows_fit("cdb_tree_attention", rows, tree)
-    _need("cdb_tree_attention", q.numel() >= rows.n_rows * desc.d and out.numel() >= padded * desc.d)
+    qp = _flat("cdb_tree_attention", q, torch.float32, n * desc.d)
+    op = _flat("cdb_tree_attention", out, torch.bfloat16, padded * desc.d)
     _check("cdb_tree_attention", lib().cdb_tree_attention(C.byref(desc), C.byref(kv), C.byref(rows), C.byref(tree), stage,
-                                                          layer, _ptr(q), _ptr(out), _ptr(ws), ws.numel(),
-                                                          _stream(stream)))
+                                                          layer, qp, op, ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
 def cdb_tree_prelude(model: cdb_model, kv: cdb_kv, state: cdb_state, rows: cdb_rows, tree: cdb_tree, tokens, ws,
@@ -158,12 +172,11 @@ def cdb_tree_coda(model: cdb_model, kv: cdb_kv, state: cdb_state, rows: cdb_rows
 def cdb_tree_accept(drafts: cdb_drafts, row0, next_ids, first_ids, out: cdb_accepted, ws, stream=None):
     """row0, first_ids: device int32 [n_trees]; next_ids: device int32, by row."""
     _trees_fit("cdb_tree_accept", drafts, out)
-    _tensor("cdb_tree_accept", row0, "int32", drafts.n_trees)
-    _tensor("cdb_tree_accept", first_ids, "int32", drafts.n_trees)
-    _tensor("cdb_tree_accept", next_ids, "int32", None)
-    _check("cdb_tree_accept", lib().cdb_tree_accept(C.byref(drafts), _ptr(row0), _ptr(next_ids), next_ids.numel(),
-                                                    _ptr(first_ids), C.byref(out), _ptr(ws), ws.numel(),
-                                                    _stream(stream)))
+    T = drafts.n_trees
+    at, first = (_flat("cdb_tree_accept", t, torch.int32, T) for t in (row0, first_ids))
+    ids = _flat("cdb_tree_accept", next_ids, torch.int32, 0)
+    _check("cdb_tree_accept", lib().cdb_tree_accept(C.byref(drafts), at, ids, next_ids.numel(), first, C.byref(out),
+                                                    ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
 def cdb_tree_commit(desc: cdb_model_desc, kv: cdb_kv, drafts: cdb_drafts, accepted: cdb_accepted, ws, stream=None):
@@ -186,7 +199,6 @@ class TreeWorkspace:
     """Scratch of the calls above, and of the package's stage calls, for up to max_rows rows and max_seqs sequences."""
 
     def __init__(self, desc: cdb_model_desc, max_rows: int, max_seqs: int, device="cuda", stream=None):
-        import torch
         n = cdb_tree_workspace_bytes(desc, max_rows, max_seqs)
         if n == 0:
             raise CdbError("cdb_tree_workspace_bytes", CDB_ERR_CAPACITY)
@@ -200,8 +212,8 @@ class Tree:
 
     def __init__(self, max_nodes: int, base, mask, rope_pos):
         n = base.numel()
-        self.base, self.rope_pos = _tensor("Tree", base, "int32", n), _tensor("Tree", rope_pos, "int32", n)
-        self.mask = _tensor("Tree", mask, "int64", n)
+        self.base, self.rope_pos = _tensor("Tree", base, torch.int32, n), _tensor("Tree", rope_pos, torch.int32, n)
+        self.mask = _tensor("Tree", mask, torch.int64, n)
         self.c = _held(cdb_tree(max_nodes, _ptr(base), _ptr(mask), _ptr(rope_pos)), base, mask, rope_pos, n_rows=n)
 
 
@@ -210,13 +222,12 @@ class PagePool:
     int32 [1].  PagePool.full(n): all n pages free, page 0 next."""
 
     def __init__(self, free_ids, free_count):
-        self.free_ids, self.free_count = _tensor("PagePool", free_ids, "int32", None), \
-            _tensor("PagePool", free_count, "int32", 1)
+        self.free_ids, self.free_count = _tensor("PagePool", free_ids, torch.int32, None), \
+            _tensor("PagePool", free_count, torch.int32, 1)
         self.c = _held(cdb_page_pool(_ptr(free_ids), _ptr(free_count), free_ids.numel()), free_ids, free_count)
 
     @classmethod
     def full(cls, n: int, device="cuda"):
-        import torch
         return cls(torch.arange(n - 1, -1, -1, dtype=torch.int32, device=device),
                    torch.tensor([n], dtype=torch.int32, device=device))
 
@@ -228,9 +239,9 @@ class Drafts:
     def __init__(self, seq, length, n_nodes, parent, tokens):
         _need("Drafts", seq.dim() == 1 and parent.dim() == 2)
         (T, N), S = parent.shape, length.numel()
-        self.seq, self.n_nodes = _tensor("Drafts", seq, "int32", T), _tensor("Drafts", n_nodes, "int32", T)
-        self.length = _tensor("Drafts", length, "int32", S)
-        self.parent, self.tokens = _tensor("Drafts", parent, "int32", T, N), _tensor("Drafts", tokens, "int32", T, N)
+        self.seq, self.n_nodes = _tensor("Drafts", seq, torch.int32, T), _tensor("Drafts", n_nodes, torch.int32, T)
+        self.length = _tensor("Drafts", length, torch.int32, S)
+        self.parent, self.tokens = _tensor("Drafts", parent, torch.int32, T, N), _tensor("Drafts", tokens, torch.int32, T, N)
         arrays = (seq, length, n_nodes, parent, tokens)
         self.c = _held(cdb_drafts(T, N, S, *(_ptr(t) for t in arrays)), *arrays)
 
@@ -240,7 +251,6 @@ class TreeRows:
     call over them, at capacity with the row count in device memory."""
 
     def __init__(self, n_trees: int, capacity: int, device="cuda"):
-        import torch
 
         def ints(n, dtype=torch.int32):
             return torch.zeros(n, dtype=dtype, device=device)
@@ -264,7 +274,6 @@ class Accepted:
     """Accepted paths (cdb_accepted): path [n_trees][max_nodes], count and next [n_trees]."""
 
     def __init__(self, n_trees: int, max_nodes: int, device="cuda"):
-        import torch
         self.path = torch.full((n_trees, max_nodes), -1, dtype=torch.int32, device=device)
         self.count = torch.zeros(n_trees, dtype=torch.int32, device=device)
         self.next = torch.zeros(n_trees, dtype=torch.int32, device=device)
