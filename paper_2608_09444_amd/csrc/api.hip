@@ -207,8 +207,6 @@ static cdb_status run_layers(const Ctx& c, int first, int count, KvTarget kv, co
     // split-K partials not yet added to h: the previous down projection's, or at
     // the start those of the loop step's adapter (h then holds zeros)
     int pending = pending_in;
-    if (tree && count > 0)
-        HIPCHK(launch_tree_plan(kv, r.seq, *tree, M, d.n_heads, d.head_dim, c.ws + c.L.total, c.err, st, dn));
     // the attention's row order (c.order) was written by the call's row-entry
     // kernel (gather, embed or state load); prefill chunks need none
     for (int l = 0; l < count; ++l) {
@@ -232,7 +230,8 @@ static cdb_status run_layers(const Ctx& c, int first, int count, KvTarget kv, co
             HIPCHK(launch_prefill_attention(c.q, kv, chunk->seq, chunk->pos0, M, d.n_heads, d.head_dim, c.x, c.err,
                                             st));
         else if (tree)
-            HIPCHK(launch_tree_attention(c.q, kv, *tree, M, d.n_heads, d.head_dim, c.ws + c.L.total, c.x, c.err, st));
+            HIPCHK(launch_tree_attention(c.q, kv, r.seq, *tree, M, d.n_heads, d.head_dim, c.ws + c.L.total, c.x, c.err,
+                                         st, dn));
         else
             HIPCHK(launch_attention(c.q, kv, r.seq, r.pos, c.order, M, d.n_heads, d.head_dim, c.x, c.err, st, dn,
                                     c.asplit.arrive ? &c.asplit : nullptr));
@@ -709,12 +708,9 @@ cdb_status cdb_tree_attention(const cdb_model_desc* desc, const cdb_kv* kv, cons
     if (s != CDB_OK || rows->n_rows == 0) return s;
     if (!tree->base || !tree->mask || kv->max_seqs < 0 || kv->max_pages < 0 || t.n_pages < 1) return CDB_ERR_INVALID_ARG;
     if (kv->max_pages > kMaxTablePages) return CDB_ERR_CAPACITY;
-    void* scratch = static_cast<unsigned char*>(ws) + 256;
-    int* err = static_cast<int*>(ws);
-    HIPCHK(launch_tree_plan(t, rows->seq, *tree, rows->n_rows, desc->n_heads, desc->head_dim, scratch, err, st,
-                            rows->d_n_rows));
-    HIPCHK(launch_tree_attention(q, t, *tree, rows->n_rows, desc->n_heads, desc->head_dim, scratch,
-                                 static_cast<uint16_t*>(out), err, st));
+    HIPCHK(launch_tree_attention(q, t, rows->seq, *tree, rows->n_rows, desc->n_heads, desc->head_dim,
+                                 static_cast<unsigned char*>(ws) + 256, static_cast<uint16_t*>(out),
+                                 static_cast<int*>(ws), st, rows->d_n_rows));
     return CDB_OK;
 }
 

@@ -230,12 +230,10 @@ hipError_t launch_ws_init(int* err, hipStream_t st);
 // first 256 bytes), and of cdb_map_pages' behind the first 256
 size_t tree_scratch_bytes(const cdb_model_desc& d, int rows);
 inline size_t map_scratch_bytes(int max_seqs) { return (4 + (size_t)max_seqs) * 4; }
-// attention of drafted rows (base, mask as in cdb_tree): the plan once per stage
-// call, into `scratch`, then every layer
-hipError_t launch_tree_plan(const KvTarget& kv, const int32_t* seq, const cdb_tree& tree, int M, int H, int hd,
-                            void* scratch, int* err, hipStream_t st, const int32_t* dn);
-hipError_t launch_tree_attention(const float* q, const KvTarget& kv, const cdb_tree& tree, int M, int H, int hd,
-                                 void* scratch, uint16_t* out, int* err, hipStream_t st);
+// attention of drafted rows (base, mask as in cdb_tree)
+hipError_t launch_tree_attention(const float* q, const KvTarget& kv, const int32_t* seq, const cdb_tree& tree, int M,
+                                 int H, int hd, void* scratch, uint16_t* out, int* err, hipStream_t st,
+                                 const int32_t* dn);
 // pools: prelude, core, coda; core_width: distinct core pages per token page;
 // scratch: 4 + S ints
 hipError_t launch_map_pages(const cdb_model_desc& md, int32_t* table, int S, int P, const cdb_page_pool* const* pools,
