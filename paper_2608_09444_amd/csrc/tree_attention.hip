@@ -58,12 +58,14 @@ constexpr int kTreeRows = 32;      // most rows of a workgroup
 constexpr int kTreeCUs = 256;
 
 // Segments of a context whose last committed position is on page npg - 1, and the
-// pages of each (the last one has the rest).
+// pages of each (the last one has the rest); a multiple of the waves' pairs.
 __host__ __device__ __forceinline__ int tree_segments(int npg, int* pages) {
-    int n = (npg + kTreeSegPages - 1) / kTreeSegPages;
-    n = n > kTreeSegs ? kTreeSegs : n;
-    constexpr int round = 2 * kTreeWaves;  // the waves' pairs
-    *pages = (npg + round * n - 1) / (round * n) * round;
+    if (npg <= kTreeSegs * kTreeSegPages) {
+        *pages = kTreeSegPages;
+        return (npg + kTreeSegPages - 1) / kTreeSegPages;
+    }
+    constexpr int round = 2 * kTreeWaves;
+    *pages = (npg + kTreeSegs * round - 1) / (kTreeSegs * round) * round;
     return (npg + *pages - 1) / *pages;
 }
 
@@ -209,11 +211,10 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
     constexpr int ROWS = 16 * NT, CAP = HALVES ? 2 * kTreeRows : ROWS;  // rows of a workgroup, of a tile
     constexpr int PITCH = HD + 4, REC = HD + 2;
     constexpr int NE = (ROWS * (HD / 2) + kTreeThreads - 1) / kTreeThreads;  // pairs of dims of the totals per thread
-    // K and V of the waves' pairs, then q operands (more than one tile of them).  At a
-    // segment's end the waves' states and factors take the place of K and V.
-    constexpr bool QLDS = NT > 1;
+    // K and V of the waves' pairs, then q operands.  At a segment's end the waves' states
+    // and factors take the place of K and V.
     constexpr int KP = kKPitch<HD>, VP = kVPitch<HD>, KROWS = 2 * kPage;
-    constexpr int VBYTES = kTreeWaves * KROWS * (KP + VP) * 2, QBYTES = QLDS ? NT * NJ * 2 * 1024 : 0;
+    constexpr int VBYTES = kTreeWaves * KROWS * (KP + VP) * 2, QBYTES = NT * NJ * 2 * 1024;
     constexpr int OBYTES = kTreeWaves * ROWS * PITCH * 4;
     struct Factors {  // of the rows: the waves' maxima, weights and factors; of the total and the segment
         float m[kTreeWaves][ROWS], l[kTreeWaves][ROWS], f[kTreeWaves][ROWS], a[ROWS], b[ROWS];
@@ -396,55 +397,54 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
     uint16_t* sk = reinterpret_cast<uint16_t*>(smem) + wave * KROWS * (KP + VP);
     uint16_t* sv = sk + KROWS * KP;
 
-    // Each work's first pair is on its way before the work before it is written out.
+    // q: operand f = wave (dims 32j + 8g .. + 7 of row c of 16-row tile t, f = t NJ + j),
+    // as loaded, then scaled, split into hi + lo, in LDS for all waves: in registers two
+    // tiles of them would not leave room for a second wave per SIMD.
+    static_assert(NT * NJ <= kTreeWaves, "one operand a wave");
+    floatx4 qraw[2];
+    auto fetch_q = [&](const Work& x) {
+        if (wave >= NT * NJ || x.n <= 0) return;
+        const int row = x.row0 + min(wave / NJ * 16 + c, x.n - 1);  // rows past the tile repeat its last one
+        const float* src = q + (size_t)row * d + x.head * HD + 32 * (wave % NJ) + 8 * g;
+        __builtin_memcpy(&qraw[0], src, 16);
+        __builtin_memcpy(&qraw[1], src + 4, 16);
+    };
+    u32x4* sq = reinterpret_cast<u32x4*>(smem + VBYTES) + lane;
+    auto stage_q = [&] {
+        if (wave >= NT * NJ) return;
+        const float v[8] = {qraw[0][0], qraw[0][1], qraw[0][2], qraw[0][3], qraw[1][0], qraw[1][1], qraw[1][2], qraw[1][3]};
+        uint32_t hw[4], lw[4];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const float v0 = v[e] * qscale, v1 = v[e + 1] * qscale;
+            const uint32_t h = pack_bf16(v0, v1);
+            hw[e / 2] = h;
+            lw[e / 2] = pack_bf16(v0 - bflo(h), v1 - bfhi(h));
+        }
+        sq[wave * 128] = u32x4{hw[0], hw[1], hw[2], hw[3]};
+        sq[wave * 128 + 64] = u32x4{lw[0], lw[1], lw[2], lw[3]};
+    };
+
+    // Each work's first pair and q are on their way before the work before it is written out.
     int work = blockIdx.x;
     if (work >= n_all) return;
     Work x = load_work(work);
     int ids = page_ids(x, x.p);
+    qraw[0] = qraw[1] = floatx4{0.f, 0.f, 0.f, 0.f};
+    fetch_q(x);
     Pair pair = pair_of(x, ids, 0);
     fetch(pair);
     while (true) {
         const int next = work + gridDim.x;
-        Work x2 = load_work(next < n_all ? next : work);
-        const int ids2 = page_ids(x2, x2.p);
-        const int head = x.head;
-
-        // q operands: row c of tile t, dims 32j + 8g .. + 7, scaled, hi + lo.  One tile's
-        // stay in each wave's registers; two would not leave enough of them for a second
-        // wave per SIMD, so all waves read them from LDS.
-        auto q_operand = [&](int t, int j, bf16x8& hi, bf16x8& lo) {
-            const int row = x.row0 + min(t * 16 + c, x.n - 1);  // rows past the tile repeat its last one
-            const float* src = q + (size_t)row * d + head * HD + 32 * j + 8 * g;
-            floatx4 a, b;
-            __builtin_memcpy(&a, src, 16);
-            __builtin_memcpy(&b, src + 4, 16);
-            const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-            uint32_t hw[4], lw[4];
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const float v0 = v[e] * qscale, v1 = v[e + 1] * qscale;
-                const uint32_t h = pack_bf16(v0, v1);
-                hw[e / 2] = h;
-                lw[e / 2] = pack_bf16(v0 - bflo(h), v1 - bfhi(h));
-            }
-            hi = __builtin_bit_cast(bf16x8, u32x4{hw[0], hw[1], hw[2], hw[3]});
-            lo = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], lw[2], lw[3]});
-        };
-        u32x4* sq = reinterpret_cast<u32x4*>(smem + VBYTES) + lane;
-        bf16x8 qr[2][QLDS ? 1 : NJ];  // hi, lo
-        if constexpr (QLDS) {
-            for (int f = wave; f < NT * NJ && x.n > 0; f += kTreeWaves) {
-                bf16x8 hi, lo;
-                q_operand(f / NJ, f % NJ, hi, lo);
-                sq[f * 128] = __builtin_bit_cast(u32x4, hi);
-                sq[f * 128 + 64] = __builtin_bit_cast(u32x4, lo);
-            }
-            __syncthreads();
-        } else {
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-                if (x.n > 0) q_operand(0, j, qr[0][j], qr[1][j]);
+        stage_q();
+        Work x2{};
+        int ids2 = -2;
+        if (next < n_all) {
+            x2 = load_work(next);
+            ids2 = page_ids(x2, x2.p);
+            fetch_q(x2);
         }
+        const int head = x.head;
         float tot[NE][2];
 #pragma unroll
         for (int k = 0; k < NE; ++k) tot[k][0] = tot[k][1] = 0.f;
@@ -452,6 +452,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
             s_tm[tid] = -1e30f;
             s_tl[tid] = 0.f;
         }
+        __syncthreads();  // q
         TreeState<HD, NT> st;
         st.clear();
         const bool whole = x.sg0 == 0 && x.sg1 == x.nseg;  // else the segments are written as records
@@ -515,10 +516,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
                         bf16x8 b[NJ];
 #pragma unroll
                         for (int j = 0; j < NJ; ++j)
-                            if constexpr (QLDS)
-                                b[j] = __builtin_bit_cast(bf16x8, sq[(t * NJ + j) * 128 + part * 64]);
-                            else
-                                b[j] = qr[part][j];
+                            b[j] = __builtin_bit_cast(bf16x8, sq[(t * NJ + j) * 128 + part * 64]);
 #pragma unroll
                         for (int j = 0; j < NJ; ++j)
 #pragma unroll
