@@ -164,13 +164,21 @@ template <int HD>
 constexpr int kVPitch = HD + 16;
 
 struct Work {
-    int row0, n;         // the workgroup's rows; n <= 0: none
-    int seq, plane, base, head;
     uint64_t seen;       // mask bits of any row of the tile
+    int row0, n;         // the workgroup's rows; n 0: none
+    int seq, plane, base, head;
     int sg0, sg1, nseg;  // the work's segments, those of the context
     int sp, npg;         // pages of a segment, of the context and the tree
-    int p, mine;         // this wave's first page, and how many pairs of pages it has
+    // from here on by wave: its first page, and how many pairs of pages it has
+    int p, mine;
+    __device__ __forceinline__ void by_wave(int wave) {
+        p = sg0 * sp + 2 * wave;
+        const int pe = sg1 == nseg ? npg : sg1 * sp;
+        // at least one pair, of pages that are not there if need be: every work is fetched alike
+        mine = pe > p ? (pe - p + 2 * kTreeWaves - 1) / (2 * kTreeWaves) : 1;
+    }
 };
+constexpr int kWorkInts = 13;  // of Work, without the last two
 
 template <int HD, int NT>
 struct TreeState {
@@ -228,6 +236,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
     __shared__ uint32_t s_tile[kMaxRows];     // works before the tile << 16 | its first row << 8 | its rows - 1
     __shared__ uint64_t s_run[4], s_first[4], s_end[4];
     __shared__ int s_sum[4];
+    __shared__ Work s_next;
     Factors& sf = *reinterpret_cast<Factors*>(smem + OBYTES);
     float* so = reinterpret_cast<float*>(smem);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -316,7 +325,8 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
         const int wh = !HALVES ? w : w / 16 * 8 + w % 8, r = !HALVES ? 0 : w / 8 % 2 * kTreeRows;
         Work x{};
         if (wh >= n_heads) {  // no rows: one pair of pages that are not there
-            x.sg1 = x.nseg = x.mine = 1;
+            x.sg1 = x.nseg = 1;
+            x.by_wave(wave);
             return x;
         }
         const int item = wh / H;
@@ -345,13 +355,10 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
         x.npg = last < 0 ? 0 : last / kPage + 1;
         x.n = max(min(rows - r, ROWS), 0);
         x.row0 = x.n > 0 ? tile0 + r : tile0;
-        x.p = x.sg0 * x.sp + 2 * wave;
-        const int pe = x.sg1 == x.nseg ? x.npg : x.sg1 * x.sp;
-        // at least one pair, of pages that are not there if need be: every work is fetched alike
-        x.mine = pe > x.p ? (pe - x.p + 2 * kTreeWaves - 1) / (2 * kTreeWaves) : 1;
         // divisions leave these in vector registers
-        for (int* f : {&x.head, &x.nseg, &x.sp, &x.sg0, &x.sg1, &x.npg, &x.p, &x.mine, &x.row0, &x.n})
+        for (int* f : {&x.head, &x.nseg, &x.sp, &x.sg0, &x.sg1, &x.npg, &x.row0, &x.n})
             *f = __builtin_amdgcn_readfirstlane(*f);
+        x.by_wave(wave);
         return x;
     };
     // lane l: the id of page l % 2 of pair l / 2 from page `from` on; -2: past the context
@@ -365,15 +372,16 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
         int there;
         const char* at[2];
     };
-    const size_t page_bytes = (size_t)2 * H * kPage * HD * 2;
-    const uint32_t v_at = (uint32_t)H * kPage * HD * 2;
-    auto pair_of = [&](const Work& x, int ids, int i) {
+    const uint32_t v_at = (uint32_t)H * kPage * HD * 2, page_bytes = 2 * v_at;
+    const char* pool = reinterpret_cast<const char*>(kv.pool + kv_offset(kv.layer, 0, kv.n_pages, 0, 0, H, 0, HD));
+    auto pair_of = [&](int head, int ids, int i) {
         const int p0 = __builtin_amdgcn_readlane(ids, 2 * (i & 31)), p1 = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + 1);
         const bool ok0 = p0 >= 0 && p0 < kv.n_pages, ok1 = p1 >= 0 && p1 < kv.n_pages;
         if (((!ok0 && p0 != -2) || (!ok1 && p1 != -2)) && lane == 0) set_err(err, CDB_DEV_UNMAPPED_PAGE);
         const int q0 = ok0 ? p0 : 0, q1 = ok1 ? p1 : q0;
-        const char* pool = reinterpret_cast<const char*>(kv.pool + kv_offset(kv.layer, 0, kv.n_pages, 0, x.head, H, 0, HD));
-        return Pair{(ok0 ? 1 : 0) | (ok1 ? 2 : 0), {pool + q0 * page_bytes, pool + q1 * page_bytes}};
+        const char* of_head = pool + (uint32_t)head * (kPage * HD * 2);
+        return Pair{(ok0 ? 1 : 0) | (ok1 ? 2 : 0),
+                    {of_head + (uint64_t)(uint32_t)q0 * page_bytes, of_head + (uint64_t)(uint32_t)q1 * page_bytes}};
     };
     // A pair's K and V, in 16-byte pieces as stored.  Each is read once by one
     // workgroup (past the caches' normal allocation), with halves by two.
@@ -432,18 +440,11 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
     int ids = page_ids(x, x.p);
     qraw[0] = qraw[1] = floatx4{0.f, 0.f, 0.f, 0.f};
     fetch_q(x);
-    Pair pair = pair_of(x, ids, 0);
+    Pair pair = pair_of(x.head, ids, 0);
     fetch(pair);
     while (true) {
         const int next = work + gridDim.x;
         stage_q();
-        Work x2{};
-        int ids2 = -2;
-        if (next < n_all) {
-            x2 = load_work(next);
-            ids2 = page_ids(x2, x2.p);
-            fetch_q(x2);
-        }
         const int head = x.head;
         float tot[NE][2];
 #pragma unroll
@@ -452,7 +453,17 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
             s_tm[tid] = -1e30f;
             s_tl[tid] = 0.f;
         }
-        __syncthreads();  // q
+        __syncthreads();  // q; every wave has read s_next
+        // the next work: its first pages and q; the rest of it waits in LDS
+        int ids2 = -2;
+        int head2 = 0;
+        if (next < n_all) {
+            const Work x2 = load_work(next);
+            ids2 = page_ids(x2, x2.p);
+            fetch_q(x2);
+            if (tid == 0) s_next = x2;
+            head2 = x2.head;
+        }
         TreeState<HD, NT> st;
         st.clear();
         const bool whole = x.sg0 == 0 && x.sg1 == x.nseg;  // else the segments are written as records
@@ -496,7 +507,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
                 const bool more = i + 1 < x.mine;
                 if (more && ((i + 1) & 31) == 0) ids = page_ids(x, p + 2 * kTreeWaves);
                 if (more || next < n_all) {
-                    pair = pair_of(more ? x : x2, more ? ids : ids2, more ? i + 1 : 0);
+                    pair = pair_of(more ? head : head2, more ? ids : ids2, more ? i + 1 : 0);
                     fetch(pair);
                 }
                 // A = K: key c of either page, dims 32j + 8g ..
@@ -699,7 +710,12 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
         }
         if (next >= n_all) break;
         __syncthreads();  // the totals and q, before the next work's
-        x = x2;
+        int f[kWorkInts];
+        __builtin_memcpy(f, &s_next, sizeof f);
+#pragma unroll
+        for (int k = 0; k < kWorkInts; ++k) f[k] = __builtin_amdgcn_readfirstlane(f[k]);
+        __builtin_memcpy(&x, f, sizeof f);
+        x.by_wave(wave);
         ids = ids2;
         work = next;
     }
