@@ -44,7 +44,6 @@
 // Nothing in a row's arithmetic depends on the other rows: not its tile, not the
 // segments, not the wave that takes a page or the workgroup that takes a segment.
 #include <algorithm>
-#include <type_traits>
 
 #include "cdb_internal.h"
 
@@ -128,18 +127,21 @@ __device__ __forceinline__ float over_rows_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-__device__ __forceinline__ uint32_t or_wave(uint32_t x) {
-    auto dpp = [](uint32_t v, auto ctrl) {
-        return v | (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xF, 0xF, true);
-    };
-    x = dpp(x, std::integral_constant<int, 0xB1>());   // quad_perm [1,0,3,2]
-    x = dpp(x, std::integral_constant<int, 0x4E>());   // quad_perm [2,3,0,1]
-    x = dpp(x, std::integral_constant<int, 0x141>());  // row_half_mirror
-    x = dpp(x, std::integral_constant<int, 0x140>());  // row_mirror
-    auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    x = r[0] | r[1];
-    r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return __builtin_amdgcn_readfirstlane(r[0] | r[1]);
+// Over groups of 8 lanes (quad swaps and a mirror of half a row); every lane gets it.
+#define CDB_TREE_DPP(v, ctrl) \
+    __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, (v)), (ctrl), 0xF, 0xF, true))
+__device__ __forceinline__ float over_8_max(float v) {
+    v = fmaxf(v, CDB_TREE_DPP(v, 0xB1));
+    v = fmaxf(v, CDB_TREE_DPP(v, 0x4E));
+    return fmaxf(v, CDB_TREE_DPP(v, 0x141));
+}
+__device__ __forceinline__ float over_8_sum(float v) {
+    v += CDB_TREE_DPP(v, 0xB1);
+    v += CDB_TREE_DPP(v, 0x4E);
+    return v + CDB_TREE_DPP(v, 0x141);
+}
+__device__ __forceinline__ float lane_value(float v, int lane) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
 }
 
 // Bits 0..3: whether positions base + off .. base + off + 3 are visible, those
@@ -158,10 +160,11 @@ __device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp
 // Rows of a page in LDS are padded so that what a read takes from several rows at
 // once lies on different banks: K 16 bytes (16 rows at one 16-byte piece), V 32
 // (8 rows at one 32-byte piece, by half a wave).
+// (8 for V where LDS is full: two rows to a bank.)
 template <int HD>
 constexpr int kKPitch = HD + 8;
-template <int HD>
-constexpr int kVPitch = HD + 16;
+template <int HD, int NT>
+constexpr int kVPitch = HD == 128 && NT == 2 ? HD + 8 : HD + 16;
 
 struct Work {
     uint64_t seen;       // mask bits of any row of the tile
@@ -218,26 +221,28 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
     constexpr int NJ = HD / 32, NB = HD / 16, CPR = HD / 8;  // K steps, dim blocks, 16-byte pieces of a row
     constexpr int ROWS = 16 * NT, CAP = HALVES ? 2 * kTreeRows : ROWS;  // rows of a workgroup, of a tile
     constexpr int PITCH = HD + 4, REC = HD + 2;
-    constexpr int NE = (ROWS * (HD / 2) + kTreeThreads - 1) / kTreeThreads;  // pairs of dims of the totals per thread
+    constexpr int NR = ROWS / kTreeWaves;  // rows whose totals a wave keeps: wave, wave + 8, ...; lane = two dims
     // K and V of the waves' pairs, then q operands.  At a segment's end the waves' states
     // and factors take the place of K and V.
-    constexpr int KP = kKPitch<HD>, VP = kVPitch<HD>, KROWS = 2 * kPage;
+    constexpr int KP = kKPitch<HD>, VP = kVPitch<HD, NT>, KROWS = 2 * kPage;
     constexpr int VBYTES = kTreeWaves * KROWS * (KP + VP) * 2, QBYTES = NT * NJ * 2 * 1024;
     constexpr int OBYTES = kTreeWaves * ROWS * PITCH * 4;
-    struct Factors {  // of the rows: the waves' maxima, weights and factors; of the total and the segment
-        float m[kTreeWaves][ROWS], l[kTreeWaves][ROWS], f[kTreeWaves][ROWS], a[ROWS], b[ROWS];
+    struct States {  // the waves' maxima and weights
+        float m[ROWS][kTreeWaves], l[ROWS][kTreeWaves];
     };
     struct Rows {  // at the start: the call's rows
         int seq[kMaxRows], plane[kMaxRows], base[kMaxRows];
     };
-    static_assert(OBYTES + sizeof(Factors) <= VBYTES && sizeof(Rows) <= VBYTES, "they leave q alone");
+    static_assert(OBYTES + sizeof(States) <= VBYTES && sizeof(Rows) <= VBYTES, "they leave q alone");
     __shared__ __align__(16) unsigned char smem[VBYTES + QBYTES];
-    __shared__ float s_tm[ROWS], s_tl[ROWS];  // the rows' totals
-    __shared__ uint32_t s_tile[kMaxRows];     // works before the tile << 16 | its first row << 8 | its rows - 1
+    __shared__ uint32_t s_tile[kMaxRows];  // works before the tile << 16 | its first row << 8 | its rows - 1
+    __shared__ int s_seq[kMaxRows], s_base[kMaxRows];  // of the tile's rows
+    __shared__ uint64_t s_seen[kMaxRows];              // mask bits of any of them
+    __shared__ uint8_t s_plane[kMaxRows];
     __shared__ uint64_t s_run[4], s_first[4], s_end[4];
     __shared__ int s_sum[4];
-    __shared__ Work s_next;
-    Factors& sf = *reinterpret_cast<Factors*>(smem + OBYTES);
+    __shared__ Work s_next[2];
+    States& sf = *reinterpret_cast<States*>(smem + OBYTES);
     float* so = reinterpret_cast<float*>(smem);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
@@ -259,6 +264,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
             sr.seq[tid] = ok ? r.seq : -1;
             sr.plane[tid] = r.plane;
             sr.base[tid] = r.base;
+            s_seen[tid] = 0;
         }
         __syncthreads();
         const bool run = ok && !(tid > 0 && sr.seq[tid - 1] == r.seq && sr.plane[tid - 1] == r.plane &&
@@ -311,7 +317,13 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
             n_works += f;
             if (k < w) at += f;
         }
-        if (first) s_tile[tile] = (uint32_t)(at - works) << 16 | (uint32_t)tid << 8 | (uint32_t)(rows - 1);
+        if (first) {
+            s_tile[tile] = (uint32_t)(at - works) << 16 | (uint32_t)tid << 8 | (uint32_t)(rows - 1);
+            s_seq[tile] = r.seq;
+            s_base[tile] = r.base;
+            s_plane[tile] = (uint8_t)r.plane;  // at most r_max + 1 <= 65
+        }
+        if (ok) atomicOr(reinterpret_cast<unsigned long long*>(&s_seen[first ? tile : tile - 1]), r.mask);
         if (tid == 0 && blockIdx.x == 0) *ts.runs = runs;
         __syncthreads();
     }
@@ -336,21 +348,15 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
             tile += __popcll(__ballot(k + lane < n_tiles && (int)(s_tile[min(k + lane, kMaxRows - 1)] >> 16) <= item));
         const uint32_t e = __builtin_amdgcn_readfirstlane(s_tile[tile]);
         const int tile0 = e >> 8 & 255, rows = (e & 255) + 1;
-        // every row of the tile has its first one's sequence, plane and base
-        uint32_t lo, hi;
-        {
-            const uint64_t m = tree.mask[tile0 + min(lane, rows - 1)];
-            lo = (uint32_t)m;
-            hi = (uint32_t)(m >> 32);
-        }
-        x.seq = seq[tile0];
-        x.base = tree.base[tile0];
-        x.plane = kv.c_row ? kv.c_row[tile0] + 1 : kv.plane_fixed;
+        x.seq = __builtin_amdgcn_readfirstlane(s_seq[tile]);
+        x.base = __builtin_amdgcn_readfirstlane(s_base[tile]);
+        x.plane = __builtin_amdgcn_readfirstlane((int)s_plane[tile]);
+        x.seen = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(s_seen[tile] >> 32)) << 32 |
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)s_seen[tile]);
         x.nseg = tree_segments(x.base / kPage + 1, &x.sp);
         const int z = min(runs, x.nseg), run = item - (int)(e >> 16);
         x.sg0 = run * x.nseg / z;
         x.sg1 = (run + 1) * x.nseg / z;
-        x.seen = (uint64_t)or_wave(hi) << 32 | or_wave(lo);
         const int last = x.seen ? x.base + 63 - __clzll((long long)x.seen) : x.base - 1;
         x.npg = last < 0 ? 0 : last / kPage + 1;
         x.n = max(min(rows - r, ROWS), 0);
@@ -442,18 +448,11 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
     fetch_q(x);
     Pair pair = pair_of(x.head, ids, 0);
     fetch(pair);
-    while (true) {
+    stage_q();
+    __syncthreads();
+    for (int turn = 0;; turn ^= 1) {
         const int next = work + gridDim.x;
-        stage_q();
         const int head = x.head;
-        float tot[NE][2];
-#pragma unroll
-        for (int k = 0; k < NE; ++k) tot[k][0] = tot[k][1] = 0.f;
-        if (tid < ROWS) {
-            s_tm[tid] = -1e30f;
-            s_tl[tid] = 0.f;
-        }
-        __syncthreads();  // q; every wave has read s_next
         // the next work: its first pages and q; the rest of it waits in LDS
         int ids2 = -2;
         int head2 = 0;
@@ -461,9 +460,12 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
             const Work x2 = load_work(next);
             ids2 = page_ids(x2, x2.p);
             fetch_q(x2);
-            if (tid == 0) s_next = x2;
+            if (tid == 0) s_next[turn] = x2;
             head2 = x2.head;
         }
+        float tot[NR][2], tm = -1e30f, tw = 0.f;  // totals; lanes 8k..: row k's maximum and weight
+#pragma unroll
+        for (int k = 0; k < NR; ++k) tot[k][0] = tot[k][1] = 0.f;
         TreeState<HD, NT> st;
         st.clear();
         const bool whole = x.sg0 == 0 && x.sg1 == x.nseg;  // else the segments are written as records
@@ -641,8 +643,8 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
             // the segment: the waves' states, [wave][row][dim]
             int tl = tid;
             asm volatile("" : "+v"(tl));  // addresses made here, not kept through the pairs
-            const int lc = tl & 15, lg = tl >> 4 & 3;
-            __syncthreads();  // every wave is done with its K and V
+            const int ll = tl & 63, lc = tl & 15, lg = tl >> 4 & 3;
+            __syncthreads();  // every wave is done with its K and V, and with q at the last segment
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const float l = over_rows_sum(st.l[t]);
@@ -650,49 +652,40 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
                 for (int b = 0; b < NB; ++b)
                     *reinterpret_cast<floatx4*>(so + (wave * ROWS + t * 16 + lc) * PITCH + 16 * b + 4 * lg) = st.o[t][b];
                 if (lg == 0) {
-                    sf.m[wave][t * 16 + lc] = st.m[t];
-                    sf.l[wave][t * 16 + lc] = l;
+                    sf.m[t * 16 + lc][wave] = st.m[t];
+                    sf.l[t * 16 + lc][wave] = l;
                 }
             }
             st.clear();
+            if (sg == x.sg1 - 1 && next < n_all) stage_q();
             __syncthreads();
-            float* rec = ts.part + (((size_t)x.row0 * H + head) * kTreeSegs + sg) * REC;  // of the first row
-            const size_t rec_row = (size_t)H * kTreeSegs * REC;
-            if (tl < x.n) {
-                float mx = sf.m[0][tl], den = 0.f;
+            // lane 8k + w: wave w's part in this wave's row k, wave + 8k
+            const int at = (wave + kTreeWaves * (min(ll, 8 * NR - 1) >> 3)) * kTreeWaves + (ll & 7);
+            const float sm = (&sf.m[0][0])[at];
+            const float mx = over_8_max(sm), f = exp2_raw(sm - mx), den = over_8_sum(f * (&sf.l[0][0])[at]);
+            float fa = 0.f, fb = 0.f;
+            if (whole) join_segment(tm, tw, mx, den, fa, fb);
 #pragma unroll
-                for (int w = 1; w < kTreeWaves; ++w) mx = fmaxf(mx, sf.m[w][tl]);
-#pragma unroll
-                for (int w = 0; w < kTreeWaves; ++w) {
-                    const float f = exp2_raw(sf.m[w][tl] - mx);
-                    sf.f[w][tl] = f;
-                    den = fmaf(f, sf.l[w][tl], den);
-                }
-                if (whole) {
-                    join_segment(s_tm[tl], s_tl[tl], mx, den, sf.a[tl], sf.b[tl]);
-                } else {
-                    rec[tl * rec_row + HD] = mx;
-                    rec[tl * rec_row + HD + 1] = den;
-                }
-            }
-            __syncthreads();
-            // thread = two dims of a row
-#pragma unroll
-            for (int k = 0; k < NE; ++k) {
-                const int e = tl + k * kTreeThreads, r = e / (HD / 2), dim = 2 * (e - r * (HD / 2));
-                if (r >= x.n) continue;
+            for (int k = 0; k < NR; ++k) {
+                const int r = wave + kTreeWaves * k;
+                if (r >= x.n) break;
                 float a = 0.f, b = 0.f;
 #pragma unroll
                 for (int w = 0; w < kTreeWaves; ++w) {
-                    const float2 o2 = *reinterpret_cast<const float2*>(so + (w * ROWS + r) * PITCH + dim);
-                    a = fmaf(sf.f[w][r], o2.x, a);
-                    b = fmaf(sf.f[w][r], o2.y, b);
+                    const float2 o2 =
+                        *reinterpret_cast<const float2*>(so + (w * ROWS + r) * PITCH + 2 * min(ll, HD / 2 - 1));
+                    const float fw = lane_value(f, 8 * k + w);
+                    a = fmaf(fw, o2.x, a);
+                    b = fmaf(fw, o2.y, b);
                 }
                 if (whole) {
-                    tot[k][0] = join_sum(tot[k][0], a, sf.a[r], sf.b[r]);
-                    tot[k][1] = join_sum(tot[k][1], b, sf.a[r], sf.b[r]);
+                    const float ta = lane_value(fa, 8 * k), tb = lane_value(fb, 8 * k);
+                    tot[k][0] = join_sum(tot[k][0], a, ta, tb);
+                    tot[k][1] = join_sum(tot[k][1], b, ta, tb);
                 } else {
-                    *reinterpret_cast<float2*>(rec + r * rec_row + dim) = make_float2(a, b);
+                    float* rec = ts.part + (((size_t)(x.row0 + r) * H + head) * kTreeSegs + sg) * REC;
+                    if (2 * ll < HD) *reinterpret_cast<float2*>(rec + 2 * ll) = make_float2(a, b);
+                    if (ll == 8 * k) *reinterpret_cast<float2*>(rec + HD) = make_float2(mx, den);
                 }
             }
             __syncthreads();  // K and V take the place of the states
@@ -700,18 +693,19 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
         if (whole) {
             int tl = tid;
             asm volatile("" : "+v"(tl));
+            const int dim = 2 * (tl & 63);
 #pragma unroll
-            for (int k = 0; k < NE; ++k) {
-                const int e = tl + k * kTreeThreads, r = e / (HD / 2), dim = 2 * (e - r * (HD / 2));
-                if (r < x.n)
+            for (int k = 0; k < NR; ++k) {
+                const int r = wave + kTreeWaves * k;
+                const float den = lane_value(tw, 8 * k);
+                if (r < x.n && dim < HD)
                     *reinterpret_cast<uint32_t*>(out + frag_index(x.row0 + r, head * HD + dim, d)) =
-                        row_out2(tot[k][0], tot[k][1], s_tl[r]);
+                        row_out2(tot[k][0], tot[k][1], den);
             }
         }
         if (next >= n_all) break;
-        __syncthreads();  // the totals and q, before the next work's
         int f[kWorkInts];
-        __builtin_memcpy(f, &s_next, sizeof f);
+        __builtin_memcpy(f, &s_next[turn], sizeof f);
 #pragma unroll
         for (int k = 0; k < kWorkInts; ++k) f[k] = __builtin_amdgcn_readfirstlane(f[k]);
         __builtin_memcpy(&x, f, sizeof f);
