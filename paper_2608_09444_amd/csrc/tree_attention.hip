@@ -253,37 +253,43 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
     int n_tiles, runs, n_works;
     {
         Rows& sr = *reinterpret_cast<Rows*>(smem);
-        const int w = wave & 3;
+        const int w = wave;
+        const bool rows_wave = w < kMaxRows / 64;
         const bool mine = tid < M;  // M <= 256
         RowSees r{};
-        if (mine) r = row_sees(kv, seq, tree, tid);
-        const int n = live_rows(dn, M);
-        const bool ok = mine && tid < n && r.ok;
-        if (mine && tid < n && !r.ok && blockIdx.x == 0) set_err(err, CDB_DEV_UNMAPPED_PAGE);
-        if (tid < kMaxRows) {
+        bool ok = false;
+        if (rows_wave) {
+            if (mine) r = row_sees(kv, seq, tree, tid);
+            ok = mine && tid < live_rows(dn, M) && r.ok;
+            if (mine && !r.ok && tid < live_rows(dn, M) && blockIdx.x == 0) set_err(err, CDB_DEV_UNMAPPED_PAGE);
             sr.seq[tid] = ok ? r.seq : -1;
             sr.plane[tid] = r.plane;
             sr.base[tid] = r.base;
             s_seen[tid] = 0;
         }
         __syncthreads();
-        const bool run = ok && !(tid > 0 && sr.seq[tid - 1] == r.seq && sr.plane[tid - 1] == r.plane &&
-                                 sr.base[tid - 1] == r.base);
-        const uint64_t my_runs = __ballot(run);
-        if (lane == 0 && wave < 4) s_run[w] = my_runs;
+        uint64_t my_runs = 0;
+        if (rows_wave) {
+            my_runs = __ballot(ok && !(tid > 0 && sr.seq[tid - 1] == r.seq && sr.plane[tid - 1] == r.plane &&
+                                       sr.base[tid - 1] == r.base));
+            if (lane == 0) s_run[w] = my_runs;
+        }
         __syncthreads();
-        int start = tid;  // the row at which this one's run started
-        {
+        bool first = false;
+        uint64_t firsts = 0, ends = 0;
+        if (rows_wave) {
+            int start = tid;  // the row at which this one's run started
             uint64_t b = my_runs & (~0ull >> (63 - lane));
             int word = w;
             while (!b && word > 0) b = s_run[--word];
             if (b) start = word * 64 + 63 - __clzll((long long)b);
-        }
-        const bool first = ok && (tid - start) % CAP == 0;
-        const uint64_t firsts = __ballot(first), ends = __ballot(first || !ok);
-        if (lane == 0 && wave < 4) {
-            s_first[w] = firsts;
-            s_end[w] = ends;
+            first = ok && (tid - start) % CAP == 0;
+            firsts = __ballot(first);
+            ends = __ballot(first || !ok);
+            if (lane == 0) {
+                s_first[w] = firsts;
+                s_end[w] = ends;
+            }
         }
         __syncthreads();
         n_tiles = 0;
@@ -304,12 +310,14 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
             works = min(runs, tree_segments(r.base / kPage + 1, &sp));
         }
         int at = works;
+        if (rows_wave) {
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int u = __shfl_up(at, o, 64);
-            if (lane >= o) at += u;
+            for (int o = 1; o < 64; o <<= 1) {
+                const int u = __shfl_up(at, o, 64);
+                if (lane >= o) at += u;
+            }
+            if (lane == 63) s_sum[w] = at;
         }
-        if (lane == 63 && wave < 4) s_sum[w] = at;
         __syncthreads();
         n_works = 0;
         for (int k = 0; k < 4; ++k) {
@@ -355,8 +363,13 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
                  (uint32_t)__builtin_amdgcn_readfirstlane((int)s_seen[tile]);
         x.nseg = tree_segments(x.base / kPage + 1, &x.sp);
         const int z = min(runs, x.nseg), run = item - (int)(e >> 16);
-        x.sg0 = run * x.nseg / z;
-        x.sg1 = (run + 1) * x.nseg / z;
+        if (z == x.nseg) {
+            x.sg0 = run;
+            x.sg1 = run + 1;
+        } else {
+            x.sg0 = run * x.nseg / z;
+            x.sg1 = (run + 1) * x.nseg / z;
+        }
         const int last = x.seen ? x.base + 63 - __clzll((long long)x.seen) : x.base - 1;
         x.npg = last < 0 ? 0 : last / kPage + 1;
         x.n = max(min(rows - r, ROWS), 0);
@@ -477,25 +490,40 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
                 const Pair now = pair;
                 const int there = now.there;
                 const bool masked = there != 3 || p * kPage + 2 * kPage > x.base;  // wave-uniform
-                bool odd = false;  // a V that is not finite where only some rows may see it
+                uint32_t odd = 0;  // bits 15, 31: a V that is not finite where only some rows may see it
                 if (masked) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                    for (int h = 0; h < 2; ++h) {
+                        if ((there >> h & 1) && (p + h + 1) * kPage <= x.base) continue;  // every row sees all of it
 #pragma unroll
                         for (int j = 0; j < NJ; ++j) {
                             const int off = (p + h) * kPage + (j * 64 + lane) / CPR - x.base;
-                            const uint32_t keep = (there >> h & 1) && (sees4(x.seen, off) & 1) ? ~0u : 0u;
-                            const uint32_t part = off < 0 ? 0u : ~0u;  // committed positions: every row sees them
-                            u32x4 x = vr[h][j] & keep;
+                            const uint64_t bit = off < 0 ? 1 : off < 64 ? x.seen >> (off & 63) : 0;
+                            vr[h][j] &= (there >> h & 1) && (bit & 1) ? ~0u : 0u;
+                            // an exponent of all ones carries into its half's top bit
+                            uint32_t o = 0;
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const uint32_t bad = ((x[e] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) |
-                                                     ((x[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
-                                odd |= (bad & part) != 0;
-                                x[e] &= ~(bad & part);
-                            }
-                            vr[h][j] = x;
+                            for (int e = 0; e < 4; ++e) o |= (vr[h][j][e] & 0x7f807f80u) + 0x00800080u;
+                            odd |= off < 0 ? 0 : o;
                         }
+                    }
+                    odd = __any((odd & 0x80008000u) != 0) ? 1 : 0;
+                    if (odd) {  // rare
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int j = 0; j < NJ; ++j) {
+                                const int off = (p + h) * kPage + (j * 64 + lane) / CPR - x.base;
+                                u32x4 v = vr[h][j];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const uint32_t top = (v[e] & 0x7f807f80u) + 0x00800080u;
+                                    const uint32_t bad = (top & 0x8000u ? 0xffffu : 0u) | (top >> 31 ? 0xffff0000u : 0u);
+                                    v[e] &= off < 0 ? ~0u : ~bad;
+                                }
+                                vr[h][j] = v;
+                            }
+                    }
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
@@ -605,7 +633,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
                         for (int t = 0; t < NT; ++t)
                             st.o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[b], part ? pl[t] : ph[t], st.o[t][b], 0, 0,
                                                                                  0);
-                if (masked && __any(odd)) {  // rare: the values taken out above, to the rows that see them
+                if (odd) {  // rare: the values taken out above, to the rows that see them
                     for (int kk = 0; kk < 2 * kPage; ++kk) {
                         const int off = p * kPage + kk - x.base;
                         if (off < 0 || off >= 64 || !(x.seen >> off & 1) || !(there >> (kk >> 4) & 1)) continue;
