@@ -52,7 +52,7 @@ namespace cdb {
 constexpr int kTreeWaves = 8;
 constexpr int kTreeThreads = kTreeWaves * 64;
 constexpr int kTreeSegs = 16;      // most segments of a context
-constexpr int kTreeSegPages = 32;  // pages of a segment, unless that makes too many
+constexpr int kTreeSegPages = 64;  // pages of a segment, unless that makes too many
 constexpr int kTreeRows = 32;      // most rows of a workgroup
 constexpr int kTreeCUs = 256;
 
@@ -564,6 +564,8 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
                             for (int h = 0; h < 2; ++h)
                                 s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[h][j], b[j], s[t][h], 0, 0, 0);
                     }
+                // with two tiles of 128 dims no registers are left for V before the scores are done
+                if constexpr (HD == 128 && NT == 2) __builtin_amdgcn_sched_barrier(0);
                 // A = V^T: dim 16b + c, keys 4g..4g+3 of both pages; lane c of group g points at key 4g + c/4, dims 4(c%4)..
                 const int vk = 4 * g + (c >> 2);
                 bf16x8 va[NB];
