@@ -241,7 +241,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
     __shared__ uint8_t s_plane[kMaxRows];
     __shared__ uint64_t s_run[4], s_first[4], s_end[4];
     __shared__ int s_sum[4];
-    __shared__ Work s_next[2];
+    __shared__ Work s_next[3];
     States& sf = *reinterpret_cast<States*>(smem + OBYTES);
     float* so = reinterpret_cast<float*>(smem);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -380,6 +380,22 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
         x.by_wave(wave);
         return x;
     };
+    // Wave 0 works a work out two turns ahead and leaves it in LDS.
+    auto put_work = [&](int slot, int w) {
+        if (wave != 0 || w >= n_all) return;
+        const Work x = load_work(w);
+        if (lane == 0) s_next[slot] = x;
+    };
+    auto get_work = [&](int slot) {
+        int f[kWorkInts];
+        __builtin_memcpy(f, &s_next[slot], sizeof f);
+#pragma unroll
+        for (int k = 0; k < kWorkInts; ++k) f[k] = __builtin_amdgcn_readfirstlane(f[k]);
+        Work x;
+        __builtin_memcpy(&x, f, sizeof f);
+        x.by_wave(wave);
+        return x;
+    };
     // lane l: the id of page l % 2 of pair l / 2 from page `from` on; -2: past the context
     auto page_ids = [&](const Work& x, int from) {
         const int pg = from + (lane >> 1) * (2 * kTreeWaves) + (lane & 1);
@@ -460,21 +476,22 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
     qraw[0] = qraw[1] = floatx4{0.f, 0.f, 0.f, 0.f};
     fetch_q(x);
     Pair pair = pair_of(x.head, ids, 0);
-    fetch(pair);
+    if (pair.there) fetch(pair);
+    put_work(0, work + gridDim.x);
     stage_q();
     __syncthreads();
-    for (int turn = 0;; turn ^= 1) {
+    for (int slot = 0;; slot = slot == 2 ? 0 : slot + 1) {
         const int next = work + gridDim.x;
         const int head = x.head;
-        // the next work: its first pages and q; the rest of it waits in LDS
+        // the next work: its first pages and q; the rest of it stays in LDS
         int ids2 = -2;
         int head2 = 0;
         if (next < n_all) {
-            const Work x2 = load_work(next);
+            const Work x2 = get_work(slot);
             ids2 = page_ids(x2, x2.p);
             fetch_q(x2);
-            if (tid == 0) s_next[turn] = x2;
             head2 = x2.head;
+            put_work(slot == 2 ? 0 : slot + 1, next + gridDim.x);
         }
         float tot[NR][2], tm = -1e30f, tw = 0.f;  // totals; lanes 8k..: row k's maximum and weight
 #pragma unroll
@@ -489,7 +506,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
             for (; i < pairs; p += 2 * kTreeWaves, ++i) {
                 const Pair now = pair;
                 const int there = now.there;
-                const bool masked = there != 3 || p * kPage + 2 * kPage > x.base;  // wave-uniform
+                const bool masked = there && (there != 3 || p * kPage + 2 * kPage > x.base);  // wave-uniform
                 uint32_t odd = 0;  // bits 15, 31: a V that is not finite where only some rows may see it
                 if (masked) {
 #pragma unroll
@@ -525,21 +542,24 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
                             }
                     }
                 }
+                if (there) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                    for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int j = 0; j < NJ; ++j) {
-                        const int f = j * 64 + lane, r = f / CPR, ch = f - r * CPR;
-                        *reinterpret_cast<u32x4*>(sk + (h * kPage + r) * KP + ch * 8) = kr[h][j];
-                        *reinterpret_cast<u32x4*>(sv + (h * kPage + r) * VP + ch * 8) = vr[h][j];
-                    }
+                        for (int j = 0; j < NJ; ++j) {
+                            const int f = j * 64 + lane, r = f / CPR, ch = f - r * CPR;
+                            *reinterpret_cast<u32x4*>(sk + (h * kPage + r) * KP + ch * 8) = kr[h][j];
+                            *reinterpret_cast<u32x4*>(sv + (h * kPage + r) * VP + ch * 8) = vr[h][j];
+                        }
+                }
                 // the next pair, of this work or the next one
                 const bool more = i + 1 < x.mine;
                 if (more && ((i + 1) & 31) == 0) ids = page_ids(x, p + 2 * kTreeWaves);
                 if (more || next < n_all) {
                     pair = pair_of(more ? head : head2, more ? ids : ids2, more ? i + 1 : 0);
-                    fetch(pair);
+                    if (pair.there) fetch(pair);
                 }
+                if (!there) continue;
                 // A = K: key c of either page, dims 32j + 8g ..
                 bf16x8 ka[2][NJ];
 #pragma unroll
@@ -734,12 +754,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
             }
         }
         if (next >= n_all) break;
-        int f[kWorkInts];
-        __builtin_memcpy(f, &s_next[turn], sizeof f);
-#pragma unroll
-        for (int k = 0; k < kWorkInts; ++k) f[k] = __builtin_amdgcn_readfirstlane(f[k]);
-        __builtin_memcpy(&x, f, sizeof f);
-        x.by_wave(wave);
+        x = get_work(slot);
         ids = ids2;
         work = next;
     }
