@@ -354,101 +354,81 @@ hipError_t launch_tree_accept(const cdb_drafts& d, const int32_t* row0, const in
 
 // ------------------------------------------------------------------ commit
 // Workgroup (unit, tree): one layer of one plane.  Entry i of the path goes from
-// position len + path[i] to len + i <= it.  A thread owns 16-byte columns of the
-// (K/V, head, dim) entry and takes the moves in order, loading eight before it
-// stores them: move i's destination is no later move's source (path[j] > path[i]
-// >= i for j > i), so nothing is overwritten before it is read.
+// position len + path[i] to len + i <= it.  Every wave reads what the move needs by
+// itself (lane = path entry, page, or plane), so nothing waits at a barrier; the
+// chain of dependent loads (path and sequence, length, page ids, data) bounds all
+// but large calls.  A thread owns 16-byte columns of the (K/V, head, dim) entry and
+// takes the moves in order, loading eight before it stores them: move i's
+// destination is no later move's source (path[j] > path[i] >= i for j > i), so
+// nothing is overwritten before it is read.
 constexpr int kCommitBatch = 8;
 
 __global__ __launch_bounds__(256) void k_tree_commit(int H, int hd, KvTarget kv, int plane0, int n_planes,
                                                      cdb_drafts dr, const int32_t* __restrict__ path_,
                                                      const int32_t* __restrict__ count_, int* err) {
-    __shared__ int s_path[CDB_TREE_MAX_NODES], s_pid[8];
-    __shared__ int s_from[CDB_TREE_MAX_NODES], s_to[CDB_TREE_MAX_NODES];  // page slot * 16 + token of each move
-    __shared__ int s_moves, s_skip;
-    const int t = blockIdx.y, tid = threadIdx.x;
+    const int t = blockIdx.y, lane = threadIdx.x & 63;
     const int layer = blockIdx.x / n_planes, plane = plane0 + blockIdx.x % n_planes;
-    const bool lead = blockIdx.x == 0;
-    const int n = count_[t];
+    const bool tells = blockIdx.x == 0 && threadIdx.x == 0;
+    const int n = count_[t], sq = dr.seq[t];
+    const int path = lane < dr.max_nodes ? path_[(size_t)t * dr.max_nodes + lane] : -1;
+    bool bad = false;
+    for (int k = lane; k < t; k += 64) bad |= dr.seq[k] == sq;  // an earlier tree of this sequence
     if (n == 0) return;
-    const int sq = dr.seq[t];
-    if (tid == 0) {
-        s_moves = 0;
-        s_skip = 0;
-    }
-    __syncthreads();
-    bool bad = n < 0 || n > dr.max_nodes || sq < 0 || sq >= kv.max_seqs || sq >= dr.max_seqs;
-    if (tid < t && dr.seq[tid] == sq) bad = true;  // t < 256 trees
-    if (!bad && tid < n) s_path[tid] = path_[(size_t)t * dr.max_nodes + tid];
-    if (bad) s_skip = 1;
-    __syncthreads();
-    if (s_skip) {
-        if (lead && tid == 0) set_err(err, CDB_DEV_BAD_INDEX);
-        return;
-    }
-    const int base = dr.len[sq];
-    if (base < 0 || base > kv.max_pages * kPage) bad = true;
-    if (tid < n) {
-        const int j = s_path[tid];
-        if (j < 0 || j >= dr.max_nodes || (tid > 0 && s_path[tid - 1] >= j) || base + j >= kv.max_pages * kPage) bad = true;
-    }
-    if (bad) s_skip = 1;
-    __syncthreads();
-    if (s_skip) {
-        if (lead && tid == 0) set_err(err, CDB_DEV_BAD_INDEX);
+    bad |= n < 0 || n > dr.max_nodes || sq < 0 || sq >= kv.max_seqs || sq >= dr.max_seqs;
+    const int before = __shfl_up(path, 1, 64);
+    bad |= lane < n && (path < 0 || path >= dr.max_nodes || (lane > 0 && before >= path));
+    if (__any(bad)) {
+        if (tells) set_err(err, CDB_DEV_BAD_INDEX);
         return;
     }
     // the moves, in order: path increases, so from the first i with path[i] > i on all entries move
-    const int pg0 = base / kPage;
-    if (tid < n && s_path[tid] != tid && (tid == 0 || s_path[tid - 1] == tid - 1)) s_moves = n - tid;
-    __syncthreads();
-    const int moves = s_moves, i0 = n - moves;
-    if (moves == 0) return;
-    const int pga = (base + i0) / kPage, pgb = (base + s_path[n - 1]) / kPage;  // pages the moves touch, at most 5
-    if (tid < moves) {
-        const int from = base + s_path[i0 + tid] - pg0 * kPage, to = base + i0 + tid - pg0 * kPage;
-        s_from[tid] = from;
-        s_to[tid] = to;
+    const uint64_t moved = __ballot(lane < n && path != lane);
+    const int base = dr.len[sq];
+    const int top = __builtin_amdgcn_readlane(path, n - 1);  // the highest node of the path
+    if (base < 0 || base > kv.max_pages * kPage || base + top >= kv.max_pages * kPage) {
+        if (tells) set_err(err, CDB_DEV_BAD_INDEX);
+        return;
     }
+    if (!moved) return;
+    const int i0 = __ffsll((unsigned long long)moved) - 1;
+    const int pga = (base + i0) / kPage, pgb = (base + top) / kPage;  // pages the moves touch, at most 5
     const int32_t* pt = kv.page_table + (size_t)sq * kv.n_planes * kv.max_pages;
-    const int32_t* own = pt + (size_t)plane * kv.max_pages;
-    if (tid >= pga - pg0 && tid <= pgb - pg0) {
-        const int id = own[pg0 + tid];
-        s_pid[tid] = id;
-        if (id < 0 || id >= kv.n_pages) {
-            set_err(err, CDB_DEV_UNMAPPED_PAGE);
-            s_skip = 1;
-        }
-    }
-    // planes of the pool with the same pages: the lowest of them moves them once
-    if (tid < n_planes && plane0 + tid != plane) {
-        const int32_t* other = pt + (size_t)(plane0 + tid) * kv.max_pages;
-        int same = 0;
+    // lane = page, then lane = plane of the pool with some, or all, of the same pages: the
+    // lowest of those that share all moves them once
+    const int pid = pga + lane <= pgb ? pt[(size_t)plane * kv.max_pages + pga + lane] : 0;
+    int same = 0;
+    if (lane < n_planes && plane0 + lane != plane) {
+        const int32_t* other = pt + (size_t)(plane0 + lane) * kv.max_pages;
+        const int32_t* own = pt + (size_t)plane * kv.max_pages;
         for (int g = pga; g <= pgb; ++g) same += other[g] == own[g];
-        if (same == pgb - pga + 1) {
-            if (plane0 + tid < plane) s_skip = 1;
-        } else if (same) {
-            set_err(err, CDB_DEV_BAD_INDEX);
-            s_skip = 1;
-        }
     }
-    __syncthreads();
-    if (s_skip) return;
+    if (__any(pid < 0 || pid >= kv.n_pages)) {
+        if (threadIdx.x == 0) set_err(err, CDB_DEV_UNMAPPED_PAGE);
+        return;
+    }
+    if (__any(same > 0 && same <= pgb - pga)) {
+        if (threadIdx.x == 0) set_err(err, CDB_DEV_BAD_INDEX);
+        return;
+    }
+    if (__any(same > 0 && plane0 + lane < plane)) return;
     const int vec_per_head = hd / 8, nvec = 2 * H * vec_per_head;
-    auto entry = [&](int at) {
-        return kv.pool + kv_offset(layer, s_pid[at / kPage], kv.n_pages, 0, 0, H, at % kPage, hd);
+    auto entry = [&](int pos) {
+        const int id = __builtin_amdgcn_readlane(pid, pos / kPage - pga);
+        return kv.pool + kv_offset(layer, id, kv.n_pages, 0, 0, H, pos % kPage, hd);
     };
-    for (int v = tid; v < nvec; v += 256) {
+    for (int v0 = 0; v0 < nvec; v0 += 256) {  // whole waves stay in the loop: they read one another's lanes
+        const int v = v0 + (int)threadIdx.x;
+        const bool in = v < nvec;
         const int kvh = v / vec_per_head, e = v - kvh * vec_per_head;
-        const size_t off = (size_t)kvh * kPage * hd + e * 8;
-        for (int b = 0; b < moves; b += kCommitBatch) {
-            uint4 buf[kCommitBatch];
+        const size_t off = in ? (size_t)kvh * kPage * hd + e * 8 : 0;
+        for (int b = i0; b < n; b += kCommitBatch) {
+            u32x4 buf[kCommitBatch];  // past the last move: that one's source again
 #pragma unroll
             for (int u = 0; u < kCommitBatch; ++u)
-                if (b + u < moves) buf[u] = *reinterpret_cast<const uint4*>(entry(s_from[b + u]) + off);
+                buf[u] = *reinterpret_cast<const u32x4*>(entry(base + __builtin_amdgcn_readlane(path, min(b + u, n - 1))) + off);
 #pragma unroll
             for (int u = 0; u < kCommitBatch; ++u)
-                if (b + u < moves) *reinterpret_cast<uint4*>(entry(s_to[b + u]) + off) = buf[u];
+                if (in && b + u < n) *reinterpret_cast<u32x4*>(entry(base + b + u) + off) = buf[u];
         }
     }
 }
