@@ -200,8 +200,8 @@ typedef struct {
  * (stage calls take up to 256 rows, cdb_prefill up to 512); 0 if unsupported. */
 size_t cdb_workspace_bytes(const cdb_model_desc* desc, int32_t max_rows);
 
-/* Clears the workspace's error code (a kernel, not a memset).  Call once after
- * allocating a workspace. */
+/* Clears the workspace's header, its error code among it (a kernel, not a
+ * memset).  Call once after allocating a workspace. */
 cdb_status cdb_workspace_init(void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Prelude stage (Section 4.1; Eq. 1 h^(0) = P(x_t)): h = E[tokens[i]], then the

@@ -59,8 +59,9 @@ typedef struct {
 } cdb_tree;
 
 /* Workspace of the calls below for up to max_rows rows (at most 256) and
- * max_seqs sequences; 0 if unsupported.  At least cdb_workspace_bytes(desc,
- * max_rows).  Cleared once by cdb_workspace_init. */
+ * max_seqs sequences (which need no room of their own); 0 if unsupported.  At
+ * least cdb_workspace_bytes(desc, max_rows).  Cleared once by
+ * cdb_workspace_init. */
 size_t cdb_tree_workspace_bytes(const cdb_model_desc* desc, int32_t max_rows, int32_t max_seqs);
 
 /* The free pages of one pool, a stack in device memory: free_ids[0 ..

@@ -645,9 +645,7 @@ cdb_status cdb_paged_attention(const cdb_model_desc* desc, const cdb_kv* kv, con
 
 size_t cdb_tree_workspace_bytes(const cdb_model_desc* desc, int32_t max_rows, int32_t max_seqs) {
     if (!desc || !desc_supported(*desc) || max_rows < 0 || max_rows > kMaxRows || max_seqs < 0) return 0;
-    // the stage layouts are not monotonic in the row count, the scratch behind them is
-    const size_t own = cdb_workspace_bytes(desc, max_rows);
-    return std::max(own + tree_scratch_bytes(*desc, max_rows), 256 + map_scratch_bytes(max_seqs));
+    return cdb_workspace_bytes(desc, max_rows) + tree_scratch_bytes(*desc, max_rows);
 }
 
 cdb_status cdb_map_pages(const cdb_model_desc* desc, int32_t* page_table, int32_t max_seqs, int32_t max_pages,
@@ -665,10 +663,9 @@ cdb_status cdb_map_pages(const cdb_model_desc* desc, int32_t* page_table, int32_
             return CDB_ERR_INVALID_ARG;
     // page and stack counts are summed in 32 bits
     if (max_pages > kMaxTablePages || (int64_t)max_seqs * max_pages * d.r_max > 0x3fffffff) return CDB_ERR_CAPACITY;
-    if (ws_bytes < 256 + map_scratch_bytes(max_seqs)) return CDB_ERR_CAPACITY;
+    if (ws_bytes < 256) return CDB_ERR_CAPACITY;
     const int width = kv_layout == 0 ? d.r_max : (kv_layout == 1 || d.r_max == 1) ? 1 : 2;
-    HIPCHK(launch_map_pages(d, page_table, max_seqs, max_pages, pools, width, len, mapped,
-                            reinterpret_cast<int32_t*>(static_cast<unsigned char*>(ws) + 256), static_cast<int*>(ws), st));
+    HIPCHK(launch_map_pages(d, page_table, max_seqs, max_pages, pools, width, len, mapped, static_cast<int*>(ws), st));
     return CDB_OK;
 }
 
@@ -760,15 +757,10 @@ cdb_status cdb_tree_commit(const cdb_model_desc* desc, const cdb_kv* kv, const c
     if (ws_bytes < 256) return CDB_ERR_CAPACITY;
     if (drafts->n_trees == 0) return CDB_OK;
     if (!accepted->path || !accepted->count || !kv->page_table) return CDB_ERR_INVALID_ARG;
-    for (int stage = 0; stage < 3; ++stage) {
-        const KvTarget t = stage_target(d, *kv, stage);
-        if (t.n_layers > 0 && (!t.pool || t.n_pages < 0)) return CDB_ERR_INVALID_ARG;
-    }
-    for (int stage = 0; stage < 3; ++stage) {
-        const KvTarget t = stage_target(d, *kv, stage);
-        HIPCHK(launch_tree_commit(d, t, stage == 1 ? 1 : t.plane_fixed, stage == 1 ? d.r_max : 1, *drafts, *accepted,
-                                  static_cast<int*>(ws), st));
-    }
+    const KvTarget t[3] = {stage_target(d, *kv, 0), stage_target(d, *kv, 1), stage_target(d, *kv, 2)};
+    for (const KvTarget& k : t)
+        if (k.n_layers > 0 && (!k.pool || k.n_pages < 0)) return CDB_ERR_INVALID_ARG;
+    HIPCHK(launch_tree_commit(d, t, *drafts, *accepted, static_cast<int*>(ws), st));
     return CDB_OK;
 }
 

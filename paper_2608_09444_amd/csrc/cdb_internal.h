@@ -67,6 +67,10 @@ __device__ __forceinline__ int live_rows(const int32_t* dn, int M) {
     return n < 0 ? 0 : (n > M ? M : n);
 }
 
+// Workspace header (ints): the sticky error code, then workgroups of a page
+// mapping that are through (0 between calls).
+constexpr int kWsArrive = 1;
+
 // First sticky error wins.
 __device__ __forceinline__ void set_err(int* err, int code) { atomicCAS(err, 0, code); }
 
@@ -227,24 +231,21 @@ hipError_t launch_ws_init(int* err, hipStream_t st);
 
 // ---------------------------------------------------------------- drafted trees
 // bytes of the tree attention's scratch behind a stage call's workspace (or its
-// first 256 bytes), and of cdb_map_pages' behind the first 256
+// first 256 bytes)
 size_t tree_scratch_bytes(const cdb_model_desc& d, int rows);
-inline size_t map_scratch_bytes(int max_seqs) { return (4 + (size_t)max_seqs) * 4; }
 // attention of drafted rows (base, mask as in cdb_tree)
 hipError_t launch_tree_attention(const float* q, const KvTarget& kv, const int32_t* seq, const cdb_tree& tree, int M,
                                  int H, int hd, void* scratch, uint16_t* out, int* err, hipStream_t st,
                                  const int32_t* dn);
-// pools: prelude, core, coda; core_width: distinct core pages per token page;
-// scratch: 4 + S ints
+// pools: prelude, core, coda; core_width: distinct core pages per token page
 hipError_t launch_map_pages(const cdb_model_desc& md, int32_t* table, int S, int P, const cdb_page_pool* const* pools,
-                            int core_width, const int32_t* len, int32_t* mapped, int32_t* scratch, int* err,
-                            hipStream_t st);
+                            int core_width, const int32_t* len, int32_t* mapped, int* ws, hipStream_t st);
 hipError_t launch_tree_rows(const cdb_drafts& d, const cdb_row_map& out, int* err, hipStream_t st);
 hipError_t launch_tree_accept(const cdb_drafts& d, const int32_t* row0, const int32_t* next_ids, int n_rows,
                               const int32_t* first_ids, const cdb_accepted& out, int* err, hipStream_t st);
-// one stage: planes plane0 .. plane0 + n_planes - 1 of kv's pool
-hipError_t launch_tree_commit(const cdb_model_desc& md, const KvTarget& kv, int plane0, int n_planes,
-                              const cdb_drafts& d, const cdb_accepted& acc, int* err, hipStream_t st);
+// kv: of the three stages
+hipError_t launch_tree_commit(const cdb_model_desc& md, const KvTarget (&kv)[3], const cdb_drafts& d,
+                              const cdb_accepted& acc, int* err, hipStream_t st);
 
 enum PackKind : int { PACK_PLAIN = 0, PACK_QKV = 1, PACK_GU = 2 };
 

@@ -572,7 +572,7 @@ __global__ void k_copy16(const uint16_t* __restrict__ s, size_t n, uint16_t* __r
 }
 
 __global__ void k_ws_init(int* err) {
-    if (threadIdx.x == 0) *err = 0;
+    if (threadIdx.x == 0) err[0] = err[kWsArrive] = 0;
 }
 
 // ------------------------------------------------------------------ launchers

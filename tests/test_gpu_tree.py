@@ -150,6 +150,14 @@ def test_pages_follow_the_lengths(layout, S, P):
     assert codes == [0] * 6
 
 
+@pytest.mark.parametrize("layout", [tree.KV_FULL, tree.KV_FIRST_THEN_SHARED])
+def test_pages_of_many_sequences(layout):
+    """Several sequences to a thread of every workgroup."""
+    S, P, shape = 1100, 3, cdbgen.shrink(cdbgen.TINY, n_prelude=0)
+    _say(f"[gpu] map pages: {S} sequences, layout {layout}")
+    assert _map_case(shape, S, P, layout, (0, S * P * shape.r_max, S * P), 5, 21) == [0] * 5
+
+
 @pytest.mark.parametrize("r_max", [1, 64])
 def test_pages_of_models_without_prelude(r_max):
     shape = cdbgen.shrink(cdbgen.TINY, n_prelude=0, n_coda=0, r_max=r_max)
@@ -815,6 +823,19 @@ def test_commit_of_wide_models(hd, H):
     _host_commit(shape, host, kv.page_table.cpu().numpy(), seq, length, path, count)
     _say(f"[gpu] commit {H} x {hd}")
     assert _run_commit(shape, kv, seq, length, path, count, ws, 50) == 0
+    assert torch.equal(kv.core.cpu(), host[0][0])
+
+
+def test_commit_of_many_layers_and_trees():
+    """1088 (layer, plane, tree) triples of 320 columns: one workgroup each."""
+    shape = _shape(64, 20)
+    shape = cdbgen.shrink(shape, n_core=16)
+    counts = [int(c) for c in np.random.default_rng(3).integers(0, 9, 17)]
+    kv, seq, length, path, count, ws = _commit_setup(shape, counts, 8, tree.KV_FULL, 31, hi=20)
+    host = [(kv.core.cpu().clone(), range(1, shape.r_max + 1))]
+    _host_commit(shape, host, kv.page_table.cpu().numpy(), seq, length, path, count)
+    _say("[gpu] commit: many layers and trees")
+    assert _run_commit(shape, kv, seq, length, path, count, ws, 8) == 0
     assert torch.equal(kv.core.cpu(), host[0][0])
 
 

@@ -36,7 +36,7 @@ def test_workspace_serves_every_smaller_call(shape):
     sizes = [tree.cdb_tree_workspace_bytes(desc, r, 300) for r in range(cdb.MAX_ROWS + 1)]
     assert all(b >= a for a, b in zip(sizes, sizes[1:]))
     assert all(b >= cdb.cdb_workspace_bytes(desc, r) for r, b in enumerate(sizes))
-    assert sizes[0] >= 256 + 4 * 300
+    assert sizes[0] >= 256
     assert tree.cdb_tree_workspace_bytes(desc, cdb.MAX_ROWS + 1, 1) == 0
     assert tree.cdb_tree_workspace_bytes(desc, -1, 1) == 0
     assert tree.cdb_tree_workspace_bytes(desc, 1, -1) == 0
@@ -54,7 +54,7 @@ def test_map_pages_refusals():
                {"core": tree.cdb_page_pool(1, 1, -1)}, {"desc": None}):
         assert call(**kw) == INVALID, kw
     assert call(desc=BAD_DESC) == UNSUPPORTED
-    assert call(nb=256 + 4 * 5) == CAPACITY  # one int per sequence and four more
+    assert call(nb=255) == CAPACITY
     assert call(P=1 << 28) == CAPACITY
     assert call(S=1 << 20, P=1 << 20) == CAPACITY
 
