@@ -85,7 +85,8 @@ typedef struct {
  * First the given-back pages go onto each stack, the last in (sequence, page,
  * plane) order first; then new ones come off it in (sequence, page, plane)
  * order.  Cutting a sequence back right after growing it so restores the stack.
- * A stack's entries from its count on are not cleared.  All or nothing: if
+ * A stack's entries from its count on keep what stood there last.  All or
+ * nothing: if
  * a pool has too few pages (or its stack too few entries), a length needs more
  * than max_pages pages, or mapped or a count is out of range, nothing changes
  * and the workspace's error code is set (CDB_DEV_NO_PAGES, CDB_DEV_BAD_INDEX). */

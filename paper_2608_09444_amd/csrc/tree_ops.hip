@@ -94,10 +94,9 @@ __device__ __forceinline__ size_t map_cell(const MapArgs& a, int k, const int* b
 // One launch: every workgroup sums the page counts of all sequences itself (a
 // thread `per` of them) and takes its share of the entries.  Entry j that is given
 // back lands on the stack at count + all - 1 - j, and the j-th one that is taken
-// comes from there, so it goes straight from cell to cell while both sides last;
-// the rest goes onto the stack, or comes off it below `count`, where this call
-// writes nothing.  The workgroup that is through last writes mapped and the
-// counts, which all have read by then.
+// comes from there, so its thread has it already; the others come off the stack
+// below `count`, where this call writes nothing.  The workgroup that is through
+// last writes mapped and the counts, which all have read by then.
 __global__ __launch_bounds__(256) void k_map_pages(MapArgs a) {
     __shared__ int s_back[256], s_more[256], red[8], s_bad, s_last;
     const int tid = threadIdx.x, per = (a.S + 255) / 256;
@@ -145,14 +144,12 @@ __global__ __launch_bounds__(256) void k_map_pages(MapArgs a) {
                     const size_t cell = map_cell(a, k, s_back, per, j, true);
                     id = a.table[cell];
                     put(cell, -1);
+                    a.free_ids[k][top - j] = id;
                 } else {
                     id = a.free_ids[k][top - j];
                 }
                 if (id < 0) set_err(a.ws, CDB_DEV_UNMAPPED_PAGE);
-                if (j < more)
-                    put(map_cell(a, k, s_more, per, j, false), id);
-                else
-                    a.free_ids[k][top - j] = id;
+                if (j < more) put(map_cell(a, k, s_more, per, j, false), id);
             }
         }
     __syncthreads();

@@ -69,6 +69,7 @@ class HostPages:
         self.mapped = np.zeros(S, np.int32)
         self.layers = (shape.n_prelude, shape.n_core, shape.n_coda)
         self.stacks = [list(s) for s in start]
+        self.arrays = [np.array(s) for s in start]  # with what stood there last above the counts
         self.caps = caps
 
     def groups(self, k):
@@ -104,6 +105,7 @@ class HostPages:
                         gone.append(int(self.table[s, planes[0], p]))
                         self.table[s, planes, p] = -1
             self.stacks[k] += gone[::-1]
+            self.arrays[k][:len(self.stacks[k])] = self.stacks[k]
             for s, w in enumerate(want):
                 for p in range(int(self.mapped[s]), w):
                     for planes in self.groups(k):
@@ -134,9 +136,9 @@ def _map_case(shape, S, P, layout, caps, steps, seed, tight=False):
         assert cdb.cdb_read_device_error(ws.buf) == code, step
         assert (table.cpu().numpy() == host.table).all(), step
         assert (mapped.cpu().numpy() == host.mapped).all(), step
-        for p, s in zip(pools, host.stacks):
+        for p, s, a in zip(pools, host.stacks, host.arrays):
             if p:
-                assert int(p.free_count) == len(s) and p.free_ids[:len(s)].tolist() == s, step
+                assert int(p.free_count) == len(s) and p.free_ids.tolist() == a.tolist(), step
     return codes
 
 
