@@ -8,8 +8,10 @@
 //
 // Tiles: adjacent rows of one sequence, plane and base, at most 16, 32 or 64 of
 // them (by cdb_tree.max_nodes).  A row's context is cut into segments
-// (tree_segments, by its base alone).  Every workgroup works out all tiles itself
-// at its start, which costs less than a launch that would do it once.
+// (tree_segments, by its base alone).  Every wave works out all tiles itself at its
+// start, which costs less than a launch that would do it once, or than barriers
+// between waves that share it (12.4 us against 13.2, 13 rows over 700 positions;
+// 256 rows lose a little: 20.0 against 19.5, 16 trees of 16 over 640).
 //
 // k_tree_attn: a workgroup takes works in turn: the segments of one tile and head,
 // or, when that leaves CUs idle, a run of them.  Its 8 waves deal a segment's
@@ -140,6 +142,33 @@ __device__ __forceinline__ float over_8_sum(float v) {
     v += CDB_TREE_DPP(v, 0x4E);
     return v + CDB_TREE_DPP(v, 0x141);
 }
+// The lane before's value (lane 0: 0).
+__device__ __forceinline__ int lane_before(int v) { return __builtin_amdgcn_update_dpp(0, v, 0x138, 0xF, 0xF, false); }
+// Inclusive prefix sum: within 16 lanes, then lane 15 of each into the next 16, lane 31 into the upper half.
+__device__ __forceinline__ int scan64(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+    return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+}
+// Over the wave: quads, halves of 16, 16, 32, 64 lanes.
+__device__ __forceinline__ uint64_t over_wave_or(uint64_t v) {
+    uint32_t w[2] = {(uint32_t)v, (uint32_t)(v >> 32)};
+#pragma unroll
+    for (uint32_t& x : w) {
+        x |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true);
+        x |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true);
+        x |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, true);
+        x |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xF, 0xF, true);
+        auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        x = r[0] | r[1];
+        r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        x = __builtin_amdgcn_readfirstlane(r[0] | r[1]);
+    }
+    return (uint64_t)w[1] << 32 | w[0];
+}
 __device__ __forceinline__ float lane_value(float v, int lane) {
     return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
 }
@@ -230,17 +259,13 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
     struct States {  // the waves' maxima and weights
         float m[ROWS][kTreeWaves], l[ROWS][kTreeWaves];
     };
-    struct Rows {  // at the start: the call's rows
-        int seq[kMaxRows], plane[kMaxRows], base[kMaxRows];
-    };
-    static_assert(OBYTES + sizeof(States) <= VBYTES && sizeof(Rows) <= VBYTES, "they leave q alone");
+    static_assert(OBYTES + sizeof(States) <= VBYTES, "they leave q alone");
     __shared__ __align__(16) unsigned char smem[VBYTES + QBYTES];
-    __shared__ uint32_t s_tile[kMaxRows];  // works before the tile << 16 | its first row << 8 | its rows - 1
-    __shared__ int s_seq[kMaxRows], s_base[kMaxRows];  // of the tile's rows
-    __shared__ uint64_t s_seen[kMaxRows];              // mask bits of any of them
-    __shared__ uint8_t s_plane[kMaxRows];
-    __shared__ uint64_t s_run[4], s_first[4], s_end[4];
-    __shared__ int s_sum[4];
+    __shared__ uint8_t s_row[kMaxRows], s_plane[kMaxRows];  // by tile: its first row, its rows' plane,
+    __shared__ int s_seq[kMaxRows], s_base[kMaxRows];       // sequence and base,
+    __shared__ uint16_t s_before[kMaxRows];                 // and the works before it, if some tile has several
+    __shared__ uint64_t s_mask[kMaxRows];                   // by row
+    __shared__ uint64_t s_ends[kMaxRows / 64 + 2];          // bit: a row that starts a tile or has none
     __shared__ Work s_next[3];
     States& sf = *reinterpret_cast<States*>(smem + OBYTES);
     float* so = reinterpret_cast<float*>(smem);
@@ -249,91 +274,69 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
     const int d = H * HD;
     const float qscale = 1.4426950408889634f / sqrtf((float)HD);
 
-    // ---- tiles (threads 0..255: thread = row)
-    int n_tiles, runs, n_works;
+    // ---- tiles.  Every wave works them out by itself (lane = row of each 64), and all
+    // leave the same values in LDS: no wave waits for another.
+    int n_tiles = 0, runs, n_works = 0;
     {
-        Rows& sr = *reinterpret_cast<Rows*>(smem);
-        const int w = wave;
-        const bool rows_wave = w < kMaxRows / 64;
-        const bool mine = tid < M;  // M <= 256
-        RowSees r{};
-        bool ok = false;
-        if (rows_wave) {
-            if (mine) r = row_sees(kv, seq, tree, tid);
-            ok = mine && tid < live_rows(dn, M) && r.ok;
-            if (mine && !r.ok && tid < live_rows(dn, M) && blockIdx.x == 0) set_err(err, CDB_DEV_UNMAPPED_PAGE);
-            sr.seq[tid] = ok ? r.seq : -1;
-            sr.plane[tid] = r.plane;
-            sr.base[tid] = r.base;
-            s_seen[tid] = 0;
-        }
-        __syncthreads();
-        uint64_t my_runs = 0;
-        if (rows_wave) {
-            my_runs = __ballot(ok && !(tid > 0 && sr.seq[tid - 1] == r.seq && sr.plane[tid - 1] == r.plane &&
-                                       sr.base[tid - 1] == r.base));
-            if (lane == 0) s_run[w] = my_runs;
-        }
-        __syncthreads();
-        bool first = false;
-        uint64_t firsts = 0, ends = 0;
-        if (rows_wave) {
-            int start = tid;  // the row at which this one's run started
-            uint64_t b = my_runs & (~0ull >> (63 - lane));
-            int word = w;
-            while (!b && word > 0) b = s_run[--word];
-            if (b) start = word * 64 + 63 - __clzll((long long)b);
-            first = ok && (tid - start) % CAP == 0;
-            firsts = __ballot(first);
-            ends = __ballot(first || !ok);
-            if (lane == 0) {
-                s_first[w] = firsts;
-                s_end[w] = ends;
-            }
-        }
-        __syncthreads();
-        n_tiles = 0;
-        int tile = __popcll(firsts & ((1ull << lane) - 1));
-        for (int k = 0; k < 4; ++k) {
-            const int f = __popcll(s_first[k]);
-            n_tiles += f;
-            if (k < w) tile += f;
-        }
-        runs = tree_runs(n_tiles * H * (HALVES ? 2 : 1));
-        int rows = 0, works = 0;
-        if (first) {
-            uint64_t b = lane == 63 ? 0 : ends & (~0ull << (lane + 1));
-            int word = w;
-            while (!b && word < 3) b = s_end[++word];
-            rows = (b ? word * 64 + __ffsll((unsigned long long)b) - 1 : kMaxRows) - tid;
-            int sp;
-            works = min(runs, tree_segments(r.base / kPage + 1, &sp));
-        }
-        int at = works;
-        if (rows_wave) {
+        constexpr int WORDS = kMaxRows / 64;
+        const int live = live_rows(dn, M);
+        RowSees r[WORDS];
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int u = __shfl_up(at, o, 64);
-                if (lane >= o) at += u;
+        for (int k = 0; k < WORDS; ++k)
+            if (64 * k < M) r[k] = row_sees(kv, seq, tree, min(64 * k + lane, M - 1));
+        int start = 0;  // the row at which the last run before these 64 started
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) {
+            uint64_t ends = ~0ull;
+            if (64 * k < M) {
+                const int row = 64 * k + lane;
+                const bool ok = row < live && r[k].ok;
+                if (row < live && !ok && wave == 0 && blockIdx.x == 0) set_err(err, CDB_DEV_UNMAPPED_PAGE);
+                if (!ok) r[k].seq = -1;
+                s_mask[row] = r[k].mask;
+                int pseq = lane_before(r[k].seq), pplane = lane_before(r[k].plane), pbase = lane_before(r[k].base);
+                if (k > 0) {
+                    const RowSees& last = r[k > 0 ? k - 1 : 0];
+                    pseq = lane > 0 ? pseq : __builtin_amdgcn_readlane(last.seq, 63);
+                    pplane = lane > 0 ? pplane : __builtin_amdgcn_readlane(last.plane, 63);
+                    pbase = lane > 0 ? pbase : __builtin_amdgcn_readlane(last.base, 63);
+                }
+                const uint64_t run =
+                    __ballot(ok && !(row > 0 && pseq == r[k].seq && pplane == r[k].plane && pbase == r[k].base));
+                const uint64_t b = run & (~0ull >> (63 - lane));
+                const bool first = ok && (row - (b ? 64 * k + 63 - __clzll((long long)b) : start)) % CAP == 0;
+                const uint64_t firsts = __ballot(first);
+                ends = __ballot(first || !ok);
+                if (run) start = 64 * k + 63 - __clzll((long long)run);
+                if (first) {
+                    const int tile = n_tiles + __builtin_amdgcn_mbcnt_hi((uint32_t)(firsts >> 32),
+                                                                         __builtin_amdgcn_mbcnt_lo((uint32_t)firsts, 0));
+                    s_row[tile] = (uint8_t)row;
+                    s_seq[tile] = r[k].seq;
+                    s_base[tile] = r[k].base;
+                    s_plane[tile] = (uint8_t)r[k].plane;  // at most r_max + 1 <= 65
+                }
+                n_tiles += __popcll(firsts);
             }
-            if (lane == 63) s_sum[w] = at;
+            s_ends[k] = ends;
         }
-        __syncthreads();
-        n_works = 0;
-        for (int k = 0; k < 4; ++k) {
-            const int f = s_sum[k];
-            n_works += f;
-            if (k < w) at += f;
+        s_ends[WORDS] = s_ends[WORDS + 1] = ~0ull;
+        runs = tree_runs(n_tiles * H * (HALVES ? 2 : 1));
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // what lanes have written, others read
+        n_works = n_tiles;
+        if (runs > 1) {
+            n_works = 0;
+            for (int t = 0; t < n_tiles; t += 64) {
+                int sp;
+                const int works =
+                    t + lane < n_tiles ? min(runs, tree_segments(s_base[min(t + lane, kMaxRows - 1)] / kPage + 1, &sp)) : 0;
+                const int at = scan64(works);
+                if (t + lane < n_tiles) s_before[t + lane] = (uint16_t)(n_works + at - works);
+                n_works += __builtin_amdgcn_readlane(at, 63);
+            }
         }
-        if (first) {
-            s_tile[tile] = (uint32_t)(at - works) << 16 | (uint32_t)tid << 8 | (uint32_t)(rows - 1);
-            s_seq[tile] = r.seq;
-            s_base[tile] = r.base;
-            s_plane[tile] = (uint8_t)r.plane;  // at most r_max + 1 <= 65
-        }
-        if (ok) atomicOr(reinterpret_cast<unsigned long long*>(&s_seen[first ? tile : tile - 1]), r.mask);
         if (tid == 0 && blockIdx.x == 0) *ts.runs = runs;
-        __syncthreads();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // what lanes have written, others read
     }
 
     // Work w: with halves, workgroups 8 apart, which run on one XCD at one time, take
@@ -351,18 +354,23 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
         }
         const int item = wh / H;
         x.head = wh - item * H;
-        int tile = -1;  // the last one whose works start at or before `item`
-        for (int k = 0; k < n_tiles; k += 64)
-            tile += __popcll(__ballot(k + lane < n_tiles && (int)(s_tile[min(k + lane, kMaxRows - 1)] >> 16) <= item));
-        const uint32_t e = __builtin_amdgcn_readfirstlane(s_tile[tile]);
-        const int tile0 = e >> 8 & 255, rows = (e & 255) + 1;
+        int tile = item, run = 0;
+        if (runs > 1) {  // the last tile whose works start at or before `item`
+            tile = -1;
+            for (int k = 0; k < n_tiles; k += 64)
+                tile += __popcll(__ballot(k + lane < n_tiles && s_before[min(k + lane, kMaxRows - 1)] <= item));
+            run = item - s_before[tile];
+        }
+        const int tile0 = __builtin_amdgcn_readfirstlane((int)s_row[tile]), from = tile0 + 1;
+        uint64_t ends = s_ends[from >> 6] >> (from & 63);
+        if (from & 63) ends |= s_ends[(from >> 6) + 1] << (64 - (from & 63));
+        const int rows = ends ? __ffsll((unsigned long long)ends) : 64;
         x.seq = __builtin_amdgcn_readfirstlane(s_seq[tile]);
         x.base = __builtin_amdgcn_readfirstlane(s_base[tile]);
         x.plane = __builtin_amdgcn_readfirstlane((int)s_plane[tile]);
-        x.seen = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(s_seen[tile] >> 32)) << 32 |
-                 (uint32_t)__builtin_amdgcn_readfirstlane((int)s_seen[tile]);
+        x.seen = over_wave_or(lane < rows ? s_mask[min(tile0 + lane, kMaxRows - 1)] : 0);
         x.nseg = tree_segments(x.base / kPage + 1, &x.sp);
-        const int z = min(runs, x.nseg), run = item - (int)(e >> 16);
+        const int z = min(runs, x.nseg);
         if (z == x.nseg) {
             x.sg0 = run;
             x.sg1 = run + 1;
@@ -606,7 +614,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     if (masked) {
-                        const uint64_t mask = tree.mask[x.row0 + max(0, min(t * 16 + c, x.n - 1))];
+                        const uint64_t mask = s_mask[x.row0 + max(0, min(t * 16 + c, x.n - 1))];
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const uint32_t see = sees4(mask, (p + h) * kPage + 4 * g - x.base) & (there >> h & 1 ? 15u : 0u);
@@ -676,7 +684,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
                             hw = __shfl(hw, from, 64);
                             lw = __shfl(lw, from, 64);
                             const float pk = kk & 1 ? bfhi(hw) + bfhi(lw) : bflo(hw) + bflo(lw);
-                            const bool see = tree.mask[x.row0 + max(0, min(t * 16 + c, x.n - 1))] >> off & 1;
+                            const bool see = s_mask[x.row0 + max(0, min(t * 16 + c, x.n - 1))] >> off & 1;
 #pragma unroll
                             for (int b = 0; b < NB; ++b)
 #pragma unroll
