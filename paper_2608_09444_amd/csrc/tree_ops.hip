@@ -344,15 +344,15 @@ hipError_t launch_tree_accept(const cdb_drafts& d, const int32_t* row0, const in
 // Workgroup (unit, tree): one layer of one plane of one stage.  Entry i of the path goes from
 // position len + path[i] to len + i <= it.  Every wave reads what the move needs by
 // itself (lane = path entry, page, or plane), so nothing waits at a barrier; the
-// chain of dependent loads (path and sequence, length, page ids, data) bounds all
-// but large calls.  A thread owns 16-byte columns of the (K/V, head, dim) entry and
-// takes the moves in order, loading eight before it stores them: move i's
-// destination is no later move's source (path[j] > path[i] >= i for j > i), so
-// nothing is overwritten before it is read.
+// chain of dependent loads (path and sequence, length, page ids, data) bounds it.  A
+// thread owns 16-byte columns of the (K/V, head, dim) entry, two at once, and takes
+// the moves in order, loading eight before it stores them: move i's destination is
+// no later move's source (path[j] > path[i] >= i for j > i), so nothing is
+// overwritten before it is read.
 constexpr int kCommitBatch = 8;
-// Up to so many (unit, tree) pairs, workgroups share a unit's columns (256 each):
-// one tree of 24 nodes over 96 units 4.8 us against 5.95; 64 of 4 over 3072 units
-// 14.5 us that way against 13.5.
+// Up to so many (unit, tree) pairs, workgroups share a unit's columns: one tree of
+// 24 nodes over 96 units 5.0 us against 5.8; 64 of 4 over 3072 units 11.1 us that
+// way against 7.9.
 constexpr int kCommitSplit = 1024;
 
 struct CommitStages {
@@ -426,19 +426,34 @@ __global__ __launch_bounds__(256) void k_tree_commit(int H, int hd, CommitStages
         const int id = __builtin_amdgcn_readlane(pid, pos / kPage - pga);
         return kv.pool + kv_offset(layer, id, kv.n_pages, 0, 0, H, pos % kPage, hd);
     };
-    for (int v0 = blockIdx.z * 256; v0 < nvec; v0 += gridDim.z * 256) {  // whole waves stay in the loop: they read one another's lanes
-        const int v = v0 + (int)threadIdx.x;
-        const bool in = v < nvec;
-        const int kvh = v / vec_per_head, e = v - kvh * vec_per_head;
-        const size_t off = in ? (size_t)kvh * kPage * hd + e * 8 : 0;
+    // two columns a thread; whole waves stay in the loop, as they read one another's lanes
+    for (int v0 = blockIdx.z * 256; v0 < nvec; v0 += gridDim.z * 512) {
+        size_t off[2];
+        bool in[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const int v = v0 + y * gridDim.z * 256 + (int)threadIdx.x;
+            in[y] = v < nvec;
+            const int kvh = v / vec_per_head, e = v - kvh * vec_per_head;
+            off[y] = in[y] ? (size_t)kvh * kPage * hd + e * 8 : 0;
+        }
         for (int b = i0; b < n; b += kCommitBatch) {
-            u32x4 buf[kCommitBatch];  // past the last move: that one's source again
+            u32x4 buf[2][kCommitBatch];
 #pragma unroll
             for (int u = 0; u < kCommitBatch; ++u)
-                buf[u] = *reinterpret_cast<const u32x4*>(entry(base + __builtin_amdgcn_readlane(path, min(b + u, n - 1))) + off);
+                if (b + u < n) {
+                    const uint16_t* at = entry(base + __builtin_amdgcn_readlane(path, b + u));
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) buf[y][u] = *reinterpret_cast<const u32x4*>(at + off[y]);
+                }
 #pragma unroll
             for (int u = 0; u < kCommitBatch; ++u)
-                if (in && b + u < n) *reinterpret_cast<u32x4*>(entry(base + b + u) + off) = buf[u];
+                if (b + u < n) {
+                    uint16_t* at = entry(base + b + u);
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        if (in[y]) *reinterpret_cast<u32x4*>(at + off[y]) = buf[y][u];
+                }
         }
     }
 }
