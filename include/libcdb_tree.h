@@ -41,7 +41,7 @@ extern "C" {
 enum { CDB_DEV_NO_PAGES = 4 };
 
 /* What a row of drafted tokens sees, beside cdb_rows (device arrays of n_rows
- * entries; rows past a device row count are not read).
+ * entries; those past a device row count do not matter).
  *   base      committed positions of the row's sequence: 0..base - 1 are visible
  *   mask      bit j: cache position base + j is visible too (its own included)
  *   rope_pos  the position the row's token stands at (RoPE); cdb_rows.pos is the
@@ -81,7 +81,8 @@ typedef struct {
  *   len, mapped device int32 [max_seqs]
  *   kv_layout   CDB_KV_FULL, CDB_KV_SHARED or CDB_KV_FIRST_THEN_SHARED
  *               (libcdb_driver.h): which core planes share a page
- *   pre, core, coda  the pools of the stages with layers (others are not read)
+ *   pre, core, coda  the pools of the stages with layers (others are not read),
+ *               each with a stack of its own
  * First the given-back pages go onto each stack, the last in (sequence, page,
  * plane) order first; then new ones come off it in (sequence, page, plane)
  * order.  Cutting a sequence back right after growing it so restores the stack.
@@ -140,7 +141,8 @@ cdb_status cdb_tree_rows(const cdb_drafts* drafts, const cdb_row_map* out, void*
  * out and stage / layer arguments): row i attends to the positions that
  * tree->base[i] and tree->mask[i] name, in its own plane.  Reads the cache only;
  * the rows' own K/V must be in it.  What a masked position holds (NaN included)
- * does not reach a row.  A row that sees nothing gets zeros.  A row whose
+ * does not reach a row.  A row that sees nothing gets zeros.  The stage's pool
+ * has at least one page, however few are mapped.  A row whose
  * sequence, loop index or positions are out of range is skipped
  * (CDB_DEV_UNMAPPED_PAGE), an unmapped page is left out (the same code). */
 cdb_status cdb_tree_attention(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_rows* rows,
@@ -185,7 +187,8 @@ cdb_status cdb_tree_accept(const cdb_drafts* drafts, const int32_t* row0, const 
 
 /* Moves the K/V of each tree's accepted nodes from cache position len + path[i]
  * to len + i, in every layer and plane of every stage (planes that share their
- * pages once), so that the context goes on without gaps.  accepted->next is not
+ * pages once), so that the context goes on without gaps.  No other sequence maps
+ * the pages of these positions.  accepted->next is not
  * read; `drafts` needs seq and len only.  The caller then adds count to len.  A
  * path that is not increasing or not in [0, max_nodes), a sequence out of range
  * or given twice (the later tree) and planes that share some but not all pages

@@ -661,6 +661,11 @@ cdb_status cdb_map_pages(const cdb_model_desc* desc, int32_t* page_table, int32_
     for (int k = 0; k < 3; ++k)
         if (layers[k] && (!pools[k] || !pools[k]->free_ids || !pools[k]->free_count || pools[k]->capacity < 0))
             return CDB_ERR_INVALID_ARG;
+    for (int k = 0; k < 3; ++k)
+        for (int j = 0; j < k; ++j)  // one stack has one owner
+            if (layers[k] && layers[j] &&
+                (pools[k]->free_ids == pools[j]->free_ids || pools[k]->free_count == pools[j]->free_count))
+                return CDB_ERR_INVALID_ARG;
     // page and stack counts are summed in 32 bits
     if (max_pages > kMaxTablePages || (int64_t)max_seqs * max_pages * d.r_max > 0x3fffffff) return CDB_ERR_CAPACITY;
     if (ws_bytes < 256) return CDB_ERR_CAPACITY;

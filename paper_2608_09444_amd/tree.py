@@ -69,12 +69,13 @@ def lib() -> C.CDLL:
     return L
 
 
-def _stream(stream) -> int:
-    """The stream's handle.  The current one is looked up without making a Stream object, which would take longer than
-    the smaller of these calls run."""
-    if stream is not None:
-        return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+def _stream(fn, stream, ws) -> int:
+    """The stream's handle.  Workspace and stream belong to the current device, on which the kernels run.  The current
+    stream is looked up without making a Stream object, which would take longer than the smaller of these calls run."""
+    here = torch.cuda.current_device()
+    if ws.device.index != here or (stream is not None and stream.device.index != here):
+        raise CdbError(fn, CDB_ERR_INVALID_ARG)
+    return torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream
 
 
 def _need(fn, ok):
@@ -114,7 +115,7 @@ def cdb_map_pages(desc: cdb_model_desc, page_table, pre, core, coda, kv_layout: 
     lens, have = (_flat("cdb_map_pages", t, torch.int32, S) for t in (length, mapped))
     _check("cdb_map_pages", lib().cdb_map_pages(C.byref(desc), page_table.data_ptr(), S, P, _ref(pre), _ref(core),
                                                 _ref(coda), kv_layout, lens, have, ws.data_ptr(), ws.numel(),
-                                                _stream(stream)))
+                                                _stream("cdb_map_pages", stream, ws)))
 
 
 def _trees_fit(fn, drafts, holder):
@@ -129,7 +130,7 @@ def _rows_fit(fn, rows, tree):
 
 def cdb_tree_rows(drafts: cdb_drafts, out: cdb_row_map, ws, stream=None):
     _trees_fit("cdb_tree_rows", drafts, out)
-    _check("cdb_tree_rows", lib().cdb_tree_rows(C.byref(drafts), C.byref(out), _ptr(ws), ws.numel(), _stream(stream)))
+    _check("cdb_tree_rows", lib().cdb_tree_rows(C.byref(drafts), C.byref(out), _ptr(ws), ws.numel(), _stream("cdb_tree_rows", stream, ws)))
 
 
 def cdb_tree_attention(desc: cdb_model_desc, kv: cdb_kv, rows: cdb_rows, tree: cdb_tree, stage: int, layer: int, q, out,
@@ -141,7 +142,7 @@ def cdb_tree_attention(desc: cdb_model_desc, kv: cdb_kv, rows: cdb_rows, tree: c
     qp = _flat("cdb_tree_attention", q, torch.float32, n * desc.d)
     op = _flat("cdb_tree_attention", out, torch.bfloat16, padded * desc.d)
     _check("cdb_tree_attention", lib().cdb_tree_attention(C.byref(desc), C.byref(kv), C.byref(rows), C.byref(tree), stage,
-                                                          layer, qp, op, ws.data_ptr(), ws.numel(), _stream(stream)))
+                                                          layer, qp, op, ws.data_ptr(), ws.numel(), _stream("cdb_tree_attention", stream, ws)))
 
 
 def cdb_tree_prelude(model: cdb_model, kv: cdb_kv, state: cdb_state, rows: cdb_rows, tree: cdb_tree, tokens, ws,
@@ -149,7 +150,7 @@ def cdb_tree_prelude(model: cdb_model, kv: cdb_kv, state: cdb_state, rows: cdb_r
     _rows_fit("cdb_tree_prelude", rows, tree)
     _check("cdb_tree_prelude", lib().cdb_tree_prelude(C.byref(model), C.byref(kv), C.byref(state), C.byref(rows),
                                                       C.byref(tree), _ptr(tokens), _ptr(ws), ws.numel(),
-                                                      _stream(stream)))
+                                                      _stream("cdb_tree_prelude", stream, ws)))
 
 
 def cdb_tree_step(model: cdb_model, kv: cdb_kv, state: cdb_state, rows: cdb_rows, tree: cdb_tree, out: cdb_step_out, ws,
@@ -158,7 +159,7 @@ def cdb_tree_step(model: cdb_model, kv: cdb_kv, state: cdb_state, rows: cdb_rows
     _rows_fit("cdb_tree_step", rows, tree)
     _check("cdb_tree_step", lib().cdb_tree_step(C.byref(model), C.byref(kv), C.byref(state), C.byref(rows),
                                                 C.byref(tree), _ref(gate), C.byref(out), _ptr(ws), ws.numel(),
-                                                _stream(stream)))
+                                                _stream("cdb_tree_step", stream, ws)))
 
 
 def cdb_tree_coda(model: cdb_model, kv: cdb_kv, state: cdb_state, rows: cdb_rows, tree: cdb_tree, logits, next_ids, ws,
@@ -166,7 +167,7 @@ def cdb_tree_coda(model: cdb_model, kv: cdb_kv, state: cdb_state, rows: cdb_rows
     _rows_fit("cdb_tree_coda", rows, tree)
     _check("cdb_tree_coda", lib().cdb_tree_coda(C.byref(model), C.byref(kv), C.byref(state), C.byref(rows),
                                                 C.byref(tree), _ptr(logits), _ptr(next_ids), _ptr(ws), ws.numel(),
-                                                _stream(stream)))
+                                                _stream("cdb_tree_coda", stream, ws)))
 
 
 def cdb_tree_accept(drafts: cdb_drafts, row0, next_ids, first_ids, out: cdb_accepted, ws, stream=None):
@@ -176,13 +177,13 @@ def cdb_tree_accept(drafts: cdb_drafts, row0, next_ids, first_ids, out: cdb_acce
     at, first = (_flat("cdb_tree_accept", t, torch.int32, T) for t in (row0, first_ids))
     ids = _flat("cdb_tree_accept", next_ids, torch.int32, 0)
     _check("cdb_tree_accept", lib().cdb_tree_accept(C.byref(drafts), at, ids, next_ids.numel(), first, C.byref(out),
-                                                    ws.data_ptr(), ws.numel(), _stream(stream)))
+                                                    ws.data_ptr(), ws.numel(), _stream("cdb_tree_accept", stream, ws)))
 
 
 def cdb_tree_commit(desc: cdb_model_desc, kv: cdb_kv, drafts: cdb_drafts, accepted: cdb_accepted, ws, stream=None):
     _trees_fit("cdb_tree_commit", drafts, accepted)
     _check("cdb_tree_commit", lib().cdb_tree_commit(C.byref(desc), C.byref(kv), C.byref(drafts), C.byref(accepted),
-                                                    _ptr(ws), ws.numel(), _stream(stream)))
+                                                    _ptr(ws), ws.numel(), _stream("cdb_tree_commit", stream, ws)))
 
 
 # ---------------------------------------------------------------- device-memory holders (torch)

@@ -44,14 +44,15 @@ def test_workspace_serves_every_smaller_call(shape):
 
 
 def test_map_pages_refusals():
-    pool = tree.cdb_page_pool(1, 1, 8)
+    one, two, three = (tree.cdb_page_pool(k, k, 8) for k in (1, 2, 3))
 
-    def call(desc=DESC, table=1, S=2, P=4, pre=pool, core=pool, coda=pool, layout=0, length=1, mapped=1, ws=1, nb=BIG):
+    def call(desc=DESC, table=1, S=2, P=4, pre=one, core=two, coda=three, layout=0, length=1, mapped=1, ws=1, nb=BIG):
         return _status("cdb_map_pages", desc, table, S, P, pre, core, coda, layout, length, mapped, ws, nb, None)
 
     for kw in ({"table": None}, {"length": None}, {"mapped": None}, {"ws": None}, {"layout": 3}, {"layout": -1}, {"S": -1},
                {"P": -1}, {"core": None}, {"pre": tree.cdb_page_pool(None, 1, 8)}, {"coda": tree.cdb_page_pool(1, None, 8)},
-               {"core": tree.cdb_page_pool(1, 1, -1)}, {"desc": None}):
+               {"core": tree.cdb_page_pool(2, 2, -1)}, {"core": one}, {"coda": tree.cdb_page_pool(2, 3, 8)},
+               {"coda": tree.cdb_page_pool(3, 1, 8)}, {"desc": None}):
         assert call(**kw) == INVALID, kw
     assert call(desc=BAD_DESC) == UNSUPPORTED
     assert call(nb=255) == CAPACITY
@@ -171,3 +172,26 @@ def test_holders_refuse_tensors_on_the_host():
         with pytest.raises(cdb.CdbError) as e:
             make()
         assert e.value.status == INVALID
+
+
+def test_calls_stay_on_the_current_device(monkeypatch):
+    """A workspace or a stream of another device is refused before anything is enqueued."""
+    class On:
+        def __init__(self, index, cuda_stream=7):
+            self.device, self.cuda_stream = torch.device("cuda", index), cuda_stream
+
+        def data_ptr(self):
+            return 1
+
+        def numel(self):
+            return BIG
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    assert tree._stream("f", On(0), On(0)) == 7
+    d, out, acc = _drafts(n_trees=0), tree.cdb_row_map(8, *[1] * 8), tree.cdb_accepted(1, 1, 1)
+    for ws, stream in ((On(1), None), (On(0), On(1)), (On(1), On(1))):
+        for call in (lambda: tree.cdb_tree_rows(d, out, ws, stream),
+                     lambda: tree.cdb_tree_commit(DESC, cdb.cdb_kv(1, 1, 1, 1, 1, 1, 1, 1, 1), d, acc, ws, stream)):
+            with pytest.raises(cdb.CdbError) as e:
+                call()
+            assert e.value.status == INVALID
