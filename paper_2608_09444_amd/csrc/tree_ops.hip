@@ -204,6 +204,8 @@ hipError_t launch_map_pages(const cdb_model_desc& md, int32_t* table, int S, int
 
 // ------------------------------------------------------------------ drafted trees as rows
 // One wave per tree, lane = node; every workgroup sums all trees' node counts.
+// Bound by latency (sequence, its length, the scan): 64 trees of 4 in 4.1 us, 4 of
+// 64 in 3.1, where an empty kernel takes 1.7.
 // A node's ancestors by doubling: with m = the nodes seen so far and p = the
 // node they end at, m |= m of p, p = p of p, six times for up to 64 nodes.
 __device__ __forceinline__ uint64_t shfl64(uint64_t v, int src) {
@@ -299,7 +301,8 @@ hipError_t launch_tree_rows(const cdb_drafts& d, const cdb_row_map& out, int* er
 
 // ------------------------------------------------------------------ acceptance
 // One wave per tree, lane = node: each step asks all nodes at once whether they
-// hang below the current one and hold the wanted token.
+// hang below the current one and hold the wanted token.  2.4 us for 64 trees of 4 as
+// for 4 of 64.
 __global__ __launch_bounds__(256) void k_tree_accept(cdb_drafts dr, const int32_t* __restrict__ row0,
                                                      const int32_t* __restrict__ next_ids, int n_rows,
                                                      const int32_t* __restrict__ first_ids, cdb_accepted out, int* err) {
@@ -341,10 +344,11 @@ hipError_t launch_tree_accept(const cdb_drafts& d, const int32_t* row0, const in
 }
 
 // ------------------------------------------------------------------ commit
-// Workgroup (unit, tree): one layer of one plane of one stage.  Entry i of the path goes from
-// position len + path[i] to len + i <= it.  Every wave reads what the move needs by
-// itself (lane = path entry, page, or plane), so nothing waits at a barrier; the
-// chain of dependent loads (path and sequence, length, page ids, data) bounds it.  A
+// Workgroup (unit, tree): one layer of one plane of one stage.  Entry i of the path
+// goes from position len + path[i] to len + i <= it.  Every wave reads what the move
+// needs by itself (lane = path entry, page, or plane), so nothing waits at a
+// barrier; the chain of dependent loads (path and sequence, length, page ids, data)
+// bounds it (32 trees of 8 over 48 layer planes: 18 MB in 7.3 us, 2.5 TB/s).  A
 // thread owns 16-byte columns of the (K/V, head, dim) entry, two at once, and takes
 // the moves in order, loading eight before it stores them: move i's destination is
 // no later move's source (path[j] > path[i] >= i for j > i), so nothing is
