@@ -489,6 +489,16 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
     Pair pair = pair_of(x.head, ids, 0);
     if (pair.there) fetch(pair);
     put_work(0, work + gridDim.x);
+    // Waves w and w + 4 share a SIMD, and the older one wins ties.  Where a workgroup has
+    // one work in which both have as many pairs (more than one), the younger goes first:
+    // 13 rows over 700 positions 12.0 us against 12.5, one tree of 64 17.6 against 18.3, 16
+    // of 16 over 640 20.2 against 20.7; over 620, 11.4 against 11.2.  With fewer pairs than
+    // the older one (13 over 500) it took 12.3 against 11.2, with several works (64 of 4
+    // over 100) 23.2 against 22.0.
+    Work low = x;
+    low.by_wave(wave % (kTreeWaves / 2));
+    if (wave >= kTreeWaves / 2 && x.mine > 1 && x.mine == low.mine && work + (int)gridDim.x >= n_all)
+        __builtin_amdgcn_s_setprio(1);
     stage_q();
     __syncthreads();
     for (int slot = 0;; slot = slot == 2 ? 0 : slot + 1) {
