@@ -370,7 +370,7 @@ size_t cdb_workspace_bytes(const cdb_model_desc* desc, int32_t max_rows) {
 cdb_status cdb_workspace_init(void* ws, size_t ws_bytes, hipStream_t st) {
     if (!ws) return CDB_ERR_INVALID_ARG;
     if (ws_bytes < 256) return CDB_ERR_CAPACITY;
-    HIPCHK(launch_ws_init(static_cast<int*>(ws), st));
+    HIPCHK(launch_ws_init(static_cast<int*>(ws), kWsHeader, st));
     return CDB_OK;
 }
 
@@ -776,8 +776,8 @@ cdb_status cdb_read_device_error(void* ws, hipStream_t st, int32_t* code) {
     if (hipStreamSynchronize(st) != hipSuccess) return CDB_ERR_HIP;
     *code = v;
     if (v != 0) {
-        int* err = static_cast<int*>(ws);
-        if (launch_ws_init(err, st) != hipSuccess) return CDB_ERR_HIP;
+        // the code alone: it may be a caller's own int32
+        if (launch_ws_init(static_cast<int*>(ws), 1, st) != hipSuccess) return CDB_ERR_HIP;
         if (hipStreamSynchronize(st) != hipSuccess) return CDB_ERR_HIP;
     }
     return CDB_OK;

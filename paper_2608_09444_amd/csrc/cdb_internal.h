@@ -69,7 +69,7 @@ __device__ __forceinline__ int live_rows(const int32_t* dn, int M) {
 
 // Workspace header (ints): the sticky error code, then workgroups of a page
 // mapping that are through (0 between calls).
-constexpr int kWsArrive = 1;
+constexpr int kWsArrive = 1, kWsHeader = 2;
 
 // First sticky error wins.
 __device__ __forceinline__ void set_err(int* err, int code) { atomicCAS(err, 0, code); }
@@ -227,7 +227,8 @@ hipError_t launch_scatter_ids(int M, const int32_t* ids, const int32_t* seq, con
 hipError_t launch_pack(int kind, const uint16_t* a, const uint16_t* b, const uint16_t* c, int N, int K, int hd,
                        uint16_t* dst, hipStream_t st);
 hipError_t launch_copy_bf16(const uint16_t* src, size_t n, uint16_t* dst, hipStream_t st);
-hipError_t launch_ws_init(int* err, hipStream_t st);
+// clears the first n <= 64 ints
+hipError_t launch_ws_init(int* ws, int n, hipStream_t st);
 
 // ---------------------------------------------------------------- drafted trees
 // bytes of the tree attention's scratch behind a stage call's workspace (or its

@@ -571,8 +571,8 @@ __global__ void k_copy16(const uint16_t* __restrict__ s, size_t n, uint16_t* __r
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) d[i] = s[i];
 }
 
-__global__ void k_ws_init(int* err) {
-    if (threadIdx.x == 0) err[0] = err[kWsArrive] = 0;
+__global__ void k_ws_init(int* ws, int n) {
+    if ((int)threadIdx.x < n) ws[threadIdx.x] = 0;
 }
 
 // ------------------------------------------------------------------ launchers
@@ -780,8 +780,8 @@ hipError_t launch_copy_bf16(const uint16_t* src, size_t n, uint16_t* dst, hipStr
     return hipGetLastError();
 }
 
-hipError_t launch_ws_init(int* err, hipStream_t st) {
-    k_ws_init<<<1, 64, 0, st>>>(err);
+hipError_t launch_ws_init(int* ws, int n, hipStream_t st) {
+    k_ws_init<<<1, 64, 0, st>>>(ws, n);
     return hipGetLastError();
 }
 

@@ -197,6 +197,16 @@ def test_bad_counts_change_nothing(what):
     assert all(torch.equal(a, b) for a, b in zip(after, before))
 
 
+def test_reading_an_error_clears_that_word_alone():
+    """An error code may stand in a caller's own int32; a workspace's header is cleared whole."""
+    words = _dev([tree.CDB_DEV_NO_PAGES, 77, 78])
+    assert cdb.cdb_read_device_error(words) == tree.CDB_DEV_NO_PAGES
+    assert words.tolist() == [0, 77, 78] and cdb.cdb_read_device_error(words) == 0
+    ws = torch.full((1024,), 255, dtype=torch.uint8, device="cuda")
+    cdb.cdb_workspace_init(ws)
+    assert ws[:8].eq(0).all() and ws[256:].eq(255).all()
+
+
 @pytest.mark.parametrize("layout", [cdb_driver.KV_FULL, cdb_driver.KV_SHARED, cdb_driver.KV_FIRST_THEN_SHARED])
 def test_pages_are_the_host_drivers(layout):
     """The table of the host driver after it admitted the same sequences to the same empty pools."""

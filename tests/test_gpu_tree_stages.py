@@ -255,6 +255,9 @@ def test_calls_at_capacity_are_those_of_their_rows(shape):
         _say(f"[gpu] trees of {sizes} in 64 rows of capacity")
         state = cdb.State(shape, 64)
         v.state = state
+        for a, junk in zip((v.laid.seq, v.laid.pos, v.laid.base, v.laid.rope_pos, v.laid.tokens, v.laid.mask),
+                           (1 << 30, -5, 0x7fffffff, 0x7fffffff, -1, -1)):
+            a[v.n:] = junk  # rows past the count do not matter
         saved = _snapshot(v)
         both = []
         for exact in (True, False):
