@@ -355,8 +355,8 @@ hipError_t launch_tree_accept(const cdb_drafts& d, const int32_t* row0, const in
 // overwritten before it is read.
 constexpr int kCommitBatch = 8;
 // Up to so many (unit, tree) pairs, workgroups share a unit's columns: one tree of
-// 24 nodes over 96 units 5.0 us against 5.8; 64 of 4 over 3072 units 11.1 us that
-// way against 7.9.
+// 24 nodes over 96 layer planes 5.0 us against 5.8; 64 of 4 over 48 layer planes
+// 11.1 us that way against 7.9.
 constexpr int kCommitSplit = 1024;
 
 struct CommitStages {
