@@ -1,8 +1,8 @@
 // Row, page and cache bookkeeping of drafted token trees: page tables from
 // sequence lengths, drafted trees as the rows of a stage call, greedy acceptance,
-// and the move of the accepted K/V.  All but the move are bound by latency
-// (a few KB to a few hundred KB per call), so each is one launch whose workgroups
-// recompute the small prefix sums they need instead of waiting for one another.
+// and the move of the accepted K/V.  All are bound by latency, so each is one launch
+// whose workgroups recompute the small prefix sums they need instead of waiting for
+// one another.
 #include <algorithm>
 
 #include "cdb_internal.h"

@@ -640,6 +640,59 @@ def test_attention_captured_and_on_another_stream():
     assert torch.equal(_attend(shape, kv, b, q, 32, ws=ws, stream=side)[:b.n], want)
 
 
+def _graph(call):
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    return graph
+
+
+def test_graphs_that_share_a_workspace():
+    """Page mapping up and down and attention of contexts with and without records, each in a graph of its own, replayed in
+    turn with eager calls between."""
+    shape = _shape(128, 4)
+    rng = np.random.default_rng(13)
+    kv, pt = _cache(shape, [(0, 2600), (1, 300), (2, 64)], 41)
+    ws, desc = _ws(shape, 64, 40), cdb.make_desc(shape)
+    calls, outs, wants = [], [], []
+    for trees, loops in (([(2500, random_parents(rng, 9))], [0]), ([(7, [-1]), (250, random_parents(rng, 13))], [0, 1])):
+        b = _batch(rng, trees, loops)
+        rows = cdb.Rows(np.arange(b.n), b.seq, b.pos, b.c)
+        see = tree.Tree(16, _dev(b.base), _dev(b.mask.view(np.int64), np.int64), _dev(b.pos))
+        q, out = _q(shape, b.n, 51 + b.n), torch.zeros((32, shape.d), dtype=torch.bfloat16, device="cuda")
+        calls.append(lambda rows=rows, see=see, q=q, out=out: tree.cdb_tree_attention(desc, kv.c, rows.c, see.c, 1, 1, q,
+                                                                                       out, ws.buf))
+        outs.append(out)
+    table = torch.full((40, shape.r_max + 2, 30), -1, dtype=torch.int32, device="cuda")
+    mapped, pool = _dev(np.zeros(40)), tree.PagePool.full(40 * 30 * shape.r_max)
+    low = rng.integers(0, 130, 40)
+    for need in (_dev(low + rng.integers(0, 350, 40)), _dev(low)):
+        calls.append(lambda need=need: tree.cdb_map_pages(desc, table, None, pool.c, None, 0, need, mapped, ws.buf))
+    for k, call in enumerate(calls):
+        call()
+        torch.cuda.synchronize()
+        wants.append(outs[k].clone() if k < 2 else None)
+    # every sequence grows, then is cut back: each state repeats, with its stack
+    states = {}
+    graphs = [_graph(call) for call in calls]
+    _say("[gpu] four graphs of one workspace")
+    for turn in range(4):
+        for k in (2, 0, 3, 1):
+            (graphs[k].replay if turn % 2 else calls[k])()
+            torch.cuda.synchronize()
+            if k < 2:
+                assert torch.equal(outs[k], wants[k]), (turn, k)
+                outs[k].zero_()
+            else:
+                now = (table.clone(), mapped.clone(), pool.free_count.clone(), pool.free_ids[:int(pool.free_count)].clone())
+                for a, b in zip(now, states.setdefault(k, now)):
+                    assert torch.equal(a, b), (turn, k)
+    assert cdb.cdb_read_device_error(ws.buf) == 0
+    del graphs
+
+
 def test_a_long_context_with_pages_past_32_bit_offsets():
     """Pages whose byte offsets in the pool pass 2^32, and 20011 positions."""
     shape = _shape(128, 16)
