@@ -74,7 +74,10 @@ __host__ __device__ __forceinline__ int tree_segments(int npg, int* pages) {
 }
 
 // Works that a tile and head is split into when there are n (tile, head, half)
-// triples: as many as fit the CUs in one round.
+// triples: as many as fit the CUs in one round.  Of the tiles, at least as many
+// count as all rows of a call without a device row count make: whether the host
+// launches k_tree_merge is decided by those, and rows that are skipped must not
+// leave segments in records that nobody joins.
 __host__ __device__ __forceinline__ int tree_runs(int n) {
     const int z = n > 0 ? kTreeCUs / n : 1;
     return z < 1 ? 1 : z > kTreeSegs ? kTreeSegs : z;
@@ -249,7 +252,7 @@ template <int HD, int NT, bool HALVES>
 __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restrict__ q, KvTarget kv,
                                                             const int32_t* __restrict__ seq, cdb_tree tree, int M, int H,
                                                             TreeScratch ts, uint16_t* __restrict__ out, int* err,
-                                                            const int32_t* __restrict__ dn) {
+                                                            const int32_t* __restrict__ dn, int least_tiles) {
     constexpr int NJ = HD / 32, NB = HD / 16, CPR = HD / 8;  // K steps, dim blocks, 16-byte pieces of a row
     constexpr int ROWS = 16 * NT, CAP = HALVES ? 2 * kTreeRows : ROWS;  // rows of a workgroup, of a tile
     constexpr int PITCH = HD + 4, REC = HD + 2;
@@ -324,7 +327,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
             s_ends[k] = ends;
         }
         s_ends[WORDS] = s_ends[WORDS + 1] = ~0ull;
-        runs = tree_runs(n_tiles * H * (HALVES ? 2 : 1));
+        runs = tree_runs(max(n_tiles, least_tiles) * H * (HALVES ? 2 : 1));
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // what lanes have written, others read
         n_works = n_tiles;
         if (runs > 1) {
@@ -828,16 +831,16 @@ static hipError_t run_tree_attn(const float* q, const KvTarget& kv, const int32_
     const int cap = tree_rows_per_tile(tree.max_nodes), halves = cap == 64 ? 2 : 1;
     int pages;
     const int segs = tree_segments(kv.max_pages + 1, &pages);  // the most a row's context may have
+    const int least = dn ? 0 : (M + cap - 1) / cap;  // tiles of all rows, at least
     // no more workgroups than there can be works, and one resident per CU
     const int most = std::min(M * H * halves * segs, kTreeCUs);
     if (cap == 16)
-        k_tree_attn<HD, 1, false><<<most, kTreeThreads, 0, st>>>(q, kv, seq, tree, M, H, ts, out, err, dn);
+        k_tree_attn<HD, 1, false><<<most, kTreeThreads, 0, st>>>(q, kv, seq, tree, M, H, ts, out, err, dn, least);
     else if (cap == 32)
-        k_tree_attn<HD, 2, false><<<most, kTreeThreads, 0, st>>>(q, kv, seq, tree, M, H, ts, out, err, dn);
+        k_tree_attn<HD, 2, false><<<most, kTreeThreads, 0, st>>>(q, kv, seq, tree, M, H, ts, out, err, dn, least);
     else  // whole groups of 16
-        k_tree_attn<HD, 2, true><<<(most + 15) / 16 * 16, kTreeThreads, 0, st>>>(q, kv, seq, tree, M, H, ts, out, err, dn);
-    // with all rows live there are at least so many tiles
-    const bool split = segs > 1 && (dn || tree_runs((M + cap - 1) / cap * H * halves) > 1);
+        k_tree_attn<HD, 2, true><<<(most + 15) / 16 * 16, kTreeThreads, 0, st>>>(q, kv, seq, tree, M, H, ts, out, err, dn, least);
+    const bool split = segs > 1 && (dn || tree_runs(least * H * halves) > 1);
     if (split) k_tree_merge<HD><<<(M * H + 3) / 4, 256, 0, st>>>(kv, seq, tree, M, H, ts, out, dn);
     return hipGetLastError();
 }
