@@ -130,7 +130,8 @@ typedef struct {
 } cdb_row_map;
 
 /* Lays the trees out as rows.  A tree with a bad count, sequence or length, or
- * of a sequence that an earlier tree has, gets no rows, and a parent that is not
+ * of a sequence that an earlier tree has, gets no rows (its row0 is that of the
+ * next tree's first row, as for a tree of no nodes), and a parent that is not
  * an earlier node of the tree makes its node a root; either sets
  * CDB_DEV_BAD_INDEX.  Trees from the first on that does not fit into `capacity`
  * get no rows, row0 = -1 and the same code. */
@@ -180,7 +181,10 @@ typedef struct {
  * with the lowest index.  row0: as cdb_tree_rows wrote it (-1: the tree has no
  * rows, nothing is accepted).  A node whose parent is not an earlier node is never
  * reached, and one whose row is outside [0, n_rows) neither (CDB_DEV_BAD_INDEX).
- * Only n_nodes, parent and tokens of `drafts` are read. */
+ * n_nodes, parent and tokens of `drafts` are read, and seq and len unless they are
+ * NULL: of a tree that cdb_tree_rows gives no rows because of its sequence, length
+ * or count nothing is accepted (CDB_DEV_BAD_INDEX, a bad count aside).  Without
+ * them the caller sees to it that every tree with nodes and a row0 >= 0 has rows. */
 cdb_status cdb_tree_accept(const cdb_drafts* drafts, const int32_t* row0, const int32_t* next_ids, int32_t n_rows,
                            const int32_t* first_ids, const cdb_accepted* out, void* ws, size_t ws_bytes,
                            hipStream_t stream);

@@ -171,7 +171,8 @@ def cdb_tree_coda(model: cdb_model, kv: cdb_kv, state: cdb_state, rows: cdb_rows
 
 
 def cdb_tree_accept(drafts: cdb_drafts, row0, next_ids, first_ids, out: cdb_accepted, ws, stream=None):
-    """row0, first_ids: device int32 [n_trees]; next_ids: device int32, by row."""
+    """row0, first_ids: device int32 [n_trees]; next_ids: device int32, by row.  drafts: seq and length as cdb_tree_rows got
+    them, so that trees it refused are known."""
     _trees_fit("cdb_tree_accept", drafts, out)
     T = drafts.n_trees
     at, first = (_flat("cdb_tree_accept", t, torch.int32, T) for t in (row0, first_ids))

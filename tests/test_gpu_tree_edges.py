@@ -42,3 +42,56 @@ def test_skipped_rows_take_nothing_from_the_others(hd, H, trees, n, good, max_no
     some = keep[:: max(1, len(keep) // 6)]
     want, tol = _want(shape, kv, pt, b.take(some), q[torch.from_numpy(some).cuda()])
     _close(got[torch.from_numpy(some).cuda()], want, tol)
+
+
+# ------------------------------------------------------------------ trees that get no rows
+
+@pytest.mark.parametrize("bad", [0, 1, 3])
+@pytest.mark.parametrize("what", ["sequence", "negative", "twice", "length", "far", "count"])
+def test_trees_without_rows_accept_nothing(what, bad):
+    """A tree that cdb_tree_rows refuses, before, between and after good ones: every root is what the model says, so it
+    would be accepted.  At capacity, as a captured round has it, with ids of earlier rounds behind the last row."""
+    rng = np.random.default_rng(bad)
+    d = _drafts(rng, [4, 3, 5, 6], 6, max_seqs=9)
+    d["parent"][:] = np.arange(6) - 1
+    d["tokens"][:] = 11
+    if what == "twice":
+        other = 2 if bad < 2 else 0
+        d["seq"][bad] = d["seq"][other]
+        refused = max(bad, other)
+    else:
+        refused = bad
+        if what == "count":
+            d["n_nodes"][bad] = 7
+        elif what in ("length", "far"):
+            d["length"][d["seq"][bad]] = -1 if what == "length" else 2 ** 31 - 2
+        else:
+            d["seq"][bad] = 9 if what == "sequence" else -1
+    T, ws, up = 4, _ws(cdbgen.TINY, 1, 1), _upload(d)
+    rows, acc = tree.TreeRows(T, 32), tree.Accepted(T, 6)
+    ids, first = _dev(np.full(32, 11)), _dev(np.full(T, 11))
+    _say(f"[gpu] rows and acceptance: tree {refused} is refused ({what})")
+    tree.cdb_tree_rows(up.c, rows.c, ws.buf)
+    torch.cuda.synchronize()
+    assert cdb.cdb_read_device_error(ws.buf) == cdb.CDB_DEV_BAD_INDEX
+    tree.cdb_tree_accept(up.c, rows.row0, ids, first, acc.c, ws.buf)
+    torch.cuda.synchronize()
+    assert cdb.cdb_read_device_error(ws.buf) in (0, cdb.CDB_DEV_BAD_INDEX)
+    count = [0 if t == refused else n for t, n in enumerate((4, 3, 5, 6))]
+    assert acc.count.tolist() == count and acc.next.tolist() == [11] * T
+    assert acc.path.tolist() == [list(range(n)) + [-1] * (6 - n) for n in count]
+    d["n_nodes"][refused] = 0
+    row0, want = _host_rows(d)
+    assert int(rows.n_rows) == len(want)
+
+
+def test_acceptance_without_sequences():
+    """Trees whose seq and len are NULL: their nodes, tokens and row0 alone count."""
+    d = _drafts(np.random.default_rng(0), [4, 0, 5], 6)
+    d["parent"][:] = np.arange(6) - 1
+    d["tokens"][:] = 11
+    up, ws, acc = _upload(d), _ws(cdbgen.TINY, 1, 1), tree.Accepted(3, 6)
+    bare = tree.cdb_drafts(3, 6, 0, None, None, up.n_nodes.data_ptr(), up.parent.data_ptr(), up.tokens.data_ptr())
+    tree.cdb_tree_accept(bare, _dev([0, 4, 4]), _dev(np.full(9, 11)), _dev(np.full(3, 11)), acc.c, ws.buf)
+    torch.cuda.synchronize()
+    assert cdb.cdb_read_device_error(ws.buf) == 0 and acc.count.tolist() == [4, 0, 5]
