@@ -87,10 +87,12 @@ typedef struct {
  * plane) order first; then new ones come off it in (sequence, page, plane)
  * order.  Cutting a sequence back right after growing it so restores the stack.
  * A stack's entries from its count on keep what stood there last.  All or
- * nothing: if
- * a pool has too few pages (or its stack too few entries), a length needs more
- * than max_pages pages, or mapped or a count is out of range, nothing changes
- * and the workspace's error code is set (CDB_DEV_NO_PAGES, CDB_DEV_BAD_INDEX). */
+ * nothing: if a pool has too few pages (or its stack too few entries), a length
+ * needs more than max_pages pages, or mapped or a count is out of range, nothing
+ * changes and the workspace's error code is set (CDB_DEV_NO_PAGES,
+ * CDB_DEV_BAD_INDEX).  If a page id among those given back or taken is negative,
+ * nothing that is mapped or free changes (CDB_DEV_UNMAPPED_PAGE); pages that were
+ * to be mapped read -1 then, and stack entries from the count on are lost. */
 cdb_status cdb_map_pages(const cdb_model_desc* desc, int32_t* page_table, int32_t max_seqs, int32_t max_pages,
                          const cdb_page_pool* pre, const cdb_page_pool* core, const cdb_page_pool* coda,
                          int32_t kv_layout, const int32_t* len, int32_t* mapped, void* ws, size_t ws_bytes,

@@ -1,8 +1,8 @@
 // Row, page and cache bookkeeping of drafted token trees: page tables from
 // sequence lengths, drafted trees as the rows of a stage call, greedy acceptance,
 // and the move of the accepted K/V.  All are bound by latency, so each is one launch
-// whose workgroups recompute the small prefix sums they need instead of waiting for
-// one another.
+// (large page mappings two) whose workgroups recompute the small prefix sums they
+// need instead of waiting for one another.
 #include <algorithm>
 
 #include "cdb_internal.h"
@@ -40,11 +40,17 @@ __device__ __forceinline__ void block_scan256(int (&v)[N], int* red, int (&total
 }
 
 // ------------------------------------------------------------------ page tables
-// Entries of the table to a workgroup, of up to 512: 128 sequences of 32 planes
-// leaving and coming take 20.1 us (two calls; 24.5 at 2048 entries, 21.8 at 256
-// workgroups), 64 that grow by 16 tokens and back 8.1 (8.5 at 2048; 7.3 in one
-// workgroup, which takes 149 us for the former).
+// Entries of the table to a workgroup, of up to 512.  Chosen when calls could not be
+// taken back yet: 128 sequences of 32 planes leaving and coming took 20.1 us (two
+// calls; 24.5 at 2048 entries, 21.8 at 256 workgroups), 64 that grow by 16 tokens and
+// back 8.1 (8.5 at 2048; 7.3 in one workgroup, which takes 149 us for the former).
 constexpr int kMapEntries = 512, kMapGroups = 512;
+// Up to so many workgroups the last one takes a call back, above a second launch
+// (k_map_pages says why): the former 28.1 us against 24.0 of that launch, the latter
+// 9.4 against 11.5.  24 workgroups that leave and come, 4 planes: 13.3 against 14.1; 384
+// that grow and are cut back, 32 planes: 20.1 against 21.3.
+constexpr int kMapThrough = 64;
+constexpr int kMapHole = 1 << 30;  // left in the workspace's header for the launch that takes back
 
 struct MapArgs {
     int32_t* table;
@@ -57,6 +63,8 @@ struct MapArgs {
     const int32_t* len;
     int32_t* mapped;
     int* ws;                   // [0] error code, [kWsArrive] workgroups that are through
+    bool through;              // stores go past this XCD's L2
+    bool undo;                 // the second launch: take back what the first one did, if it met a hole
 };
 
 struct MapPages {
@@ -91,16 +99,39 @@ __device__ __forceinline__ size_t map_cell(const MapArgs& a, int k, const int* b
     return ((size_t)min(s, a.S - 1) * a.planes + a.first[k] + (e - page * w)) * a.P + p;
 }
 
-// One launch: every workgroup sums the page counts of all sequences itself (a
+__device__ __forceinline__ void map_store(const MapArgs& a, int32_t* p, int value) {
+    if (a.through)
+        __hip_atomic_store(p, value, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    else
+        *p = value;
+}
+// Entry j's cell, and with the last page that a token page has the planes that share it.
+__device__ __forceinline__ void map_put(const MapArgs& a, int k, size_t cell, int j, int value) {
+    const int w = a.width[k];
+    map_store(a, a.table + cell, value);
+    if (j % w == w - 1)
+        for (int q = w; q < a.n_planes[k]; ++q) map_store(a, a.table + cell + (size_t)(q - w + 1) * a.P, value);
+}
+
+// Every workgroup sums the page counts of all sequences itself (a
 // thread `per` of them) and takes its share of the entries.  Entry j that is given
 // back lands on the stack at count + all - 1 - j, and the j-th one that is taken
 // comes from there, so its thread has it already; the others come off the stack
 // below `count`, where this call writes nothing.  The workgroup that is through
 // last writes mapped and the counts, which all have read by then.
+//
+// A page id below 0, in a cell to be given back or on the stack, shows only while
+// entries move, and then the whole call is taken back: the ids that were given back
+// all stand on the stack above `count`, so the last workgroup puts them into their
+// cells again and unmaps the taken ones.  It must not be overtaken by the others'
+// stores, so these go to memory (agent scope) and are through before a workgroup
+// counts itself in; of large tables, whose scattered words cost more that way than
+// another launch, a second launch of one workgroup takes back.
 __global__ __launch_bounds__(256) void k_map_pages(MapArgs a) {
-    __shared__ int s_back[256], s_more[256], red[8], s_bad, s_last;
+    __shared__ int s_back[256], s_more[256], red[8], s_bad, s_last, s_hole;
     const int tid = threadIdx.x, per = (a.S + 255) / 256;
-    if (tid == 0) s_bad = 0;
+    if (a.undo && a.ws[kWsArrive] != kMapHole) return;
+    if (tid == 0) s_bad = s_hole = 0;
     int count[3];
 #pragma unroll
     for (int k = 0; k < 3; ++k) count[k] = a.width[k] ? *a.free_count[k] : 0;
@@ -127,7 +158,7 @@ __global__ __launch_bounds__(256) void k_map_pages(MapArgs a) {
         else if (!code && (up > a.capacity[k] || up < all[1] * a.width[k]))
             code = CDB_DEV_NO_PAGES;
     }
-    if (!code)
+    if (!code && !a.undo)
 #pragma unroll
         for (int k = 0; k < 3; ++k) {
             const int w = a.width[k];
@@ -135,34 +166,43 @@ __global__ __launch_bounds__(256) void k_map_pages(MapArgs a) {
             const int back = all[0] * w, more = all[1] * w, top = count[k] + back - 1;
             for (int j = blockIdx.x * 256 + tid; j < max(back, more); j += gridDim.x * 256) {
                 int id;
-                auto put = [&](size_t cell, int value) {
-                    a.table[cell] = value;
-                    if (j % w == w - 1)  // the planes that share the last page
-                        for (int q = w; q < a.n_planes[k]; ++q) a.table[cell + (size_t)(q - w + 1) * a.P] = value;
-                };
                 if (j < back) {
                     const size_t cell = map_cell(a, k, s_back, per, j, true);
                     id = a.table[cell];
-                    put(cell, -1);
-                    a.free_ids[k][top - j] = id;
+                    map_put(a, k, cell, j, -1);
+                    map_store(a, a.free_ids[k] + top - j, id);
                 } else {
                     id = a.free_ids[k][top - j];
                 }
-                if (id < 0) set_err(a.ws, CDB_DEV_UNMAPPED_PAGE);
-                if (j < more) put(map_cell(a, k, s_more, per, j, false), id);
+                if (id < 0) s_hole = 1;
+                if (j < more) map_put(a, k, map_cell(a, k, s_more, per, j, false), j, id);
             }
         }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's stores have reached memory
     __syncthreads();
-    if (tid == 0) {
-        const int n = gridDim.x == 1 ? 0 : atomicAdd(a.ws + kWsArrive, 1);
-        s_last = n == (int)gridDim.x - 1;
+    if (tid == 0) {  // workgroups that are through, those with a hole from bit 16 on
+        const int own = 1 + (s_hole << 16), n = gridDim.x == 1 ? 0 : atomicAdd(a.ws + kWsArrive, own);
+        s_last = (n & 0xffff) == (int)gridDim.x - 1;
+        s_hole = (n + own) >> 16 | a.undo;
         if (s_last) {
-            if (n) atomicExch(a.ws + kWsArrive, 0);
-            if (code) set_err(a.ws, code);
+            if (n || a.undo) atomicExch(a.ws + kWsArrive, s_hole && !a.through ? kMapHole : 0);
+            if (code || s_hole) set_err(a.ws, code ? code : CDB_DEV_UNMAPPED_PAGE);
         }
     }
     __syncthreads();
     if (!s_last || code) return;
+    if (s_hole && !a.through) return;
+    if (s_hole) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const int w = a.width[k], back = all[0] * w, more = all[1] * w, top = count[k] + back - 1;
+            for (int j = tid; j < back; j += 256)
+                map_put(a, k, map_cell(a, k, s_back, per, j, true), j,
+                        __hip_atomic_load(a.free_ids[k] + top - j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+            for (int j = tid; j < more; j += 256) map_put(a, k, map_cell(a, k, s_more, per, j, false), j, -1);
+        }
+        return;
+    }
     for (int s = tid; s < a.S; s += 256) {
         const MapPages m = map_pages_of(a, s, bad);
         if (m.now != m.old) a.mapped[s] = m.now;
@@ -198,7 +238,12 @@ hipError_t launch_map_pages(const cdb_model_desc& md, int32_t* table, int S, int
     a.ws = ws;
     // every sequence may come or go, but most calls change few of the pages
     const int groups = (int)std::min<int64_t>(kMapGroups, std::max<int64_t>(1, entries / kMapEntries));
+    a.through = groups <= kMapThrough;
     k_map_pages<<<groups, 256, 0, st>>>(a);
+    if (!a.through) {
+        a.through = a.undo = true;
+        k_map_pages<<<1, 256, 0, st>>>(a);
+    }
     return hipGetLastError();
 }
 

@@ -95,3 +95,68 @@ def test_acceptance_without_sequences():
     tree.cdb_tree_accept(bare, _dev([0, 4, 4]), _dev(np.full(9, 11)), _dev(np.full(3, 11)), acc.c, ws.buf)
     torch.cuda.synchronize()
     assert cdb.cdb_read_device_error(ws.buf) == 0 and acc.count.tolist() == [4, 0, 5]
+
+
+# ------------------------------------------------------------------ page tables and stacks with holes
+
+@pytest.mark.parametrize("layout", [tree.KV_FULL, tree.KV_SHARED, tree.KV_FIRST_THEN_SHARED])
+@pytest.mark.parametrize("S,P", [(5, 7), (60, 5), (200, 30), (300, 40)])
+@pytest.mark.parametrize("where", ["table", "stack", "stack at once"])
+def test_holes_in_tables_and_stacks_change_nothing(where, S, P, layout):
+    """An unmapped page that a call would give back, or a hole among the pages that it would hand out: the call changes
+    nothing that is mapped or free, and runs once the hole is mended.  In one workgroup and in many."""
+    shape = cdbgen.TINY
+    rng = np.random.default_rng(S + layout)
+    caps = (S * P, S * P * shape.r_max, S * P)
+    start = [rng.permutation(c).astype(np.int32) for c in caps]
+    host = HostPages(shape, S, P, caps, layout, start)
+    desc, ws = cdb.make_desc(shape), _ws(shape, 1, S)
+    table, mapped = _dev(host.table), _dev(host.mapped)
+    pools = [tree.PagePool(_dev(s), _dev([len(s)])) for s in start]
+
+    def run(length):
+        tree.cdb_map_pages(desc, table, *(p.c for p in pools), layout, _dev(length), mapped, ws.buf)
+        torch.cuda.synchronize()
+        return cdb.cdb_read_device_error(ws.buf)
+
+    def same():
+        n = torch.from_numpy(host.mapped).cuda()
+        live = (torch.arange(P, device="cuda") < n[:, None])[:, None, :].expand(table.shape)
+        assert torch.equal(table[live], torch.from_numpy(host.table).cuda()[live])
+        assert (table[~live] == -1).all() and mapped.tolist() == host.mapped.tolist()
+        for p, s in zip(pools, host.stacks):
+            assert int(p.free_count) == len(s) and p.free_ids[:len(s)].tolist() == s
+
+    half = rng.integers(0, 8 * P + 1, S)
+    half[:2] = 16, 16 * P
+    assert run(half) == host.run(half) == 0
+    up = rng.random(S) < 0.5  # these grow, the others shrink
+    up[:2] = True, False
+    need = np.where(up, 16 * P, rng.integers(0, 9, S))
+    _say(f"[gpu] map pages: {S} sequences, layout {layout}, a hole in the {where}")
+    for k, planes in ((1, host.groups(1)[-1]), (0, [0])):
+        stack = host.stacks[k]
+        back = sum(max(0, int(m) - -(-int(n) // 16)) for m, n in zip(host.mapped, need)) * len(host.groups(k))
+        more = sum(max(0, -(-int(n) // 16) - int(m)) for m, n in zip(host.mapped, need)) * len(host.groups(k))
+        if where == "table" or more <= back:
+            cell = (1, planes, int(host.mapped[1]) - 1)
+            keep = int(host.table[1, planes[0], cell[2]])
+            host.table[cell] = -1
+            table[1, planes[0]:planes[-1] + 1, cell[2]] = -1
+        else:
+            at = len(stack) - (more - back if where == "stack" else 1)
+            keep, stack[at] = stack[at], -1
+            pools[k].free_ids[at] = -1
+        for _ in range(2):
+            assert run(need) == cdb.CDB_DEV_UNMAPPED_PAGE
+            same()
+        if where == "table" or more <= back:
+            host.table[cell] = keep
+            table[1, planes[0]:planes[-1] + 1, cell[2]] = keep
+        else:
+            stack[at] = keep
+            pools[k].free_ids[at] = keep
+    assert run(need) == host.run(need) == 0
+    same()
+    assert run(np.zeros(S)) == host.run(np.zeros(S)) == 0
+    same()
