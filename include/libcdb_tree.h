@@ -144,7 +144,9 @@ cdb_status cdb_tree_rows(const cdb_drafts* drafts, const cdb_row_map* out, void*
  * out and stage / layer arguments): row i attends to the positions that
  * tree->base[i] and tree->mask[i] name, in its own plane.  Reads the cache only;
  * the rows' own K/V must be in it.  What a masked position holds (NaN included)
- * does not reach a row.  A row that sees nothing gets zeros.  The stage's pool
+ * does not reach a row.  What a row sees may be infinite or NaN, and its scores and
+ * sums as large as 32 bits hold: it gets what softmax and sum give then, at a slower
+ * pace.  A row that sees nothing gets zeros.  The stage's pool
  * has at least one page, however few are mapped.  A row whose
  * sequence, loop index or positions are out of range is skipped
  * (CDB_DEV_UNMAPPED_PAGE), an unmapped page is left out (the same code). */

@@ -46,6 +46,10 @@
 // of the product, which would multiply it by the others' zeros, and added to those
 // rows alone.
 //
+// A row whose sums end as no number, or whose weights are all 0, is worked out again in
+// plain fp32 (attend_plain), for the dims that are no number; looking for that takes 0
+// to 0.4 us of a call.
+//
 // Nothing in a row's arithmetic depends on the other rows: not its tile, not the
 // segments, not the wave that takes a page or the workgroup that takes a segment.
 #include <algorithm>
@@ -243,9 +247,94 @@ __device__ __forceinline__ void join_segment(float& tm, float& tl, float sm, flo
     tm = mx;
 }
 __device__ __forceinline__ float join_sum(float t, float s, float a, float b) { return fmaf(t, a, s * b); }
-// den 0: the row sees nothing
-__device__ __forceinline__ uint32_t row_out2(float a, float b, float den) {
-    return den != 0.f ? pack_bf16(a / den, b / den) : 0u;
+
+// One row and head in plain fp32, by one wave: lane = key for the scores, then two
+// dims.  Three turns over the context (maximum, sum, weights already divided by it), as
+// only rows take it whose sums in the products above are not to be had: an infinite K
+// or V times the low part of q or p is not what it is times the whole, and sums of
+// values that are themselves near the largest number overflow.  64 trees of 4 over
+// 2048..4223 positions with every V infinite take 4.1 ms (261-277 us otherwise).
+template <int HD>
+__device__ __forceinline__ float2 attend_plain(const float* q, const KvTarget& kv, int seq, int plane, int base,
+                                               uint64_t mask, int head, int H) {
+    const int lane = threadIdx.x & 63, dim = 2 * min(lane, HD / 2 - 1);
+    const int n = mask ? base + 64 - __clzll((long long)mask) : base;
+    const int32_t* ids = kv.page_table + ((size_t)seq * kv.n_planes + plane) * kv.max_pages;
+    const float qscale = 1.4426950408889634f / sqrtf((float)HD);
+    float m = -INFINITY, l = 0.f, oa = 0.f, ob = 0.f;
+    bool any = false;
+#pragma unroll 1
+    for (int turn = 0; turn < 3; ++turn) {
+#pragma unroll 1
+        for (int k0 = 0; k0 < n; k0 += 64) {
+            const int key = k0 + lane, off = key - base;
+            bool see = key < n && (off < 0 || (mask >> (off & 63) & 1));
+            const int id = see ? ids[key / kPage] : -1;
+            see = id >= 0 && id < kv.n_pages;
+            const uint16_t* k = kv.pool + kv_offset(kv.layer, see ? id : 0, kv.n_pages, 0, head, H, key % kPage, HD);
+            float s = 0.f;
+#pragma unroll 2
+            for (int j = 0; j < HD; j += 8) {
+                const u32x4 w = *reinterpret_cast<const u32x4*>(k + j);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s = fmaf(q[j + 2 * e], bflo(w[e]), s);
+                    s = fmaf(q[j + 2 * e + 1], bfhi(w[e]), s);
+                }
+            }
+            s *= qscale;
+            if (turn == 0) {
+                m = see ? fmaxf(m, s) : m;
+                any |= see;
+                continue;
+            }
+            float p = see ? exp2f(s - m) : 0.f;
+            if (turn == 1) {
+                l += p;
+                continue;
+            }
+            p /= l;
+            const uint64_t seen = __ballot(see);
+#pragma unroll 1
+            for (int u0 = 0; u0 < 64; u0 += 8) {
+                uint32_t v[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int at = __builtin_amdgcn_readlane(see ? id : 0, u0 + u);
+                    v[u] = *reinterpret_cast<const uint32_t*>(
+                        kv.pool + kv_offset(kv.layer, at, kv.n_pages, 1, head, H, (k0 + u0 + u) % kPage, HD) + dim);
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (seen >> (u0 + u) & 1) {
+                        const float pu = lane_value(p, u0 + u);
+                        oa = fmaf(pu, bflo(v[u]), oa);
+                        ob = fmaf(pu, bfhi(v[u]), ob);
+                    }
+            }
+        }
+        if (!__any(any)) break;
+#pragma unroll 1
+        for (int o = 1; o < 64 && turn < 2; o <<= 1) {
+            const float x = __shfl_xor(turn ? l : m, o, 64);
+            if (turn)
+                l += x;
+            else
+                m = fmaxf(m, x);
+        }
+    }
+    return make_float2(oa, ob);
+}
+
+// A row's values (a lane's two dims: sums over the sum of the weights) that are no
+// numbers, because of the products or because all weights are 0, become what
+// attend_plain finds; a row that sees nothing gets 0 from there.
+__device__ __forceinline__ bool row_odd(float a, float b) { return !__builtin_isfinite(a) || !__builtin_isfinite(b); }
+template <int HD>
+__device__ __forceinline__ uint32_t row_plain(float a, float b, const float* q, const KvTarget& kv, int seq, int plane,
+                                              int base, uint64_t mask, int head, int H) {
+    const float2 v = attend_plain<HD>(q, kv, seq, plane, base, mask, head, H);
+    return pack_bf16(__builtin_isfinite(a) ? a : v.x, __builtin_isfinite(b) ? b : v.y);
 }
 
 template <int HD, int NT, bool HALVES>
@@ -768,13 +857,32 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
             int tl = tid;
             asm volatile("" : "+v"(tl));
             const int dim = 2 * (tl & 63);
+            uint32_t odd_rows = 0;
 #pragma unroll
             for (int k = 0; k < NR; ++k) {
                 const int r = wave + kTreeWaves * k;
                 const float den = lane_value(tw, 8 * k);
-                if (r < x.n && dim < HD)
-                    *reinterpret_cast<uint32_t*>(out + frag_index(x.row0 + r, head * HD + dim, d)) =
-                        row_out2(tot[k][0], tot[k][1], den);
+                tot[k][0] /= den;
+                tot[k][1] /= den;
+                if (r < x.n) {
+                    odd_rows |= __any(row_odd(tot[k][0], tot[k][1])) ? 1u << k : 0u;
+                    if (dim < HD)
+                        *reinterpret_cast<uint32_t*>(out + frag_index(x.row0 + r, head * HD + dim, d)) =
+                            pack_bf16(tot[k][0], tot[k][1]);
+                }
+            }
+            while (__builtin_expect(odd_rows != 0, 0)) {  // rare
+                const int at = __ffs(odd_rows) - 1, row = x.row0 + wave + kTreeWaves * at;
+                odd_rows &= odd_rows - 1;
+                float a = tot[0][0], b = tot[0][1];
+#pragma unroll
+                for (int k = 1; k < NR; ++k) {
+                    a = at == k ? tot[k][0] : a;
+                    b = at == k ? tot[k][1] : b;
+                }
+                const uint32_t o = row_plain<HD>(a, b, q + (size_t)row * d + head * HD, kv, x.seq, x.plane, x.base,
+                                                 s_mask[row], head, H);
+                if (dim < HD) *reinterpret_cast<uint32_t*>(out + frag_index(row, head * HD + dim, d)) = o;
             }
         }
         if (next >= n_all) break;
@@ -787,7 +895,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const float* __restr
 // Rows whose segments went to several workgroups: their records joined, in segment
 // order.  One wave per (row, head), lane = two dims.
 template <int HD>
-__global__ __launch_bounds__(256) void k_tree_merge(KvTarget kv, const int32_t* __restrict__ seq, cdb_tree tree, int M,
+__global__ __launch_bounds__(256) void k_tree_merge(const float* __restrict__ q, KvTarget kv, const int32_t* __restrict__ seq, cdb_tree tree, int M,
                                                     int H, TreeScratch ts, uint16_t* __restrict__ out,
                                                     const int32_t* __restrict__ dn) {
     constexpr int REC = HD + 2;
@@ -818,8 +926,12 @@ __global__ __launch_bounds__(256) void k_tree_merge(KvTarget kv, const int32_t* 
             tb = join_sum(tb, v[u].y, a, b);
         }
     }
-    if (2 * lane < HD)
-        *reinterpret_cast<uint32_t*>(out + frag_index(row, head * HD + dim, H * HD)) = row_out2(ta, tb, tl);
+    ta /= tl;
+    tb /= tl;
+    uint32_t o = pack_bf16(ta, tb);
+    if (__builtin_expect(__any(row_odd(ta, tb)), 0))
+        o = row_plain<HD>(ta, tb, q + ((size_t)row * H + head) * HD, kv, s.seq, s.plane, s.base, s.mask, head, H);
+    if (2 * lane < HD) *reinterpret_cast<uint32_t*>(out + frag_index(row, head * HD + dim, H * HD)) = o;
 }
 
 // rows per tile
@@ -841,7 +953,7 @@ static hipError_t run_tree_attn(const float* q, const KvTarget& kv, const int32_
     else  // whole groups of 16
         k_tree_attn<HD, 2, true><<<(most + 15) / 16 * 16, kTreeThreads, 0, st>>>(q, kv, seq, tree, M, H, ts, out, err, dn, least);
     const bool split = segs > 1 && (dn || tree_runs(least * H * halves) > 1);
-    if (split) k_tree_merge<HD><<<(M * H + 3) / 4, 256, 0, st>>>(kv, seq, tree, M, H, ts, out, dn);
+    if (split) k_tree_merge<HD><<<(M * H + 3) / 4, 256, 0, st>>>(q, kv, seq, tree, M, H, ts, out, dn);
     return hipGetLastError();
 }
 

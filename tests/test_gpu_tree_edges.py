@@ -160,3 +160,123 @@ def test_holes_in_tables_and_stacks_change_nothing(where, S, P, layout):
     same()
     assert run(np.zeros(S)) == host.run(np.zeros(S)) == 0
     same()
+
+
+# ------------------------------------------------------------------ committed K/V that are not finite, or large
+
+def _place(pt, t, position, loop):
+    """(page id, token) of a position of sequence t in the loop's plane."""
+    return int(pt[t, loop + 1, position // 16]), position % 16
+
+
+LOOPS = (3, 0, 1, 2, 0)  # of _mixed's trees
+
+
+@pytest.mark.parametrize("hd,H", HEADS)
+@pytest.mark.parametrize("value", [float("inf"), -float("inf"), float("nan")])
+def test_committed_values_that_are_not_finite(hd, H, value):
+    """V of one dim of a committed position, in contexts of one segment and of several: that dim of the tree's rows becomes
+    what 64-bit arithmetic gets, everything else keeps its bits."""
+    shape, trees, b, kv, pt, q = _mixed(hd, H)
+    clean = _attend(shape, kv, b, q, 32)[:b.n]
+    dim = 1 * hd + 9
+    for t, position in ((0, 130), (2, 46), (3, 1050), (3, 17), (4, 3)):
+        page, tok = _place(pt, t, position, LOOPS[t])
+        before = kv.core[1, page, 1, 1, tok, 9].clone()
+        kv.core[1, page, 1, 1, tok, 9] = value
+        _say(f"[gpu] tree attention {H} x {hd}: V {value} at committed position {position}")
+        got = _attend(shape, kv, b, q, 32)[:b.n]
+        kv.core[1, page, 1, 1, tok, 9] = before
+        mine = torch.from_numpy(b.seq == t).cuda()
+        if value == value:
+            assert bool((got[mine, dim] == value).all()), (t, got[mine, dim])
+        else:
+            assert bool(got[mine, dim].isnan().all())
+        got[mine, dim] = clean[mine, dim]
+        assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("max_nodes", [16, 32, 64])
+def test_committed_values_that_are_not_finite_in_full_batches(max_nodes):
+    """Segments joined in registers (144 tiles and heads or more): the same."""
+    shape = _shape(128, 16)
+    rng = np.random.default_rng(4)
+    made = [(1030 + 5 * t, random_parents(rng, 3)) for t in range(9)]
+    b = _batch(rng, made, [0] * 9)
+    kv, pt = _cache(shape, [(0, base + 3) for base, _ in made], 8)
+    q = _q(shape, b.n, 8)
+    clean = _attend(shape, kv, b, q, max_nodes)[:b.n]
+    for t in (0, 4, 8):
+        page, tok = _place(pt, t, 500 + t, 0)
+        kv.core[1, page, 1, 5, tok, 77] = float("inf")
+    _say(f"[gpu] tree attention 16 x 128: infinite committed V, 9 trees, max_nodes {max_nodes}")
+    got = _attend(shape, kv, b, q, max_nodes)[:b.n]
+    mine, dim = torch.from_numpy(b.seq % 4 == 0).cuda(), 5 * 128 + 77
+    assert bool((got[mine, dim] == float("inf")).all())
+    got[mine, dim] = clean[mine, dim]
+    assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("hd,H", HEADS)
+def test_committed_keys_that_are_not_finite(hd, H):
+    """One dim of one committed K is -inf: where q is positive there the key has no weight, where it is negative its score
+    is +inf and the head's output NaN; other heads and trees keep their bits."""
+    shape, trees, b, kv, pt, q = _mixed(hd, H)
+    _say(f"[gpu] tree attention {H} x {hd}: K -inf at a committed position")
+    clean, signs = _attend(shape, kv, b, q, 32)[:b.n], set()
+    for t, position in ((0, 131), (3, 1049), (3, 5), (4, 15)):
+        page, tok = _place(pt, t, position, LOOPS[t])
+        before = kv.core[1, page, 0, 1, tok].clone()
+        rows = np.flatnonzero(b.seq == t)
+        sel = torch.from_numpy(rows).cuda()
+        kv.core[1, page, 0, 1, tok, 3] = -float("inf")
+        got = _attend(shape, kv, b, q, 32)[:b.n]
+        plus = q[sel][:, hd + 3].cpu() > 0
+        signs |= set(plus.tolist())
+        for i, r in enumerate(rows):
+            mine = got[r].cpu().double().view(H, hd)[1]
+            if not plus[i]:
+                assert bool(mine.isnan().all()), (t, position, r)
+                continue
+            core = kv.core[1].cpu().double()
+            seen = list(range(int(b.base[r]))) + [int(b.base[r]) + j for j in range(64) if int(b.mask[r]) >> j & 1]
+            seen.remove(position)
+            ids = torch.tensor([int(pt[t, LOOPS[t] + 1, p // 16]) for p in seen])
+            at = torch.tensor([p % 16 for p in seen])
+            k, v = core[ids, 0, 1, at], core[ids, 1, 1, at]
+            qi = q[r].cpu().double().view(H, hd)[1]
+            p = torch.softmax((k * qi).sum(-1) / hd ** 0.5, -1)
+            w = (p[:, None] * v).sum(0)
+            S = ((k * qi).abs().sum(-1) / hd ** 0.5).max()
+            bound = w.abs() * 2.0 ** -8 + (p[:, None] * v.abs()).sum(0) * \
+                (S * 2.0 ** -15 + 2.0 ** -16 + 2.0 ** -19 + len(seen) * 2.0 ** -23)
+            assert bool(((mine - w).abs() <= bound).all()), (t, position, r)
+        kv.core[1, page, 0, 1, tok] = before
+        got.view(b.n, H, hd)[sel, 1] = clean.view(b.n, H, hd)[sel, 1]
+        assert torch.equal(got, clean)
+    assert signs == {True, False}
+
+
+def _one_sequence(hd, H, base, k, v, q):
+    """One row over `base` committed positions and its own, all with these K and V."""
+    shape = _shape(hd, H)
+    b = _batch(np.random.default_rng(0), [(base, np.array([-1], np.int32))], [0])
+    kv, pt = _cache(shape, [(0, base + 1)], 1)
+    kv.core[1, :, 0] = k
+    kv.core[1, :, 1] = v
+    return shape, b, kv, torch.full((1, shape.d), q, device="cuda")
+
+
+@pytest.mark.parametrize("hd,H", HEADS)
+@pytest.mark.parametrize("base", [0, 1, 40, 1200])
+def test_scores_and_sums_at_the_ends_of_the_range(hd, H, base):
+    """Equal keys, so the output is V itself (each weight the same; off by the sum of base + 1 weights in 32 bits, and half a
+    step): scores of about -1e33, and V of 2e38, whose plain sum has no 32-bit value.  Nothing but scores of -inf: NaN."""
+    n = base + 1
+    for k, v, q in ((-2.0 ** 50, 1.25, 2.0 ** 57), (0.0, 2.0 ** 127 * 1.25, 1.0), (2.0 ** 50, -3.0, -(2.0 ** 57))):
+        shape, b, kv, qq = _one_sequence(hd, H, base, k, v, q)
+        _say(f"[gpu] tree attention {H} x {hd}: {n} keys of {k}, values of {v}")
+        got = _attend(shape, kv, b, qq, 1)[:1].double().cpu()
+        assert bool(((got - v).abs() <= abs(v) * (2.0 ** -8 + n * 2.0 ** -22)).all()), got
+    shape, b, kv, qq = _one_sequence(hd, H, base, -float("inf"), 1.0, 1.0)
+    assert bool(_attend(shape, kv, b, qq, 1)[0].isnan().all())
