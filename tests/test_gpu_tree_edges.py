@@ -280,3 +280,71 @@ def test_scores_and_sums_at_the_ends_of_the_range(hd, H, base):
         assert bool(((got - v).abs() <= abs(v) * (2.0 ** -8 + n * 2.0 ** -22)).all()), got
     shape, b, kv, qq = _one_sequence(hd, H, base, -float("inf"), 1.0, 1.0)
     assert bool(_attend(shape, kv, b, qq, 1)[0].isnan().all())
+
+
+# ------------------------------------------------------------------ one row, every way its segments are joined
+
+@pytest.mark.parametrize("hd,H", [(64, 16), (96, 16), (128, 16)])
+@pytest.mark.parametrize("max_nodes,n", [(16, 13), (32, 25), (64, 28)])
+def test_records_and_registers_give_the_same_bits(hd, H, max_nodes, n):
+    """Trees over several segments, in a batch of at least 144 (tile, head) pairs, whose segments are joined in registers, and
+    alone, where they go through records."""
+    shape = _shape(hd, H)
+    rng = np.random.default_rng(n)
+    made = [(1010 + 150 * t, random_parents(rng, n)) for t in range(9)]
+    assert 9 * n <= 256
+    b = _batch(rng, made, [t % shape.r_max for t in range(9)])
+    kv, pt = _cache(shape, [(t % shape.r_max, base + n) for t, (base, _) in enumerate(made)], n)
+    q = _q(shape, b.n, 9)
+    _say(f"[gpu] tree attention {H} x {hd}: 9 trees of {n} together and alone, max_nodes {max_nodes}")
+    whole = _attend(shape, kv, b, q, max_nodes)[:b.n]
+    for t in range(9):
+        idx = np.flatnonzero(b.seq == t)
+        sel = torch.from_numpy(idx).cuda()
+        got = _attend(shape, kv, b.take(idx), q[sel].contiguous(), max_nodes)[:n]
+        assert torch.equal(got, whole[sel]), t
+    some = np.arange(0, b.n, 29)
+    want, tol = _want(shape, kv, pt, b.take(some), q[torch.from_numpy(some).cuda()])
+    _close(whole[torch.from_numpy(some).cuda()], want, tol)
+
+
+@pytest.mark.parametrize("hd,H", [(64, 4), (128, 2)])
+def test_stage_calls_over_several_segments(hd, H):
+    """Stage calls over contexts past one segment, whose records stand behind the stage's own scratch: at capacity and of
+    exactly the rows the same bits, and every tree alone too."""
+    from test_gpu_tree_stages import Verify, _restore, _snapshot
+    shape = cdbgen.shrink(cdbgen.TINY, name=f"long-{H}x{hd}", d=H * hd, n_heads=H, head_dim=hd, d_ff=96)
+    rng = np.random.default_rng(hd)
+    v = Verify(shape, cdbgen.model_weights(shape), [(b, random_parents(rng, n)) for b, n in ((1100, 7), (3, 4), (2300, 9))],
+               tree.KV_FULL, 12, capacity=64)
+    v.state = cdb.State(shape, 64)
+    saved, both = _snapshot(v), []
+    _say(f"[gpu] stage calls {H} x {hd} over 1100, 3 and 2300 positions")
+    for exact in (True, False):
+        _restore(v, saved)
+        n = v.n if exact else 64
+        c, dep = np.zeros(n), np.full(n, 2)
+        if exact:
+            rows, see, tok = v.pick(np.arange(v.n), c, dep)
+        else:
+            rows, see, tok = v.laid.rows(np.arange(64), c, dep), v.laid.tree(v.max_nodes), v.laid.tokens
+        logits, ids = torch.zeros((n, shape.vocab), device="cuda"), torch.full((n,), -7, dtype=torch.int32, device="cuda")
+        tree.cdb_tree_prelude(v.model.model, v.kv.c, v.state.c, rows.c, see.c, tok, v.ws.buf)
+        tree.cdb_tree_step(v.model.model, v.kv.c, v.state.c, rows.c, see.c, cdb.StepOut(n).c, v.ws.buf)
+        tree.cdb_tree_coda(v.model.model, v.kv.c, v.state.c, rows.c, see.c, logits, ids, v.ws.buf)
+        torch.cuda.synchronize()
+        assert v.error() == 0
+        both.append([x[:v.n] if x.dim() == 2 else x for x in _snapshot(v)] + [logits[:v.n].clone(), ids[:v.n].clone()])
+    for k, (a, b) in enumerate(zip(*both)):
+        assert torch.equal(a, b), k
+    for t in range(3):
+        _restore(v, saved)
+        live = np.flatnonzero(v.row_tree == t)
+        rows, see, tok = v.pick(live, np.zeros(len(live)), np.full(len(live), 2))
+        logits, ids = torch.zeros((len(live), shape.vocab), device="cuda"), torch.zeros(len(live), dtype=torch.int32, device="cuda")
+        tree.cdb_tree_prelude(v.model.model, v.kv.c, v.state.c, rows.c, see.c, tok, v.ws.buf)
+        tree.cdb_tree_step(v.model.model, v.kv.c, v.state.c, rows.c, see.c, cdb.StepOut(len(live)).c, v.ws.buf)
+        tree.cdb_tree_coda(v.model.model, v.kv.c, v.state.c, rows.c, see.c, logits, ids, v.ws.buf)
+        torch.cuda.synchronize()
+        at = torch.from_numpy(live).cuda()
+        assert torch.equal(logits, both[0][-2][at]) and torch.equal(ids, both[0][-1][at]), t
