@@ -410,16 +410,17 @@ hipError_t launch_tree_accept(const cdb_drafts& d, const int32_t* row0, const in
 // goes from position len + path[i] to len + i <= it.  Every wave reads what the move
 // needs by itself (lane = path entry, page, or plane), so nothing waits at a
 // barrier; the chain of dependent loads (path and sequence, length, page ids, data)
-// bounds it (32 trees of 8 over 48 layer planes: 18 MB in 7.3 us, 2.5 TB/s).  A
+// bounds it (32 trees of 8 over 48 layer planes: 18 MB in 6.5 us, 2.8 TB/s).  A
 // thread owns 16-byte columns of the (K/V, head, dim) entry, two at once, and takes
 // the moves in order, loading eight before it stores them: move i's destination is
 // no later move's source (path[j] > path[i] >= i for j > i), so nothing is
 // overwritten before it is read.
 constexpr int kCommitBatch = 8;
-// Up to so many (unit, tree) pairs, workgroups share a unit's columns: one tree of
-// 24 nodes over 96 layer planes 5.0 us against 5.8; 64 of 4 over 48 layer planes
-// 11.1 us that way against 7.9.
-constexpr int kCommitSplit = 1024;
+// Up to so many (unit, tree) pairs, workgroups share a unit's columns; by pairs, shared
+// and not, trees of 8 over 48 layer planes of 16 x 128 heads: 240 4.1 and 4.2 us, 432 4.3
+// both, 480 5.3 and 4.6, 768 6.4 and 5.0, 1536 8.8 and 6.5; over 34 of 55 x 96: 272 5.1 and
+// 6.5, 408 5.2 and 5.6, 544 7.0 and 6.4; one tree of 24 over 96 of 16 x 128: 4.6 and 5.3.
+constexpr int kCommitSplit = 448;
 
 struct CommitStages {
     uint16_t* pool[3];
