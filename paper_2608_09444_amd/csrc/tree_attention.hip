@@ -5,9 +5,9 @@
 // The rows of one tree share their context, so its K and V are read once for up
 // to 64 of them and multiplied on MFMA (v_mfma_f32_16x16x32_bf16); with so few
 // rows per byte large calls are bound by HBM (64 trees of 4 over 2048..4223
-// positions, 16 x 128 heads: 1.63 GB in 261 us, 6.2 TB/s), wide trees by the
-// instructions of two waves per SIMD (4 trees of up to 64 over 1024..2047, 55 x 96
-// heads: 150 MB in 51 us) and small calls by latency (13 rows over 700: 12.1 us).
+// positions, 16 x 128 heads: 1.63 GB in 261-277 us, 5.9-6.2 TB/s), wide trees by the
+// instructions of two waves per SIMD (4 trees of 32-64 over 1024..2047, 55 x 96
+// heads: 150 MB in 50-55 us) and small calls by latency (13 rows over 700: 12.2 us).
 //
 // Tiles: adjacent rows of one sequence, plane and base, at most 16, 32 or 64 of
 // them (by cdb_tree.max_nodes).  A row's context is cut into segments

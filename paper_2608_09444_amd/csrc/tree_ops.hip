@@ -249,8 +249,8 @@ hipError_t launch_map_pages(const cdb_model_desc& md, int32_t* table, int S, int
 
 // ------------------------------------------------------------------ drafted trees as rows
 // One wave per tree, lane = node; every workgroup sums all trees' node counts.
-// Bound by latency (sequence, its length, the scan): 64 trees of 4 in 4.1 us, 4 of
-// 64 in 3.1, where an empty kernel takes 1.7.
+// Bound by latency (sequence, its length, the scan): 64 trees of 4 in 4.0 us, 4 of
+// 64 in 3.0, where an empty kernel takes 1.7.
 // A node's ancestors by doubling: with m = the nodes seen so far and p = the
 // node they end at, m |= m of p, p = p of p, six times for up to 64 nodes.
 __device__ __forceinline__ uint64_t shfl64(uint64_t v, int src) {
