@@ -8,8 +8,8 @@ import torch
 import cdbgen
 import paper_2608_09444_amd as cdb
 from paper_2608_09444_amd import tree
-from test_gpu_tree import (HEADS, HostPages, _attend, _batch, _cache, _close, _dev, _drafts, _host_rows, _mixed, _q, _say,
-                           _shape, _upload, _want, _ws, random_parents)
+from test_gpu_tree import (HEADS, HostPages, _attend, _batch, _cache, _close, _dev, _drafts, _graph, _host_rows, _mixed, _q,
+                           _say, _shape, _upload, _want, _ws, random_parents)
 
 pytestmark = pytest.mark.gpu
 
@@ -160,6 +160,42 @@ def test_holes_in_tables_and_stacks_change_nothing(where, S, P, layout):
     same()
     assert run(np.zeros(S)) == host.run(np.zeros(S)) == 0
     same()
+
+
+@pytest.mark.parametrize("S,P", [(60, 5), (300, 40)])
+def test_captured_mappings_and_holes(S, P):
+    """Growing and cutting back in graphs, replayed in turn; now and then a hole, mended before the next replay."""
+    shape, layout = cdbgen.TINY, tree.KV_FULL
+    rng = np.random.default_rng(S)
+    caps = (S * P, S * P * shape.r_max, S * P)
+    start = [rng.permutation(c).astype(np.int32) for c in caps]
+    host = HostPages(shape, S, P, caps, layout, start)
+    desc, ws = cdb.make_desc(shape), _ws(shape, 1, S)
+    table, mapped = _dev(host.table), _dev(host.mapped)
+    pools = [tree.PagePool(_dev(s), _dev([len(s)])) for s in start]
+    needs = [np.where(rng.random(S) < 0.1, -1, rng.integers(16, 16 * P + 1, S)), rng.integers(0, 16 * P + 1, S)]
+    needs[0][0], needs[1][0] = 16 * P, 0
+    up = [_dev(n) for n in needs]
+    calls = [lambda n=n: tree.cdb_map_pages(desc, table, *(p.c for p in pools), layout, n, mapped, ws.buf) for n in up]
+    graphs = [_graph(call) for call in calls]
+    _say(f"[gpu] captured mappings of {S} sequences")
+    for turn in range(8):
+        k = turn % 2
+        cell = (0, 2, P - 1)
+        if k == 1 and turn % 4 == 3:  # the first sequence gives everything back
+            keep = int(host.table[cell])
+            table[cell] = -1
+            graphs[k].replay()
+            torch.cuda.synchronize()
+            assert cdb.cdb_read_device_error(ws.buf) == cdb.CDB_DEV_UNMAPPED_PAGE and mapped.tolist() == host.mapped.tolist()
+            table[cell] = keep
+        (calls[k] if turn in (2, 5) else graphs[k].replay)()
+        torch.cuda.synchronize()
+        assert host.run(needs[k]) == 0 and cdb.cdb_read_device_error(ws.buf) == 0
+        assert (table.cpu().numpy() == host.table).all() and mapped.tolist() == host.mapped.tolist(), turn
+        for p, s in zip(pools, host.stacks):
+            assert int(p.free_count) == len(s) and p.free_ids[:len(s)].tolist() == s, turn
+    del graphs
 
 
 # ------------------------------------------------------------------ committed K/V that are not finite, or large
