@@ -9,7 +9,9 @@
  *   cdb_tree_prelude, cdb_tree_step, cdb_tree_coda
  *                      the stage calls, with cdb_tree_attention in every layer
  *   cdb_tree_accept    the path of drafted tokens that the model would have
- *                      produced itself (greedy), and the token that follows it
+ *                      produced itself (greedy), and the token that follows it,
+ *   or cdb_tree_sample a path and a token that are distributed as the model's own
+ *                      samples
  *   cdb_tree_commit    the K/V of that path moved to the positions it takes
  *   cdb_map_pages      the pages behind it given back
  *
@@ -192,6 +194,54 @@ typedef struct {
 cdb_status cdb_tree_accept(const cdb_drafts* drafts, const int32_t* row0, const int32_t* next_ids, int32_t n_rows,
                            const int32_t* first_ids, const cdb_accepted* out, void* ws, size_t ws_bytes,
                            hipStream_t stream);
+
+/* Device error code beside those above: logits that are no distribution (a NaN, an infinity
+ * that is not -inf, or nothing else than -inf), or a temperature that is not above 0. */
+enum { CDB_DEV_BAD_VALUE = 5 };
+
+#define CDB_SAMPLE_MAX_VOCAB (1 << 20)
+
+/* What sampled acceptance reads beside the trees (device):
+ *   logits         fp32, row r at logits + r * logits_stride: the target's after every
+ *                  drafted node, by row, as the coda writes them
+ *   draft_logits   the drafter's after every node, likewise: those that the node's children
+ *                  were drawn from, each by itself.  NULL: the drafter was sure of each
+ *                  token that it guessed (probability 1)
+ *   *_stride       in values, at least the model's vocab, a multiple of 4; the logits'
+ *                  addresses are multiples of 16
+ *   temperature, draft_temperature   fp32 [n_trees], above 0: the probabilities are
+ *                  softmax(logits / temperature); NULL: 1
+ *   u_node         fp32 [n_trees][max_nodes] random numbers, even in [0, 1), one per node
+ *   u_next         fp32 [n_trees] one per tree, for the token that follows
+ * -inf among the logits is a probability of 0 (tokens that are masked out). */
+typedef struct {
+    const float* logits;
+    const float* draft_logits;
+    int64_t logits_stride, draft_stride;
+    const float* temperature;
+    const float* draft_temperature;
+    const float* u_node;
+    const float* u_next;
+} cdb_sampling;
+
+/* Sampled acceptance: the accepted tokens and `next` are distributed as if each had
+ * been drawn from the target's probabilities in turn, whatever the drafter's are.  Walks down
+ * each tree: at first to the lowest root with token first_ids[t] (int32 [n_trees], the
+ * token already drawn after the committed positions; none: nothing is accepted and next is
+ * that token).  At a node with target p and drafter q, r = p; for its children in
+ * order, with token x and u of u_node:
+ *   u q(x) < r(x):  the child is accepted, and the walk goes on there;
+ *   otherwise       r <- max(r - q, 0), divided by its sum (a sure drafter: r without x,
+ *                   divided by its sum; if nothing is left, r stays).
+ * When no child is left, next is the first token whose cumulated r, from token 0 on, is above
+ * u_next times the sum of r.  Probabilities and sums are in 64 bits.
+ * The trees, row0, n_rows (at most 256 here) and `out` are as for cdb_tree_accept, with the
+ * same refusals; a drafted token outside [0, vocab) is not accepted (CDB_DEV_BAD_INDEX).
+ * A walk that comes to logits that are no distribution ends there, next = -1
+ * (CDB_DEV_BAD_VALUE); a tree with a bad temperature accepts nothing (the same code). */
+cdb_status cdb_tree_sample(const cdb_model_desc* desc, const cdb_drafts* drafts, const int32_t* row0, int32_t n_rows,
+                           const int32_t* first_ids, const cdb_sampling* sampling, const cdb_accepted* out, void* ws,
+                           size_t ws_bytes, hipStream_t stream);
 
 /* Moves the K/V of each tree's accepted nodes from cache position len + path[i]
  * to len + i, in every layer and plane of every stage (planes that share their

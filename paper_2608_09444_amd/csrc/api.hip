@@ -645,7 +645,8 @@ cdb_status cdb_paged_attention(const cdb_model_desc* desc, const cdb_kv* kv, con
 
 size_t cdb_tree_workspace_bytes(const cdb_model_desc* desc, int32_t max_rows, int32_t max_seqs) {
     if (!desc || !desc_supported(*desc) || max_rows < 0 || max_rows > kMaxRows || max_seqs < 0) return 0;
-    return cdb_workspace_bytes(desc, max_rows) + tree_scratch_bytes(*desc, max_rows);
+    return std::max(cdb_workspace_bytes(desc, max_rows) + tree_scratch_bytes(*desc, max_rows),
+                    256 + tree_sample_bytes(*desc, max_rows));
 }
 
 cdb_status cdb_map_pages(const cdb_model_desc* desc, int32_t* page_table, int32_t max_seqs, int32_t max_pages,
@@ -750,6 +751,29 @@ cdb_status cdb_tree_accept(const cdb_drafts* drafts, const int32_t* row0, const 
     return CDB_OK;
 }
 
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+cdb_status cdb_tree_sample(const cdb_model_desc* desc, const cdb_drafts* drafts, const int32_t* row0, int32_t n_rows,
+                           const int32_t* first_ids, const cdb_sampling* sampling, const cdb_accepted* out, void* ws,
+                           size_t ws_bytes, hipStream_t st) {
+    if (!desc || !ws || !sampling || !out || n_rows < 0) return CDB_ERR_INVALID_ARG;
+    if (!desc_supported(*desc) || desc->vocab > CDB_SAMPLE_MAX_VOCAB) return CDB_ERR_UNSUPPORTED;
+    const cdb_status s = check_drafts(drafts, false, true);
+    if (s != CDB_OK) return s;
+    if (n_rows > kMaxRows || ws_bytes < 256 + tree_sample_bytes(*desc, n_rows)) return CDB_ERR_CAPACITY;
+    if (drafts->n_trees == 0) return CDB_OK;
+    const cdb_sampling& m = *sampling;
+    if (!row0 || !first_ids || !m.u_node || !m.u_next || !out->path || !out->count || !out->next) return CDB_ERR_INVALID_ARG;
+    if (n_rows > 0) {
+        if (!m.logits || !aligned16(m.logits) || !aligned16(m.draft_logits)) return CDB_ERR_INVALID_ARG;
+        if (m.logits_stride < desc->vocab || m.logits_stride % 4) return CDB_ERR_INVALID_ARG;
+        if (m.draft_logits && (m.draft_stride < desc->vocab || m.draft_stride % 4)) return CDB_ERR_INVALID_ARG;
+    }
+    HIPCHK(launch_tree_sample(*desc, *drafts, row0, n_rows, first_ids, m, *out, static_cast<unsigned char*>(ws) + 256,
+                              static_cast<int*>(ws), st));
+    return CDB_OK;
+}
+
 cdb_status cdb_tree_commit(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_drafts* drafts,
                            const cdb_accepted* accepted, void* ws, size_t ws_bytes, hipStream_t st) {
     if (!desc || !kv || !accepted || !ws) return CDB_ERR_INVALID_ARG;
@@ -766,6 +790,75 @@ cdb_status cdb_tree_commit(const cdb_model_desc* desc, const cdb_kv* kv, const c
     for (const KvTarget& k : t)
         if (k.n_layers > 0 && (!k.pool || k.n_pages < 0)) return CDB_ERR_INVALID_ARG;
     HIPCHK(launch_tree_commit(d, t, *drafts, *accepted, static_cast<int*>(ws), st));
+    return CDB_OK;
+}
+
+// ---------------------------------------------------------------- chunks of new tokens
+
+size_t cdb_chunk_workspace_bytes(const cdb_model_desc* desc, int32_t max_rows, int32_t max_chunks) {
+    if (!desc || !desc_supported(*desc) || max_rows < 0 || max_rows > CDB_MAX_CHUNK_ROWS || max_chunks < 0 ||
+        max_chunks > CDB_MAX_CHUNKS)
+        return 0;
+    return 256 + chunk_scratch_bytes(*desc, max_rows);
+}
+
+// What both calls check; *t: the layer's cache.  *nothing: there are no rows.
+static cdb_status check_chunks(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_chunks* ch, int32_t stage,
+                               int32_t layer, int32_t q_type, const void* ws, KvTarget* t, bool* nothing) {
+    *nothing = true;
+    if (!desc || !kv || !ch || !ws) return CDB_ERR_INVALID_ARG;
+    const cdb_model_desc& d = *desc;
+    if (!desc_supported(d)) return CDB_ERR_UNSUPPORTED;
+    if (stage < 0 || stage > 2 || ch->n_chunks < 0 || ch->n_rows < 0) return CDB_ERR_INVALID_ARG;
+    if (q_type != CDB_F32 && q_type != CDB_BF16) return CDB_ERR_INVALID_ARG;
+    const int layers = stage == 0 ? d.n_prelude : (stage == 1 ? d.n_core : d.n_coda);
+    if (layer < 0 || layer >= layers) return CDB_ERR_INVALID_ARG;
+    if (ch->n_chunks > CDB_MAX_CHUNKS || ch->n_rows > CDB_MAX_CHUNK_ROWS) return CDB_ERR_CAPACITY;
+    if (ch->n_chunks == 0 || ch->n_rows == 0) return CDB_OK;
+    if (!ch->row0 || !ch->seq || !ch->pos0 || (stage == 1 && !ch->c) || !kv->page_table) return CDB_ERR_INVALID_ARG;
+    *t = stage_target(d, *kv, stage);
+    if (!t->pool || kv->max_seqs < 0 || kv->max_pages < 0 || t->n_pages < 1) return CDB_ERR_INVALID_ARG;
+    if (kv->max_pages > kMaxTablePages) return CDB_ERR_CAPACITY;
+    t->layer = layer;
+    if (stage == 1) t->c_row = ch->c;
+    *nothing = false;
+    return CDB_OK;
+}
+
+cdb_status cdb_chunk_qkv(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_chunks* chunks, int32_t stage,
+                         int32_t layer, const cdb_qkv* in, void* q_out, int32_t q_type, void* ws, size_t ws_bytes,
+                         hipStream_t st) {
+    KvTarget t{};
+    bool nothing;
+    const cdb_status s = check_chunks(desc, kv, chunks, stage, layer, q_type, ws, &t, &nothing);
+    if (s != CDB_OK) return s;
+    if (!in || (in->type != CDB_F32 && in->type != CDB_BF16) || (in->norm != 0 && in->norm != 1)) return CDB_ERR_INVALID_ARG;
+    if (ws_bytes < 256) return CDB_ERR_CAPACITY;
+    if (nothing) return CDB_OK;
+    if (!in->q || !in->k || !in->v || !q_out) return CDB_ERR_INVALID_ARG;
+    const int per16 = in->type == CDB_F32 ? 4 : 8;
+    for (const int64_t n : {in->q_stride, in->k_stride, in->v_stride})
+        if (n < desc->d || n % per16) return CDB_ERR_INVALID_ARG;
+    for (const void* p : {in->q, in->k, in->v, static_cast<const void*>(q_out), in->q_gain, in->k_gain})
+        if (!aligned16(p)) return CDB_ERR_INVALID_ARG;
+    HIPCHK(launch_chunk_qkv(*desc, *chunks, t, *in, q_out, q_type, static_cast<int*>(ws), st));
+    return CDB_OK;
+}
+
+cdb_status cdb_chunk_attention(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_chunks* chunks, int32_t stage,
+                               int32_t layer, const void* q, int32_t q_type, void* out, int32_t out_order, void* ws,
+                               size_t ws_bytes, hipStream_t st) {
+    KvTarget t{};
+    bool nothing;
+    const cdb_status s = check_chunks(desc, kv, chunks, stage, layer, q_type, ws, &t, &nothing);
+    if (s != CDB_OK) return s;
+    if (out_order != CDB_ORDER_FRAGMENTS && out_order != CDB_ORDER_ROWS) return CDB_ERR_INVALID_ARG;
+    if (ws_bytes < 256 + chunk_scratch_bytes(*desc, chunks->n_rows)) return CDB_ERR_CAPACITY;
+    if (nothing) return CDB_OK;
+    if (!q || !out || !aligned16(q) || !aligned16(out)) return CDB_ERR_INVALID_ARG;
+    HIPCHK(launch_chunk_attention(*chunks, t, q, q_type, desc->n_heads, desc->head_dim,
+                                  static_cast<unsigned char*>(ws) + 256, static_cast<uint16_t*>(out), out_order,
+                                  static_cast<int*>(ws), st));
     return CDB_OK;
 }
 

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "../../include/libcdb.h"
+#include "../../include/libcdb_chunk.h"
 #include "../../include/libcdb_tree.h"
 
 namespace cdb {
@@ -244,9 +245,30 @@ hipError_t launch_map_pages(const cdb_model_desc& md, int32_t* table, int S, int
 hipError_t launch_tree_rows(const cdb_drafts& d, const cdb_row_map& out, int* err, hipStream_t st);
 hipError_t launch_tree_accept(const cdb_drafts& d, const int32_t* row0, const int32_t* next_ids, int n_rows,
                               const int32_t* first_ids, const cdb_accepted& out, int* err, hipStream_t st);
+// bytes of the sampled acceptance's scratch behind a workspace's first 256
+size_t tree_sample_bytes(const cdb_model_desc& d, int rows);
+hipError_t launch_tree_sample(const cdb_model_desc& md, const cdb_drafts& d, const int32_t* row0, int n_rows,
+                              const int32_t* first_ids, const cdb_sampling& sm, const cdb_accepted& out, void* scratch,
+                              int* err, hipStream_t st);
 // kv: of the three stages
 hipError_t launch_tree_commit(const cdb_model_desc& md, const KvTarget (&kv)[3], const cdb_drafts& d,
                               const cdb_accepted& acc, int* err, hipStream_t st);
+
+// ---------------------------------------------------------------- chunks of new tokens
+// Segments of a context: how many a launch wants for each (tile, head), and the most that
+// there are records for, kChunkSegments and kChunkRecordRows / n_rows.
+constexpr int kChunkSegments = 16, kChunkRecordRows = 4096;
+struct ChunkSplit {
+    int want, most;
+};
+ChunkSplit chunk_split(int H, int n_chunks, int n_rows, int max_pages);
+// bytes of the attention's scratch behind the workspace's first 256, for calls of up to `rows` rows
+size_t chunk_scratch_bytes(const cdb_model_desc& d, int rows);
+// kv.c_row: the chunks' loops
+hipError_t launch_chunk_attention(const cdb_chunks& ch, const KvTarget& kv, const void* q, int q_type, int H, int hd,
+                                  void* scratch, uint16_t* out, int order, int* err, hipStream_t st);
+hipError_t launch_chunk_qkv(const cdb_model_desc& md, const cdb_chunks& ch, const KvTarget& kv, const cdb_qkv& in,
+                            void* q_out, int q_type, int* err, hipStream_t st);
 
 enum PackKind : int { PACK_PLAIN = 0, PACK_QKV = 1, PACK_GU = 2 };
 

@@ -1,0 +1,461 @@
+// Causal attention of chunks of new tokens (several sequences, one to thousands of
+// rows each) over the paged, depth-indexed KV cache.
+#include <algorithm>
+
+#include "cdb_internal.h"
+
+namespace cdb {
+
+constexpr int kTileRows = 128;  // rows of a workgroup: 32 to each of its 4 waves
+constexpr int kStep = 64;       // keys that a workgroup stages at a time, a page to each wave
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// Segments that a context of `keys` positions is cut into: as many as the launch wants to fill the
+// GPU (of 256 positions at least), and none longer than 2048 positions, as far as
+// there are records for them.
+__host__ __device__ __forceinline__ int chunk_segments(int keys, const ChunkSplit& s, int* len) {
+    const int fill = (keys + 255) / 256;
+    int n = (keys + 2047) / 2048;
+    if (n < (fill < s.want ? fill : s.want)) n = fill < s.want ? fill : s.want;
+    if (n > s.most) n = s.most;
+    *len = ((keys + n - 1) / n + kStep - 1) / kStep * kStep;
+    return (keys + *len - 1) / *len;
+}
+
+ChunkSplit chunk_split(int H, int n_chunks, int n_rows, int max_pages) {
+    ChunkSplit s{1, 1};
+    const int tiles = std::max(n_chunks, (n_rows + kTileRows - 1) / kTileRows);
+    s.want = std::max(1, (512 + tiles * H - 1) / std::max(1, tiles * H));
+    s.most = std::max(1, std::min(kChunkSegments, kChunkRecordRows / std::max(1, n_rows)));
+    const int64_t longest = (int64_t)max_pages * kPage;
+    if (longest <= 256 || (s.want == 1 && longest <= 2048)) s.most = 1;
+    return s;
+}
+
+size_t chunk_scratch_bytes(const cdb_model_desc& d, int rows) {
+    const int64_t n = std::min<int64_t>((int64_t)rows * kChunkSegments, kChunkRecordRows);
+    return (size_t)n * d.n_heads * (d.head_dim + 2) * 4;
+}
+
+struct ChunkAttnArgs {
+    cdb_chunks ch;
+    KvTarget kv;
+    const void* q;
+    uint16_t* out;
+    int order, H, xcd_heads;
+    ChunkSplit split;
+    float* part;  // [rows][H][split.most][hd], then maxima and weights [rows][H][split.most][2]
+    float2* ml;
+    int* err;
+};
+
+// A tile of one chunk's rows.
+struct ChunkTile {
+    int row, n;     // first row in the call's buffers, rows
+    int pos;        // position of the first row
+    int seq, plane;
+    int found;
+};
+
+// The from_last-th tile from the end (later tiles of a chunk see longer contexts,
+// so they come first).  Run by all 256 threads, thread = chunk; false: there is no
+// such tile, or nothing is to be done for it.
+__device__ __forceinline__ bool chunk_tile(const ChunkAttnArgs& a, int from_last, ChunkTile* s_tile, int* s_red, bool tells) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    int r0 = 0, r1 = 0, seq = -1, pos = 0, c = 0;
+    if (tid < a.ch.n_chunks) {
+        r0 = a.ch.row0[tid];
+        r1 = a.ch.row0[tid + 1];
+        seq = a.ch.seq[tid];
+        pos = a.ch.pos0[tid];
+        if (a.kv.c_row) c = a.kv.c_row[tid];
+    }
+    const bool bad = r0 < 0 || r1 < r0 || r1 > a.ch.n_rows;
+    const int nt = bad ? 0 : (r1 - r0 + kTileRows - 1) / kTileRows;
+    int v = nt;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(v, o, 64);
+        if (lane >= o) v += u;
+    }
+    const bool any_bad = __any(bad);
+    if (lane == 63) s_red[w] = any_bad ? 1 << 20 : v;
+    if (tid == 0) s_tile->found = 0;
+    __syncthreads();
+    int total = 0, before = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i < w) before += s_red[i];
+        total += s_red[i];
+    }
+    if (total >= 1 << 20) {
+        if (tells && tid == 0) set_err(a.err, CDB_DEV_BAD_INDEX);
+        return false;
+    }
+    const int tile = total - 1 - from_last, first = before + v - nt;
+    if (tile < 0) return false;
+    if (tile >= first && tile < first + nt) {
+        const int n = r1 - r0, skip = (tile - first) * kTileRows;
+        const int plane = a.kv.c_row ? c + 1 : a.kv.plane_fixed;
+        const bool ok = seq >= 0 && seq < a.kv.max_seqs && pos >= 0 && pos <= a.kv.max_pages * kPage - n &&
+                        (!a.kv.c_row || (c >= 0 && c < a.kv.n_planes - 2));
+        if (!ok) set_err(a.err, CDB_DEV_BAD_INDEX);
+        *s_tile = ChunkTile{r0 + skip, min(kTileRows, n - skip), pos + skip, seq, plane, ok};
+    }
+    __syncthreads();
+    return s_tile->found;
+}
+
+// (head, rest) of a workgroup.  Workgroups go round the 8 XCDs by their index, so
+// with xcd_heads a head stays on one of them, whose L2 then holds its K and V for
+// all tiles.
+__device__ __forceinline__ bool chunk_head(const ChunkAttnArgs& a, int id, int* head, int* rest) {
+    if (!a.xcd_heads) {
+        *head = id % a.H;
+        *rest = id / a.H;
+        return true;
+    }
+    const int slot = id >> 3;
+    *head = (slot % a.xcd_heads) * 8 + (id & 7);
+    *rest = slot / a.xcd_heads;
+    return *head < a.H;
+}
+
+__device__ __forceinline__ uint16_t* chunk_out(const ChunkAttnArgs& a, int row, int k, int d) {
+    return a.out + (a.order == CDB_ORDER_ROWS ? (size_t)row * d + k : frag_index(row, k, d));
+}
+
+__device__ __forceinline__ bool odd_words(u32x4 x) {  // an infinity or NaN among 8 bf16 values
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) odd |= (x[i] & 0x7f80u) == 0x7f80u || (x[i] & 0x7f800000u) == 0x7f800000u;
+    return odd;
+}
+
+template <int HD, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
+    constexpr int NT = HD / 16, NB = HD / 32, NL = HD / 32, CPK = HD / 8;
+    constexpr int KP = HD + 8;                      // K row pitch: consecutive keys 4 banks apart (mod 64)
+    constexpr int VP = HD == 96 ? HD : HD + 32;     // V row pitch: consecutive keys 16 banks apart (mod 64)
+    __shared__ __align__(16) uint16_t sk[2][kStep * KP];
+    __shared__ __align__(16) uint16_t sv[2][kStep * VP];
+    __shared__ __align__(16) int s_flag[2][4];
+    __shared__ ChunkTile s_tile;
+    __shared__ int s_red[4];
+    int head, rest;
+    if (!chunk_head(a, blockIdx.x, &head, &rest)) return;
+    const int seg = rest % a.split.most;
+    if (!chunk_tile(a, rest / a.split.most, &s_tile, s_red, blockIdx.x == 0)) return;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int t_row = __builtin_amdgcn_readfirstlane(s_tile.row), t_n = __builtin_amdgcn_readfirstlane(s_tile.n);
+    const int t_pos = __builtin_amdgcn_readfirstlane(s_tile.pos);
+    const int last = t_pos + t_n - 1;  // the last position that any row sees
+    int seg_len;
+    const int segs = chunk_segments(last + 1, a.split, &seg_len);
+    if (seg >= segs) return;
+    const int k0 = seg * seg_len, k1 = min(last + 1, k0 + seg_len);
+    const int d = a.H * HD;
+    const int my = w * 32 + c32;  // this lane's row in the tile
+    const int qpos = t_pos + my;
+    const int w_last = t_pos + min(t_n, w * 32 + 32) - 1;  // the last position that the wave's rows see
+    const bool w_any = w * 32 < t_n;
+    const int32_t* pt = a.kv.page_table + ((size_t)__builtin_amdgcn_readfirstlane(s_tile.seq) * a.kv.n_planes +
+                                           __builtin_amdgcn_readfirstlane(s_tile.plane)) * a.kv.max_pages;
+
+    // staging: wave w takes page w of a step
+    u32x4 kr[NL], vr[NL];
+    auto page_of = [&](int k) {  // -1: behind the segment, or not mapped
+        const int at = k + w * kPage;
+        if (at >= k1) return -2;
+        const int pid = __builtin_amdgcn_readfirstlane(pt[at / kPage]);
+        return pid >= 0 && pid < a.kv.n_pages ? pid : -1;
+    };
+    auto fetch = [&](int pid) {
+        if (pid >= 0) {
+            const uint16_t* at = a.kv.pool + kv_offset(a.kv.layer, pid, a.kv.n_pages, 0, head, a.H, 0, HD) + lane * 8;
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                kr[i] = *reinterpret_cast<const u32x4*>(at + i * 512);
+                vr[i] = *reinterpret_cast<const u32x4*>(at + (size_t)a.H * kPage * HD + i * 512);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NL; ++i) kr[i] = vr[i] = u32x4{0, 0, 0, 0};
+        }
+    };
+    // A step whose keys not all rows see: V behind the last position becomes 0, and a V that is not finite too
+    // (put_odd adds it to the rows that see it).
+    auto stage = [&](int k, int pid, int b) {
+        int flag = pid >= 0;
+        if (k + kStep - 1 > t_pos && pid >= 0) {
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int key = k + w * kPage + (i * 64 + lane) / CPK;
+                const bool gone = key > last, o = !gone && odd_words(vr[i]);
+                odd |= o;
+                if (gone) vr[i] = u32x4{0, 0, 0, 0};
+                if (o)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        if ((vr[i][x] & 0x7f80u) == 0x7f80u) vr[i][x] &= 0xffff0000u;
+                        if ((vr[i][x] & 0x7f800000u) == 0x7f800000u) vr[i][x] &= 0xffffu;
+                    }
+            }
+            if (__any(odd)) flag |= 2;
+        }
+        if (pid == -1 && lane == 0) set_err(a.err, CDB_DEV_UNMAPPED_PAGE);
+        if (lane == 0) s_flag[b][w] = flag;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int f = i * 64 + lane, key = w * kPage + f / CPK, cc = f % CPK;
+            *reinterpret_cast<u32x4*>(&sk[b][key * KP + cc * 8]) = kr[i];
+            *reinterpret_cast<u32x4*>(&sv[b][key * VP + cc * 8]) = vr[i];
+        }
+    };
+
+    int pid = page_of(k0), pid_next = page_of(k0 + kStep);
+    fetch(pid);
+
+    // q as the B operand: dims 16 t + 8 half + e of row c32; in two parts it takes the scale along
+    const float scale = 1.4426950408889634f / sqrtf((float)HD);
+    bf16x8 qh[NT], ql[SPLIT ? NT : 1];
+    {
+        const bool live = my < t_n;
+        const size_t at = (size_t)(t_row + (live ? my : 0)) * d + head * HD + half * 8;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if constexpr (SPLIT) {
+                const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + t * 16);
+                const float4 x = src[0], y = src[1];
+                const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                uint32_t hw[4], lw[4];
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float v0 = v[e] * scale, v1 = v[e + 1] * scale;
+                    const uint32_t h = pack_bf16(v0, v1);
+                    hw[e / 2] = h;
+                    lw[e / 2] = pack_bf16(v0 - bflo(h), v1 - bfhi(h));
+                }
+                qh[t] = __builtin_bit_cast(bf16x8, u32x4{hw[0], hw[1], hw[2], hw[3]});
+                ql[t] = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], lw[2], lw[3]});
+            } else {
+                qh[t] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) + at + t * 16));
+            }
+        }
+    }
+    const float s_scale = SPLIT ? 1.f : scale;
+
+    floatx16 o[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[b][j] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    stage(k0, pid, 0);
+    for (int k = k0, b = 0; k < k1; k += kStep, b ^= 1) {
+        __syncthreads();
+        const bool more = k + kStep < k1;
+        if (more) {
+            pid = pid_next;
+            fetch(pid);
+            pid_next = page_of(k + 2 * kStep);
+        }
+        if (w_any && k <= w_last) {
+            const u32x4 fl = *reinterpret_cast<const u32x4*>(s_flag[b]);
+            const int there = __builtin_amdgcn_readfirstlane((fl[0] & 1) | (fl[1] & 1) << 1 | (fl[2] & 1) << 2 | (fl[3] & 1) << 3);
+            const bool odd = __builtin_amdgcn_readfirstlane((fl[0] | fl[1] | fl[2] | fl[3]) & 2);
+            const bool masked = k + kStep - 1 > t_pos + w * 32 || there != 15;
+            floatx16 s[2];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[kb][j] = 0.f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const bf16x8 ka = *reinterpret_cast<const bf16x8*>(&sk[b][(kb * 32 + c32) * KP + t * 16 + half * 8]);
+                    if constexpr (SPLIT) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, ql[t], s[kb], 0, 0, 0);
+                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qh[t], s[kb], 0, 0, 0);
+                }
+            if (masked)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const int key = k + kb * 32 + (j >> 2) * 8 + half * 4 + (j & 3);
+                        if (key > qpos || !(there >> (kb * 2 + (j >> 3)) & 1)) s[kb][j] = -INFINITY;
+                    }
+            float mx = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+            for (int j = 1; j < 16; ++j) mx = fmaxf(fmaxf(mx, s[0][j]), s[1][j]);
+            {
+                const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * s_scale;
+            }
+            const bool up = mx > m + 8.f;
+            if (__any(up)) {
+                const float corr = up ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
+                m = up ? mx : m;
+                l *= corr;
+#pragma unroll
+                for (int x = 0; x < NB; ++x)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[x][j] *= corr;
+            }
+            const float mref = m == -INFINITY ? 0.f : m;  // nothing seen yet: every weight 0
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    uint32_t hw[4], lw[4];
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kb][st * 8 + e], s_scale, -mref));
+                        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[kb][st * 8 + e + 1], s_scale, -mref));
+                        l += p0 + p1;
+                        hw[e / 2] = pack_bf16(p0, p1);
+                        if constexpr (SPLIT) lw[e / 2] = pack_bf16(p0 - bflo(hw[e / 2]), p1 - bfhi(hw[e / 2]));
+                    }
+                    const bf16x8 ph = __builtin_bit_cast(bf16x8, u32x4{hw[0], hw[1], hw[2], hw[3]});
+                    bf16x8 pl = ph;
+                    if constexpr (SPLIT) pl = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], lw[2], lw[3]});
+                    const int g = lane >> 4, c = lane & 15;
+                    const uint16_t* vb = &sv[b][(kb * 32 + st * 16 + 4 * half + (c >> 2)) * VP + (g & 1) * 16 + (c & 3) * 4];
+#pragma unroll
+                    for (int x = 0; x < NB; ++x) {
+                        const uint2 w0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                                       (__attribute__((address_space(3))) s16x4*)(vb + x * 32)));
+                        const uint2 w1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                                       (__attribute__((address_space(3))) s16x4*)(vb + 8 * VP + x * 32)));
+                        const bf16x8 va = __builtin_bit_cast(bf16x8, u32x4{w0.x, w0.y, w1.x, w1.y});
+                        if constexpr (SPLIT) o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pl, o[x], 0, 0, 0);
+                        o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, ph, o[x], 0, 0, 0);
+                    }
+                }
+            if (odd) {  // rare: values taken out by stage, to the rows that see them
+#pragma unroll 1
+                for (int key = k; key < min(k + kStep, last + 1); ++key) {
+                    const int id = pt[key / kPage];
+                    if (id < 0 || id >= a.kv.n_pages) continue;
+                    const uint16_t* at = a.kv.pool + kv_offset(a.kv.layer, id, a.kv.n_pages, 1, head, a.H, key % kPage, HD) + half * 4;
+#pragma unroll
+                    for (int x = 0; x < NB; ++x)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const uint16_t v = at[x * 32 + (j >> 2) * 8 + (j & 3)];
+                            if ((v & 0x7f80) == 0x7f80 && key <= qpos) o[x][j] += bf2f(v);
+                        }
+                }
+            }
+        }
+        if (more) stage(k + kStep, pid, b ^ 1);
+    }
+
+    {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+        l = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (my >= t_n) return;
+    const int row = t_row + my;
+    if (segs == 1) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int x = 0; x < NB; ++x)
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                uint2 v;
+                v.x = pack_bf16(o[x][j] * inv, o[x][j + 1] * inv);
+                v.y = pack_bf16(o[x][j + 2] * inv, o[x][j + 3] * inv);
+                *reinterpret_cast<uint2*>(chunk_out(a, row, head * HD + x * 32 + j * 2 + half * 4, d)) = v;
+            }
+        return;
+    }
+    const size_t rec = ((size_t)row * a.H + head) * a.split.most + seg;
+    if (half == 0) a.ml[rec] = make_float2(m, l);
+#pragma unroll
+    for (int x = 0; x < NB; ++x)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4)
+            *reinterpret_cast<float4*>(a.part + rec * HD + x * 32 + j * 2 + half * 4) =
+                make_float4(o[x][j], o[x][j + 1], o[x][j + 2], o[x][j + 3]);
+}
+
+// Segments of a tile's rows joined, in order.  Workgroup = (head, tile).
+template <int HD>
+__global__ __launch_bounds__(256) void k_chunk_merge(ChunkAttnArgs a) {
+    __shared__ ChunkTile s_tile;
+    __shared__ int s_red[4];
+    const int head = blockIdx.x % a.H;
+    if (!chunk_tile(a, blockIdx.x / a.H, &s_tile, s_red, false)) return;
+    const ChunkTile t = s_tile;
+    int seg_len;
+    const int segs = chunk_segments(t.pos + t.n, a.split, &seg_len);
+    if (segs == 1) return;
+    constexpr int CPR = HD / 8;  // threads of a row
+    for (int i = threadIdx.x; i < t.n * CPR; i += 256) {
+        const int row = t.row + i / CPR, c = i % CPR;
+        const size_t rec = ((size_t)row * a.H + head) * a.split.most;
+        float top = -INFINITY;
+        for (int s = 0; s < segs; ++s) top = fmaxf(top, a.ml[rec + s].x);
+        float num[8] = {}, den = 0.f;
+        if (top > -INFINITY)
+            for (int s = 0; s < segs; ++s) {
+                const float2 x = a.ml[rec + s];
+                const float f = __builtin_amdgcn_exp2f(x.x - top);
+                den += f * x.y;
+                const float4* p = reinterpret_cast<const float4*>(a.part + (rec + s) * HD + c * 8);
+                const float4 u = p[0], v = p[1];
+                const float y[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) num[e] += f * y[e];
+            }
+        const float inv = den == 0.f ? 0.f : 1.f / den;
+        u32x4 out;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = pack_bf16(num[2 * e] * inv, num[2 * e + 1] * inv);
+        *reinterpret_cast<u32x4*>(chunk_out(a, row, head * HD + c * 8, a.H * HD)) = out;
+    }
+}
+
+template <int HD>
+static void launch_hd(const ChunkAttnArgs& a, bool split, int groups, int tiles, hipStream_t st) {
+    if (split)
+        k_chunk_attn<HD, true><<<groups, 256, 0, st>>>(a);
+    else
+        k_chunk_attn<HD, false><<<groups, 256, 0, st>>>(a);
+    if (a.split.most > 1) k_chunk_merge<HD><<<tiles * a.H, 256, 0, st>>>(a);
+}
+
+hipError_t launch_chunk_attention(const cdb_chunks& ch, const KvTarget& kv, const void* q, int q_type, int H, int hd,
+                                  void* scratch, uint16_t* out, int order, int* err, hipStream_t st) {
+    if (ch.n_chunks <= 0 || ch.n_rows <= 0) return hipSuccess;
+    ChunkAttnArgs a{};
+    a.ch = ch;
+    a.kv = kv;
+    a.q = q;
+    a.out = out;
+    a.order = order;
+    a.H = H;
+    a.xcd_heads = (H + 7) / 8 * 8 * 8 <= H * 9 ? (H + 7) / 8 : 0;
+    a.split = chunk_split(H, ch.n_chunks, ch.n_rows, kv.max_pages);
+    a.part = static_cast<float*>(scratch);
+    a.ml = reinterpret_cast<float2*>(a.part + (size_t)ch.n_rows * H * a.split.most * hd);
+    a.err = err;
+    // every chunk has one tile that is not full at most
+    const int tiles = std::min(ch.n_chunks, ch.n_rows) + ch.n_rows / kTileRows;
+    const int groups = (a.xcd_heads ? a.xcd_heads * 8 : H) * tiles * a.split.most;
+    switch (hd) {
+        case 64: launch_hd<64>(a, q_type == CDB_F32, groups, tiles, st); break;
+        case 96: launch_hd<96>(a, q_type == CDB_F32, groups, tiles, st); break;
+        case 128: launch_hd<128>(a, q_type == CDB_F32, groups, tiles, st); break;
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace cdb

@@ -1,5 +1,5 @@
 """Python binding of libcdb's verification of drafted tokens (include/libcdb_tree.h): page tables from sequence lengths,
-drafted trees as rows, their attention and stage calls, greedy acceptance, and the move of the accepted K/V.
+drafted trees as rows, their attention and stage calls, greedy and sampled acceptance, and the move of the accepted K/V.
 
 Argument marshalling only; the calls run in the HIP kernels of libcdb.so.  The holder classes check their tensors (device,
 type, size, contiguity) and raise CdbError(CDB_ERR_INVALID_ARG); the calls take their C structs, as those of the package do
@@ -15,11 +15,11 @@ from . import (CDB_ERR_CAPACITY, CDB_ERR_INVALID_ARG, MAX_ROWS, CdbError, _check
                cdb_model_desc, cdb_rows, cdb_state, cdb_step_out, cdb_workspace_init, lib as _lib)
 
 EXPORTED = ("cdb_tree_workspace_bytes", "cdb_map_pages", "cdb_tree_rows", "cdb_tree_attention", "cdb_tree_prelude",
-            "cdb_tree_step", "cdb_tree_coda", "cdb_tree_accept", "cdb_tree_commit")
+            "cdb_tree_step", "cdb_tree_coda", "cdb_tree_accept", "cdb_tree_sample", "cdb_tree_commit")
 
 MAX_NODES, MAX_TREES = 64, 256
 KV_FULL, KV_SHARED, KV_FIRST_THEN_SHARED = 0, 1, 2
-CDB_DEV_NO_PAGES = 4
+CDB_DEV_NO_PAGES, CDB_DEV_BAD_VALUE = 4, 5
 
 
 class cdb_tree(C.Structure):
@@ -45,6 +45,12 @@ class cdb_accepted(C.Structure):
     _fields_ = [("path", C.c_void_p), ("count", C.c_void_p), ("next", C.c_void_p)]
 
 
+class cdb_sampling(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("draft_logits", C.c_void_p), ("logits_stride", C.c_int64),
+                ("draft_stride", C.c_int64), ("temperature", C.c_void_p), ("draft_temperature", C.c_void_p),
+                ("u_node", C.c_void_p), ("u_next", C.c_void_p)]
+
+
 _bound = False
 
 
@@ -62,6 +68,7 @@ def lib() -> C.CDLL:
         L.cdb_tree_step.argtypes = [P, P, P, P, P, P, P, P, S, P]
         L.cdb_tree_coda.argtypes = [P, P, P, P, P, P, P, P, S, P]
         L.cdb_tree_accept.argtypes = [P, P, P, I, P, P, P, S, P]
+        L.cdb_tree_sample.argtypes = [P, P, P, I, P, P, P, P, S, P]
         L.cdb_tree_commit.argtypes = [P, P, P, P, P, S, P]
         for f in EXPORTED[1:]:
             getattr(L, f).restype = C.c_int
@@ -181,6 +188,18 @@ def cdb_tree_accept(drafts: cdb_drafts, row0, next_ids, first_ids, out: cdb_acce
                                                     ws.data_ptr(), ws.numel(), _stream("cdb_tree_accept", stream, ws)))
 
 
+def cdb_tree_sample(desc: cdb_model_desc, drafts: cdb_drafts, row0, first_ids, sampling: cdb_sampling, out: cdb_accepted,
+                    ws, stream=None):
+    """row0, first_ids: device int32 [n_trees].  drafts: as for cdb_tree_accept."""
+    _trees_fit("cdb_tree_sample", drafts, out)
+    _trees_fit("cdb_tree_sample", drafts, sampling)
+    _need("cdb_tree_sample", getattr(sampling, "vocab", desc.vocab) == desc.vocab)
+    at, first = (_flat("cdb_tree_sample", t, torch.int32, drafts.n_trees) for t in (row0, first_ids))
+    _check("cdb_tree_sample", lib().cdb_tree_sample(C.byref(desc), C.byref(drafts), at, sampling.n_rows, first,
+                                                    C.byref(sampling), C.byref(out), ws.data_ptr(), ws.numel(),
+                                                    _stream("cdb_tree_sample", stream, ws)))
+
+
 def cdb_tree_commit(desc: cdb_model_desc, kv: cdb_kv, drafts: cdb_drafts, accepted: cdb_accepted, ws, stream=None):
     _trees_fit("cdb_tree_commit", drafts, accepted)
     _check("cdb_tree_commit", lib().cdb_tree_commit(C.byref(desc), C.byref(kv), C.byref(drafts), C.byref(accepted),
@@ -281,3 +300,28 @@ class Accepted:
         self.next = torch.zeros(n_trees, dtype=torch.int32, device=device)
         arrays = (self.path, self.count, self.next)
         self.c = _held(cdb_accepted(*(_ptr(t) for t in arrays)), *arrays, trees=n_trees, nodes=max_nodes)
+
+
+class Sampling:
+    """What sampled acceptance reads (cdb_sampling), fp32: logits and draft_logits [n_rows][vocab] with contiguous rows
+    (draft_logits None: a drafter that was sure), u_node [n_trees][max_nodes], u_next, temperature and draft_temperature
+    [n_trees] (temperatures None: 1)."""
+
+    def __init__(self, logits, u_node, u_next, draft_logits=None, temperature=None, draft_temperature=None):
+        f = torch.float32
+        _need("Sampling", u_node.dim() == 2 and logits.dim() == 2)
+        (T, N), (M, V) = u_node.shape, logits.shape
+        _tensor("Sampling", u_node, f, T, N), _tensor("Sampling", u_next, f, T)
+        for t in (temperature, draft_temperature):
+            _need("Sampling", t is None or _tensor("Sampling", t, f, T) is t)
+        for t in (logits, draft_logits):
+            _need("Sampling", t is None or (t.is_cuda and t.dtype is f and t.shape == (M, V) and
+                                            (M * V == 0 or t.stride(1) == 1)))
+        arrays = (logits, draft_logits, temperature, draft_temperature, u_node, u_next)
+        self.logits, self.draft_logits, self.temperature, self.draft_temperature, self.u_node, self.u_next = arrays
+
+        def stride(t):  # of one row any
+            return 0 if t is None else t.stride(0) if M > 1 else V
+
+        self.c = _held(cdb_sampling(_ptr(logits), _ptr(draft_logits), stride(logits), stride(draft_logits),
+                                    *(_ptr(t) for t in arrays[2:])), *arrays, trees=T, nodes=N, n_rows=M, vocab=V)
