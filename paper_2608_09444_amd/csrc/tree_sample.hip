@@ -11,8 +11,7 @@
 
 namespace cdb {
 
-constexpr int kPiece = 4096;  // logits of a workgroup's part of a row
-constexpr int kFinish = 1024; // threads that finish a tree
+constexpr int kPiece = 4096;  // logits of a workgroup's part of a row, 16 to each of its 256 threads
 
 struct SampleArgs {
     cdb_drafts dr;
@@ -22,11 +21,36 @@ struct SampleArgs {
     cdb_accepted out;
     int n_rows, V, pieces;
     double2* stats;  // [target, drafter][n_rows][pieces] maximum, sum of exp((l - maximum) / temperature)
+    double* rest;    // [trees][pieces] what the first rejection leaves of a piece
+    int* arrive;     // [trees] pieces of it that are summed, 0 between launches
     int* err;
 };
 
-static size_t sample_stats_bytes(int rows, int V) { return (size_t)2 * rows * ((V + kPiece - 1) / kPiece) * sizeof(double2); }
-size_t tree_sample_bytes(const cdb_model_desc& d, int rows) { return sample_stats_bytes(rows, d.vocab); }
+static int sample_pieces(const cdb_model_desc& d) { return (d.vocab + kPiece - 1) / kPiece; }
+size_t tree_sample_bytes(const cdb_model_desc& d, int rows) {
+    return ((size_t)2 * rows * sizeof(double2) + CDB_TREE_MAX_TREES * sizeof(double)) * sample_pieces(d) +
+           CDB_TREE_MAX_TREES * sizeof(int);
+}
+
+// 2^y for y <= 0 (or a little above): 2^n 2^f with f in [-1/2, 1/2], the latter by its Taylor
+// series, whose rest is below (ln 2 / 2)^11 / 11! = 2.2e-13.
+__device__ __forceinline__ double exp2_64(double y) {
+    y = fmax(y, -1100.0);
+    const double n = rint(y), f = y - n;
+    double p = 7.0549116208011209e-09;  // ln(2)^k / k!, k = 10 .. 0
+    p = fma(p, f, 1.0178086009239696e-07);
+    p = fma(p, f, 1.3215486790144305e-06);
+    p = fma(p, f, 1.5252733804059838e-05);
+    p = fma(p, f, 1.5403530393381606e-04);
+    p = fma(p, f, 1.3333558146428441e-03);
+    p = fma(p, f, 9.6181291076284769e-03);
+    p = fma(p, f, 5.5504108664821576e-02);
+    p = fma(p, f, 2.4022650695910069e-01);
+    p = fma(p, f, 6.9314718055994529e-01);
+    p = fma(p, f, 1.0);
+    return ldexp(p, (int)n);
+}
+constexpr double kLog2e = 1.4426950408889634;
 
 __device__ __forceinline__ bool tree_len_ok(int l) { return l >= 0 && l <= 0x7fffffff - CDB_TREE_MAX_NODES; }
 
@@ -66,6 +90,7 @@ __global__ __launch_bounds__(256) void k_sample_stats(SampleArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = logits4(src, piece * kPiece + i * 1024 + tid * 4, a.V);
     if (tid == 0) s_found = s_kids = 0;
+    if (piece + row + blockIdx.z == 0) a.arrive[tid] = 0;  // CDB_TREE_MAX_TREES = 256 of them
     __syncthreads();
     bool mine = false;
     int first = 0;
@@ -91,24 +116,27 @@ __global__ __launch_bounds__(256) void k_sample_stats(SampleArgs a) {
         if (!s_kids) return;
     }
     const float* temps = target ? a.sm.temperature : a.sm.draft_temperature;
-    const double inv = temps ? 1.0 / (double)temps[t] : 1.0;
+    const double scale = temps ? kLog2e / (double)temps[t] : kLog2e;
     float m = -INFINITY;
+    bool nan = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m = fmaxf(fmaxf(fmaxf(m, x[i].x), fmaxf(x[i].y, x[i].z)), x[i].w);
+    for (int i = 0; i < 4; ++i) {
+        m = fmaxf(fmaxf(fmaxf(m, x[i].x), fmaxf(x[i].y, x[i].z)), x[i].w);
+        nan |= x[i].x != x[i].x || x[i].y != x[i].y || x[i].z != x[i].z || x[i].w != x[i].w;
+    }
     m = wave_all(m, [](float p, float q) { return fmaxf(p, q); });
     if (lane == 0) s_max[w] = m;
     __syncthreads();
     m = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
-    double s = 0.0;
-    if (m > -INFINITY)
+    double s = nan || m == INFINITY ? NAN : 0.0;
+    if (m > -INFINITY) {
+        const double mc = -scale * m;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            s += exp(((double)x[i].x - m) * inv) + exp(((double)x[i].y - m) * inv);
-            s += exp(((double)x[i].z - m) * inv) + exp(((double)x[i].w - m) * inv);
+            s += exp2_64(fma((double)x[i].x, scale, mc)) + exp2_64(fma((double)x[i].y, scale, mc));
+            s += exp2_64(fma((double)x[i].z, scale, mc)) + exp2_64(fma((double)x[i].w, scale, mc));
         }
-    else  // nothing but -inf, or NaN
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s += x[i].x != x[i].x || x[i].y != x[i].y || x[i].z != x[i].z || x[i].w != x[i].w ? NAN : 0.0;
+    }
     s = wave_all(s, [](double p, double q) { return p + q; });
     if (lane == 0) s_sum[w] = s;
     __syncthreads();
@@ -116,101 +144,98 @@ __global__ __launch_bounds__(256) void k_sample_stats(SampleArgs a) {
         a.stats[((size_t)(target ? 0 : a.n_rows) + row) * a.pieces + piece] = make_double2(m, s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]);
 }
 
-// A row's maximum and 1 / sum; 1 / sum is NaN or infinite where the row is no distribution.
-struct RowStat {
-    double m, inv;
-};
-__device__ __forceinline__ RowStat row_stat(const double2* s, int pieces, double inv_t) {
-    double m = -INFINITY;
-    for (int i = 0; i < pieces; ++i) m = fmax(m, s[i].x);
-    double z = 0.0;
-    for (int i = 0; i < pieces; ++i) z += s[i].y * (s[i].x > -INFINITY ? exp((s[i].x - m) * inv_t) : 1.0);
-    return {m, m < INFINITY ? 1.0 / z : NAN};
-}
-
-// One workgroup per tree: wave 0 walks (lane = node), all sum what a rejection leaves.
-__global__ __launch_bounds__(kFinish) void k_sample_finish(SampleArgs a) {
-    constexpr int W = kFinish / 64, E = kFinish * 4;  // waves; logits a round
-    extern __shared__ double s_sum[];  // [rounds][W]
+// One workgroup per tree, or, for a drafter's probabilities, per (piece, tree).  Wave 0 walks (lane = node).  All
+// workgroups of a tree walk alike up to its first rejection; each then sums what that leaves of its own
+// piece, and the one that is through last has all sums and goes on alone.
+__global__ __launch_bounds__(256) void k_sample_walk(SampleArgs a) {
+    extern __shared__ double s_sum[];  // [pieces] what is left of the target's probabilities at the current node
+    __shared__ double s_m[2][CDB_TREE_MAX_NODES], s_inv[2][CDB_TREE_MAX_NODES];  // each node's maximum x scale, 1 / sum
     __shared__ double s_z[CDB_TREE_MAX_NODES + 1];  // 1 / Z_k after k rejections at the current node
-    __shared__ int s_out[CDB_TREE_MAX_NODES];        // their tokens
-    __shared__ int s_cur, s_k, s_end;
-    __shared__ double s_pm, s_pinv, s_qm, s_qinv, s_total;
-    const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    __shared__ double s_red[4];
+    __shared__ int s_out[CDB_TREE_MAX_NODES];  // the tokens of the rejections
+    __shared__ int s_par[CDB_TREE_MAX_NODES];
+    __shared__ int s_cur, s_k, s_todo, s_pick[4];
+    const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const bool dense = a.sm.draft_logits != nullptr;
-    const double inv_t = a.sm.temperature ? 1.0 / (double)a.sm.temperature[t] : 1.0;
-    const double inv_d = dense && a.sm.draft_temperature ? 1.0 / (double)a.sm.draft_temperature[t] : 1.0;
-    const int rounds = (a.V + E - 1) / E, r0 = a.row0[t];
-
-    // wave 0: the nodes
-    const size_t at = (size_t)t * a.dr.max_nodes + lane;
-    bool live = false;
-    int par = -2, token = 0, path = -1, count = 0, cur = -1, tried = -1, k = 0;
-    int next = 0;
-    double u = 0.0, pj = 0.0, qj = 1.0;
-    RowStat sp{0.0, 0.0}, sq{0.0, 0.0};
-    bool bad_p = false, bad_q = false;
-    if (w == 0) {
-        int n = a.dr.n_nodes[t];
-        next = a.first_ids[t];
-        if (n < 0 || n > a.dr.max_nodes) n = 0;
-        if (n > 0) {
-            bool refused = false;
-            if (a.dr.seq) {
-                const int s = a.dr.seq[t];
-                for (int i = lane; i < t; i += 64) refused |= a.dr.seq[i] == s;
-                refused |= s < 0 || s >= a.dr.max_seqs;
-                if (a.dr.len && !__any(refused)) refused = !tree_len_ok(a.dr.len[s]);
-            }
-            if (__any(refused)) {
-                if (lane == 0) set_err(a.err, CDB_DEV_BAD_INDEX);
-                n = 0;
-            } else if ((a.sm.temperature && !temperature_ok(a.sm.temperature[t])) ||
-                       (dense && a.sm.draft_temperature && !temperature_ok(a.sm.draft_temperature[t]))) {
-                if (lane == 0) set_err(a.err, CDB_DEV_BAD_VALUE);
-                n = 0;
-            }
+    const float temp = a.sm.temperature ? a.sm.temperature[t] : 1.f;
+    const float dtemp = dense && a.sm.draft_temperature ? a.sm.draft_temperature[t] : 1.f;
+    const double scale[2] = {kLog2e / (double)temp, kLog2e / (double)dtemp};
+    const int r0 = a.row0[t], N = a.dr.max_nodes;
+    const bool tells = blockIdx.x == 0;
+    // the nodes, in every wave
+    int n = a.dr.n_nodes[t];
+    if (n < 0 || n > N) n = 0;
+    const size_t at = (size_t)t * N + lane;
+    int par = lane < n ? a.dr.parent[at] : -2;
+    const int token = lane < n ? a.dr.tokens[at] : 0;
+    const double u = lane < n ? a.sm.u_node[at] : 0.0;
+    int next = a.first_ids[t];
+    bool live = lane < n && r0 >= 0;
+    if (n > 0) {
+        bool refused = false;
+        if (a.dr.seq) {
+            const int s = a.dr.seq[t];
+            for (int i = lane; i < t; i += 64) refused |= a.dr.seq[i] == s;
+            refused |= s < 0 || s >= a.dr.max_seqs;
+            if (a.dr.len && !__any(refused)) refused = !tree_len_ok(a.dr.len[s]);
         }
-        live = lane < n && r0 >= 0;
-        if (live && r0 > a.n_rows - 1 - lane) {
-            set_err(a.err, CDB_DEV_BAD_INDEX);
+        refused = __any(refused);
+        const bool cold = !temperature_ok(temp) || !temperature_ok(dtemp);
+        if (refused || cold) {
+            if (tells && tid == 0) set_err(a.err, refused ? CDB_DEV_BAD_INDEX : CDB_DEV_BAD_VALUE);
             live = false;
-        }
-        if (live) {
-            par = a.dr.parent[at];
-            token = a.dr.tokens[at];
-            u = a.sm.u_node[at];
-        }
-        live = live && par < lane;
-        if (live && par >= 0 && (token < 0 || token >= a.V)) {
-            set_err(a.err, CDB_DEV_BAD_INDEX);
-            live = false;
-        }
-        bool kids = false;
-        for (int j = 1; j < a.dr.max_nodes; ++j) kids |= __shfl(live ? par : -2, j, 64) == lane;
-        if (live) {
-            sp = row_stat(a.stats + (size_t)(r0 + lane) * a.pieces, a.pieces, inv_t);
-            bad_p = !(sp.inv < INFINITY);
-            if (dense && kids) {
-                sq = row_stat(a.stats + (size_t)(a.n_rows + r0 + lane) * a.pieces, a.pieces, inv_d);
-                bad_q = !(sq.inv < INFINITY);
-            }
-        }
-        // this node's token after its parent
-        const int from = live && par >= 0 ? par : lane;
-        const double pm = __shfl(sp.m, from, 64), pi = __shfl(sp.inv, from, 64);
-        const double qm = __shfl(sq.m, from, 64), qi = __shfl(sq.inv, from, 64);
-        if (live && par >= 0) {
-            pj = exp(((double)a.sm.logits[(size_t)(r0 + par) * a.sm.logits_stride + token] - pm) * inv_t) * pi;
-            if (dense) qj = exp(((double)a.sm.draft_logits[(size_t)(r0 + par) * a.sm.draft_stride + token] - qm) * inv_d) * qi;
         }
     }
-    // what is left of the target's probability of token i at the current node after k rejections
-    auto left = [&](float lp, float lq, int i, int k) {
-        double r = exp(((double)lp - s_pm) * inv_t) * s_pinv;
+    if (live && r0 > a.n_rows - 1 - lane) {
+        if (tells && w == 0) set_err(a.err, CDB_DEV_BAD_INDEX);
+        live = false;
+    }
+    live = live && par < lane;
+    if (live && par >= 0 && (token < 0 || token >= a.V)) {
+        if (tells && w == 0) set_err(a.err, CDB_DEV_BAD_INDEX);
+        live = false;
+    }
+    if (!live) par = -2;
+    const uint64_t lives = __ballot(live);
+    if (w == 0) s_par[lane] = par;
+    __syncthreads();
+    // statistics of the nodes' rows: four threads to a node
+    {
+        const int node = tid >> 2, sub = tid & 3;
+        const bool here = lives >> node & 1;
+        bool kids = false;
+        if (here && dense)
+            for (int j = node + 1; j < n; ++j) kids |= s_par[j] == node;
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+            double m = -INFINITY, sum = 0.0;
+            if (here && (z == 0 || kids)) {
+                const double2* st = a.stats + ((size_t)(z ? a.n_rows : 0) + r0 + node) * a.pieces;
+#pragma unroll 4
+                for (int i = sub; i < a.pieces; i += 4) m = fmax(m, st[i].x);
+                m = fmax(m, __shfl_xor(m, 1, 64));
+                m = fmax(m, __shfl_xor(m, 2, 64));
+#pragma unroll 4
+                for (int i = sub; i < a.pieces; i += 4) {
+                    const double2 x = st[i];  // of a piece of nothing but -inf (or NaN): 0 (or NaN)
+                    sum += x.x > -INFINITY ? x.y * exp2_64((x.x - m) * scale[z]) : x.y;
+                }
+                sum += __shfl_xor(sum, 1, 64);
+                sum += __shfl_xor(sum, 2, 64);
+            }
+            if (sub == 0) {
+                s_m[z][node] = m * scale[z];
+                s_inv[z][node] = m < INFINITY ? 1.0 / sum : NAN;  // NaN or infinite: no distribution
+            }
+        }
+    }
+    __syncthreads();
+    // what is left of the target's probability of token i after k rejections at the current node
+    auto left = [&](float lp, float lq, int i, int cur, int k) {
+        double r = exp2_64(fma((double)lp, scale[0], -s_m[0][cur])) * s_inv[0][cur];
         if (dense) {
             if (k) {
-                const double q = exp(((double)lq - s_qm) * inv_d) * s_qinv;
+                const double q = exp2_64(fma((double)lq, scale[1], -s_m[1][cur])) * s_inv[1][cur];
                 for (int s = 1; s < k; ++s) r = fmax(r - q, 0.0) * s_z[s];
                 r = fmax(r - q, 0.0);
             }
@@ -219,19 +244,56 @@ __global__ __launch_bounds__(kFinish) void k_sample_finish(SampleArgs a) {
         }
         return r;
     };
+    auto target_row = [&](int cur) { return a.sm.logits + (size_t)(r0 + cur) * a.sm.logits_stride; };
+    auto draft_row = [&](int cur) { return a.sm.draft_logits + (size_t)(r0 + cur) * a.sm.draft_stride; };
+    // a piece's sum, in s_red[0] for all; by the whole workgroup
+    auto piece_sum = [&](int piece, int cur, int k) {
+        double s = 0.0;
+        float4 x[4], y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = piece * kPiece + i * 1024 + tid * 4;
+            x[i] = logits4(target_row(cur), e, a.V);
+            y[i] = dense && k ? logits4(draft_row(cur), e, a.V) : x[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = piece * kPiece + i * 1024 + tid * 4;
+            s += left(x[i].x, y[i].x, e, cur, k) + left(x[i].y, y[i].y, e + 1, cur, k);
+            s += left(x[i].z, y[i].z, e + 2, cur, k) + left(x[i].w, y[i].w, e + 3, cur, k);
+        }
+        s = wave_all(s, [](double p, double q) { return p + q; });
+        __syncthreads();
+        if (lane == 0) s_red[w] = s;
+        __syncthreads();
+        return s_red[0] + s_red[1] + s_red[2] + s_red[3];
+    };
+
+    // this node's token after its parent (wave 0)
+    double pj = 0.0, qj = 1.0;
+    bool bad = false;
+    if (w == 0) {
+        if (live && par >= 0) {
+            const float lp = target_row(par)[token], lq = dense ? draft_row(par)[token] : 0.f;
+            pj = exp2_64(fma((double)lp, scale[0], -s_m[0][par])) * s_inv[0][par];
+            if (dense) qj = exp2_64(fma((double)lq, scale[1], -s_m[1][par])) * s_inv[1][par];
+        }
+    }
+    int path = -1, count = 0, cur = -1, tried = -1, k = 0;
+    bool alone = !dense;
     for (;;) {
-        // 0: walk on; the walk needs sums (1: after a rejection, 2: at the end) or is over (3)
+        // the walk needs sums after a rejection (1), or a token (2), or is over (3)
         if (w == 0) {
             int todo = 0;
             while (!todo) {
-                const uint64_t kids = __ballot(live && par == cur && lane > tried);
+                const uint64_t kids = __ballot(par == cur && lane > tried && live);
+                if (cur >= 0 && (!(s_inv[0][cur] < INFINITY) || (dense && kids && !(s_inv[1][cur] < INFINITY)))) {
+                    bad = true;
+                    todo = 3;
+                    break;
+                }
                 if (!kids) {
                     todo = cur < 0 ? 3 : 2;
-                    if (todo == 2 && __shfl(bad_p, cur, 64)) {
-                        if (lane == 0) set_err(a.err, CDB_DEV_BAD_VALUE);
-                        next = -1;
-                        todo = 3;
-                    }
                     break;
                 }
                 const int j = __ffsll((unsigned long long)kids) - 1;
@@ -240,19 +302,12 @@ __global__ __launch_bounds__(kFinish) void k_sample_finish(SampleArgs a) {
                 if (cur < 0) {
                     yes = __shfl(token, j, 64) == next;
                 } else {
-                    if (__shfl(bad_p || bad_q, cur, 64)) {
-                        if (lane == 0) set_err(a.err, CDB_DEV_BAD_VALUE);
-                        next = -1;
-                        todo = 3;
-                        break;
-                    }
                     double r = pj;
                     if (dense) {
                         for (int s = 1; s <= k; ++s) r = fmax(r - qj, 0.0) * s_z[s];
                     } else {
-                        bool out = false;
-                        for (int s = 0; s < k; ++s) out |= s_out[s] == token;
-                        r = out ? 0.0 : k ? r * s_z[k] : r;
+                        for (int s = 0; s < k; ++s) r = s_out[s] == token ? 0.0 : r;
+                        if (k) r *= s_z[k];
                     }
                     yes = __shfl((int)(u * qj < r), j, 64);
                 }
@@ -268,109 +323,155 @@ __global__ __launch_bounds__(kFinish) void k_sample_finish(SampleArgs a) {
                     todo = 1;
                 }
             }
-            const int from = cur < 0 ? 0 : cur;
-            const double v0 = __shfl(sp.m, from, 64), v1 = __shfl(sp.inv, from, 64), v2 = __shfl(sq.m, from, 64), v3 = __shfl(sq.inv, from, 64);
             if (lane == 0) {
                 s_cur = cur;
                 s_k = k;
-                s_end = todo;
-                s_pm = v0, s_pinv = v1, s_qm = v2, s_qinv = v3;
+                s_todo = todo;
             }
         }
         __syncthreads();
-        const int todo = s_end;
+        const int todo = s_todo, c = s_cur;
         int kk = s_k;
+        if (todo != 1 && !alone) {  // no rejection so far: every workgroup of the tree knows the same
+            if (!tells) return;
+            alone = true;
+        }
         if (todo == 3) break;
-        const float* lp = a.sm.logits + (size_t)(r0 + s_cur) * a.sm.logits_stride;
-        const float* lq = a.sm.draft_logits + (size_t)(r0 + s_cur) * a.sm.draft_stride;
-        for (bool again = todo == 1 || kk == 0; again;) {
-            for (int i = 0; i < rounds; ++i) {
-                const int e = i * E + tid * 4;
-                const float4 x = logits4(lp, e, a.V), y = dense && kk ? logits4(lq, e, a.V) : x;
-                double s = left(x.x, y.x, e, kk) + left(x.y, y.y, e + 1, kk);
-                s += left(x.z, y.z, e + 2, kk) + left(x.w, y.w, e + 3, kk);
-                s = wave_all(s, [](double p, double q) { return p + q; });
-                if (lane == 0) s_sum[i * W + w] = s;
+        // sums at a node that nothing was rejected at, from the statistics
+        auto fresh = [&]() {
+            for (int i = tid; i < a.pieces; i += 256) {
+                const double2 x = a.stats[(size_t)(r0 + c) * a.pieces + i];
+                s_sum[i] = x.x > -INFINITY ? x.y * exp2_64(fma(x.x, scale[0], -s_m[0][c])) * s_inv[0][c] : 0.0;
             }
             __syncthreads();
-            if (w == 0) {
-                double z = 0.0;
-                for (int i = lane; i < rounds * W; i += 64) z += s_sum[i];
-                z = wave_all(z, [](double p, double q) { return p + q; });
-                if (lane == 0) {
-                    s_total = z;
-                    s_z[kk] = 1.0 / z;
-                }
+        };
+        auto total = [&]() {  // every thread's own, in order
+            double z = 0.0;
+            for (int i = 0; i < a.pieces; ++i) z += s_sum[i];
+            return z;
+        };
+        if (todo == 2) {
+            if (kk == 0) fresh();
+            break;
+        }
+        double z;
+        if (dense && !alone) {
+            const double own = piece_sum(blockIdx.x, c, kk);
+            if (tid == 0) {
+                __hip_atomic_store(a.rest + (size_t)t * a.pieces + blockIdx.x, own, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                s_pick[0] = __hip_atomic_fetch_add(a.arrive + t, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
             }
             __syncthreads();
-            // nothing is left: the rejection does not count, what was there before is summed again
-            again = kk > 0 && !(s_total > 0.0);
-            if (again) --kk;
+            if (s_pick[0] != a.pieces - 1) return;
+            alone = true;
+            for (int i = tid; i < a.pieces; i += 256)
+                s_sum[i] = __hip_atomic_load(a.rest + (size_t)t * a.pieces + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __syncthreads();
+        } else if (dense) {
+            for (int i = 0; i < a.pieces; ++i) {
+                const double own = piece_sum(i, c, kk);
+                if (tid == 0) s_sum[i] = own;
+            }
+            __syncthreads();
+        } else {  // a piece without the rejected token
+            if (kk == 1) fresh();
+            const int i = s_out[kk - 1] / kPiece;
+            const double own = piece_sum(i, c, kk);
+            if (tid == 0) s_sum[i] = own;
+            __syncthreads();
         }
-        if (w == 0) {
-            k = kk;
-            if (lane == 0) s_k = kk;
-        }
+        z = total();
         __syncthreads();
-        if (todo == 2) break;
-    }
-    if (w != 0) return;
-    if (s_end == 2) {
-        // the first 256 logits whose cumulated sum passes u, then the first logit
-        const double aim = (double)a.sm.u_next[t] * s_total;
-        double before = 0.0, start = 0.0;
-        int seg = -1, some = 0;
-        double some_start = 0.0;
-        for (int i = 0; i < rounds * W && seg < 0; i += 64) {
-            const double own = i + lane < rounds * W ? s_sum[i + lane] : 0.0;
-            double v = own;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const double x = __shfl_up(v, o, 64);
-                if (lane >= o) v += x;
+        if (!(z > 0.0)) {  // nothing is left: the rejection does not count
+            --kk;
+            if (kk == 0) {
+                fresh();
+            } else if (dense) {
+                for (int i = 0; i < a.pieces; ++i) {
+                    const double own = piece_sum(i, c, kk);
+                    if (tid == 0) s_sum[i] = own;
+                }
+                __syncthreads();
+            } else {
+                const int i = s_out[kk] / kPiece;
+                const double own = piece_sum(i, c, kk);
+                if (tid == 0) s_sum[i] = own;
+                __syncthreads();
             }
-            const uint64_t hit = __ballot(before + v > aim && own > 0.0), has = __ballot(own > 0.0);
-            if (hit) {
-                const int j = __ffsll((unsigned long long)hit) - 1;
-                seg = i + j;
-                start = before + __shfl(v - own, j, 64);
-            }
-            if (has) {
-                const int j = 63 - __clzll((long long)has);
-                some = i + j;
-                some_start = before + __shfl(v - own, j, 64);
-            }
-            before += __shfl(v, 63, 64);
+        } else if (tid == 0) {
+            s_z[kk] = 1.0 / z;
         }
-        if (seg < 0) seg = some, start = some_start;  // u is 1 to rounding: the last logit with a probability
-        const float* lp = a.sm.logits + (size_t)(r0 + s_cur) * a.sm.logits_stride;
-        const float* lq = a.sm.draft_logits + (size_t)(r0 + s_cur) * a.sm.draft_stride;
-        const int e = seg * 256 + lane * 4;
-        const float4 x = logits4(lp, e, a.V), y = dense && s_k ? logits4(lq, e, a.V) : x;
-        const double r[4] = {left(x.x, y.x, e, s_k), left(x.y, y.y, e + 1, s_k), left(x.z, y.z, e + 2, s_k),
-                             left(x.w, y.w, e + 3, s_k)};
-        const double own = r[0] + r[1] + r[2] + r[3];
+        k = kk;
+        if (tid == 0) s_k = kk;
+        __syncthreads();
+    }
+    if (s_todo == 2) {
+        // the piece in which the cumulated sum passes u_next, then the logit
+        const int c = s_cur, kk = s_k;
+        double aim = 0.0;
+        for (int i = 0; i < a.pieces; ++i) aim += s_sum[i];
+        aim *= (double)a.sm.u_next[t];
+        double before = 0.0, start = 0.0;
+        int piece = -1;
+        for (int i = 0; i < a.pieces; ++i) {
+            const double own = s_sum[i];
+            if (own > 0.0) {
+                piece = i;
+                start = before;
+                if (before + own > aim) break;
+            }
+            before += own;
+        }  // none (u_next is 1 to rounding): the last one with anything
+        piece = piece < 0 ? 0 : piece;
+        const int e = piece * kPiece + tid * 16;
+        double r[16], own = 0.0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 x = logits4(target_row(c), e + i * 4, a.V), y = dense && kk ? logits4(draft_row(c), e + i * 4, a.V) : x;
+            r[i * 4] = left(x.x, y.x, e + i * 4, c, kk);
+            r[i * 4 + 1] = left(x.y, y.y, e + i * 4 + 1, c, kk);
+            r[i * 4 + 2] = left(x.z, y.z, e + i * 4 + 2, c, kk);
+            r[i * 4 + 3] = left(x.w, y.w, e + i * 4 + 3, c, kk);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) own += r[i];
         double v = own;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
-            const double z = __shfl_up(v, o, 64);
-            if (lane >= o) v += z;
+            const double x = __shfl_up(v, o, 64);
+            if (lane >= o) v += x;
         }
-        double c = start + (v - own);
-        int pick = -1, last = -1;
+        if (lane == 63) s_red[w] = v;
+        __syncthreads();
+        double run = start;
+        for (int i = 0; i < w; ++i) run += s_red[i];
+        run += v - own;
+        int pick = 0x7fffffff, last = -1;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            c += r[i];
-            if (r[i] > 0.0) last = e + i;
-            if (pick < 0 && r[i] > 0.0 && c > aim) pick = e + i;
+        for (int i = 0; i < 16; ++i) {
+            run += r[i];
+            if (r[i] > 0.0) {
+                last = e + i;
+                if (run > aim && pick == 0x7fffffff) pick = e + i;
+            }
         }
-        const uint64_t hit = __ballot(pick >= 0), has = __ballot(last >= 0);
-        if (hit)
-            next = __shfl(pick, __ffsll((unsigned long long)hit) - 1, 64);
-        else
-            next = has ? __shfl(last, 63 - __clzll((long long)has), 64) : 0;
+        pick = wave_all(pick, [](int p, int q) { return min(p, q); });
+        last = wave_all(last, [](int p, int q) { return max(p, q); });
+        if (lane == 0) s_pick[w] = pick;
+        __syncthreads();
+        pick = min(min(s_pick[0], s_pick[1]), min(s_pick[2], s_pick[3]));
+        __syncthreads();
+        if (lane == 0) s_pick[w] = last;
+        __syncthreads();
+        last = max(max(s_pick[0], s_pick[1]), max(s_pick[2], s_pick[3]));
+        next = pick != 0x7fffffff ? pick : last < 0 ? 0 : last;
     }
-    if (lane < a.dr.max_nodes) a.out.path[at] = path;
+    if (w != 0) return;
+    if (bad) {
+        if (lane == 0) set_err(a.err, CDB_DEV_BAD_VALUE);
+        next = -1;
+    }
+    if (lane < N) a.out.path[at] = path;
     if (lane == 0) {
         a.out.count[t] = count;
         a.out.next[t] = next;
@@ -389,12 +490,14 @@ hipError_t launch_tree_sample(const cdb_model_desc& md, const cdb_drafts& d, con
     a.out = out;
     a.n_rows = n_rows;
     a.V = md.vocab;
-    a.pieces = (md.vocab + kPiece - 1) / kPiece;
+    a.pieces = sample_pieces(md);
     a.stats = static_cast<double2*>(scratch);
+    a.rest = reinterpret_cast<double*>(a.stats + (size_t)2 * n_rows * a.pieces);
+    a.arrive = reinterpret_cast<int*>(a.rest + (size_t)CDB_TREE_MAX_TREES * a.pieces);
     a.err = err;
     if (n_rows > 0) k_sample_stats<<<dim3(a.pieces, n_rows, sm.draft_logits ? 2 : 1), 256, 0, st>>>(a);
-    const int rounds = (md.vocab + kFinish * 4 - 1) / (kFinish * 4);
-    k_sample_finish<<<d.n_trees, kFinish, (size_t)rounds * (kFinish / 64) * sizeof(double), st>>>(a);
+    const int split = sm.draft_logits ? a.pieces : 1;
+    k_sample_walk<<<dim3(split, d.n_trees), 256, a.pieces * sizeof(double), st>>>(a);
     return hipGetLastError();
 }
 

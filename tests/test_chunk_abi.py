@@ -44,7 +44,7 @@ def test_workspace_serves_every_smaller_call(shape):
     # a tree workspace holds what sampled acceptance needs
     pieces = (shape.vocab + 4095) // 4096
     for rows in (1, 256):
-        assert tree.cdb_tree_workspace_bytes(desc, rows, 1) >= 256 + 2 * rows * pieces * 16
+        assert tree.cdb_tree_workspace_bytes(desc, rows, 1) >= 256 + (2 * rows * 16 + 256 * 8) * pieces + 256 * 4
 
 
 def _chunks(**kw):
@@ -118,7 +118,7 @@ def test_tree_sample_refusals():
         assert _sample(**kw) == INVALID, kw
     assert _sample(desc=BAD_DESC) == UNSUPPORTED
     assert _sample(desc=cdb.make_desc(cdbgen.shrink(cdbgen.TINY, vocab=(1 << 20) + 32))) == UNSUPPORTED
-    for kw in ({"n_rows": 257}, {"nb": 256 + 2 * 8 * 16 - 1}, {"n_trees": 257}):
+    for kw in ({"n_rows": 257}, {"nb": 256 + 2 * 8 * 16 + 256 * 8 + 256 * 4 - 1}, {"n_trees": 257}):
         assert _sample(**kw) == CAPACITY, kw
     assert _sample(n_trees=0, row0=None, first=None) == cdb.CDB_OK
 
