@@ -12,6 +12,8 @@
 namespace cdb {
 
 constexpr int kPiece = 4096;  // logits of a workgroup's part of a row, 16 to each of its 256 threads
+constexpr int kRounds = 2;    // most launches of k_sample_walk
+constexpr int kTrees = CDB_TREE_MAX_TREES;
 
 struct SampleArgs {
     cdb_drafts dr;
@@ -21,16 +23,22 @@ struct SampleArgs {
     cdb_accepted out;
     int n_rows, V, pieces;
     double2* stats;  // [target, drafter][n_rows][pieces] maximum, sum of exp((l - maximum) / temperature)
-    double* rest;    // [trees][pieces] what the first rejection leaves of a piece
-    int* arrive;     // [trees] pieces of it that are summed, 0 between launches
+    double* rest;    // [trees][pieces] what a rejection leaves of a piece
+    double* left;    // [kRounds][trees] and of all pieces
+    int* arrive;     // [kRounds][trees] pieces that are summed
+    int* done;       // [trees] whether the walk is over
+    int round, rounds;
     int* err;
 };
 
 static int sample_pieces(const cdb_model_desc& d) { return (d.vocab + kPiece - 1) / kPiece; }
 size_t tree_sample_bytes(const cdb_model_desc& d, int rows) {
-    return ((size_t)2 * rows * sizeof(double2) + CDB_TREE_MAX_TREES * sizeof(double)) * sample_pieces(d) +
-           CDB_TREE_MAX_TREES * sizeof(int);
+    const size_t doubles = ((size_t)4 * rows + kTrees) * sample_pieces(d) + kTrees * kRounds;
+    return doubles * 8 + (size_t)kTrees * (kRounds + 1) * 4;
 }
+
+// By its bits: a ballot of x < INFINITY was compiled to one that a NaN passes.
+__device__ __forceinline__ bool is_finite(double x) { return (__double2hiint(x) & 0x7ff00000) != 0x7ff00000; }
 
 // 2^y for y <= 0 (or a little above): 2^n 2^f with f in [-1/2, 1/2], the latter by its Taylor
 // series, whose rest is below (ln 2 / 2)^11 / 11! = 2.2e-13.
@@ -90,7 +98,8 @@ __global__ __launch_bounds__(256) void k_sample_stats(SampleArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = logits4(src, piece * kPiece + i * 1024 + tid * 4, a.V);
     if (tid == 0) s_found = s_kids = 0;
-    if (piece + row + blockIdx.z == 0) a.arrive[tid] = 0;  // CDB_TREE_MAX_TREES = 256 of them
+    if (piece + row + blockIdx.z == 0)  // for the launches of k_sample_walk
+        for (int i = tid; i < kTrees * (kRounds + 1); i += 256) a.arrive[i] = 0;
     __syncthreads();
     bool mine = false;
     int first = 0;
@@ -144,47 +153,49 @@ __global__ __launch_bounds__(256) void k_sample_stats(SampleArgs a) {
         a.stats[((size_t)(target ? 0 : a.n_rows) + row) * a.pieces + piece] = make_double2(m, s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]);
 }
 
-// One workgroup per tree, or, for a drafter's probabilities, per (piece, tree).  Wave 0 walks (lane = node).  All
-// workgroups of a tree walk alike up to its first rejection; each then sums what that leaves of its own
-// piece, and the one that is through last has all sums and goes on alone.
-__global__ __launch_bounds__(256) void k_sample_walk(SampleArgs a) {
+// One workgroup per tree, or, for a drafter's probabilities, per (piece, tree).  Wave 0 walks (lane = node), up to
+// the first rejection whose sum is not known yet, the round-th one; each workgroup then sums what that leaves of its
+// own piece, and the one that is through last has all sums and walks on alone.  Where that meets
+// another rejection, it leaves it to the next round, or, in the last one, sums by itself.
+__global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
     extern __shared__ double s_sum[];  // [pieces] what is left of the target's probabilities at the current node
+    double* s_part = s_sum + a.pieces; // [pieces][4] the waves' parts
     __shared__ double s_m[2][CDB_TREE_MAX_NODES], s_inv[2][CDB_TREE_MAX_NODES];  // each node's maximum x scale, 1 / sum
     __shared__ double s_z[CDB_TREE_MAX_NODES + 1];  // 1 / Z_k after k rejections at the current node
     __shared__ double s_red[4];
     __shared__ int s_out[CDB_TREE_MAX_NODES];  // the tokens of the rejections
     __shared__ int s_par[CDB_TREE_MAX_NODES];
-    __shared__ int s_cur, s_k, s_todo, s_pick[4];
+    __shared__ int s_cur, s_k, s_todo, s_pick[8];
     const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const bool dense = a.sm.draft_logits != nullptr;
+    const bool dense = a.sm.draft_logits != nullptr, tells = blockIdx.x == 0;
+    const int N = a.dr.max_nodes;
+    const size_t at = (size_t)t * N + lane;
+    // all that does not depend on another load
+    const int done = a.round > 0 ? a.done[t] : 0;
+    const int r0 = a.row0[t];
+    int n = a.dr.n_nodes[t], next = a.first_ids[t];
     const float temp = a.sm.temperature ? a.sm.temperature[t] : 1.f;
     const float dtemp = dense && a.sm.draft_temperature ? a.sm.draft_temperature[t] : 1.f;
+    const float un = a.sm.u_next[t];
+    int par = lane < N ? a.dr.parent[at] : -2, token = lane < N ? a.dr.tokens[at] : 0;
+    const double u = lane < N ? a.sm.u_node[at] : 0.f;
+    bool refused = false;
+    if (a.dr.seq) {
+        const int sq = a.dr.seq[t];
+        for (int i = lane; i < t; i += 64) refused |= a.dr.seq[i] == sq;
+        refused |= sq < 0 || sq >= a.dr.max_seqs;
+        if (a.dr.len && !__any(refused)) refused = !tree_len_ok(a.dr.len[sq]);
+    }
+    if (done) return;
+    refused = __any(refused);
     const double scale[2] = {kLog2e / (double)temp, kLog2e / (double)dtemp};
-    const int r0 = a.row0[t], N = a.dr.max_nodes;
-    const bool tells = blockIdx.x == 0;
-    // the nodes, in every wave
-    int n = a.dr.n_nodes[t];
+    auto target_row = [&](int node) { return a.sm.logits + (size_t)(r0 + node) * a.sm.logits_stride; };
+    auto draft_row = [&](int node) { return a.sm.draft_logits + (size_t)(r0 + node) * a.sm.draft_stride; };
     if (n < 0 || n > N) n = 0;
-    const size_t at = (size_t)t * N + lane;
-    int par = lane < n ? a.dr.parent[at] : -2;
-    const int token = lane < n ? a.dr.tokens[at] : 0;
-    const double u = lane < n ? a.sm.u_node[at] : 0.0;
-    int next = a.first_ids[t];
     bool live = lane < n && r0 >= 0;
-    if (n > 0) {
-        bool refused = false;
-        if (a.dr.seq) {
-            const int s = a.dr.seq[t];
-            for (int i = lane; i < t; i += 64) refused |= a.dr.seq[i] == s;
-            refused |= s < 0 || s >= a.dr.max_seqs;
-            if (a.dr.len && !__any(refused)) refused = !tree_len_ok(a.dr.len[s]);
-        }
-        refused = __any(refused);
-        const bool cold = !temperature_ok(temp) || !temperature_ok(dtemp);
-        if (refused || cold) {
-            if (tells && tid == 0) set_err(a.err, refused ? CDB_DEV_BAD_INDEX : CDB_DEV_BAD_VALUE);
-            live = false;
-        }
+    if (n > 0 && (refused || !temperature_ok(temp) || !temperature_ok(dtemp))) {
+        if (tells && tid == 0) set_err(a.err, refused ? CDB_DEV_BAD_INDEX : CDB_DEV_BAD_VALUE);
+        live = false;
     }
     if (live && r0 > a.n_rows - 1 - lane) {
         if (tells && w == 0) set_err(a.err, CDB_DEV_BAD_INDEX);
@@ -196,98 +207,108 @@ __global__ __launch_bounds__(256) void k_sample_walk(SampleArgs a) {
         live = false;
     }
     if (!live) par = -2;
+    float lp = 0.f, lq = 0.f;  // this node's token after its parent
+    if (w == 0 && par >= 0) {
+        lp = target_row(par)[token];
+        if (dense) lq = draft_row(par)[token];
+    }
     const uint64_t lives = __ballot(live);
     if (w == 0) s_par[lane] = par;
     __syncthreads();
-    // statistics of the nodes' rows: four threads to a node
-    {
+    {  // statistics of the nodes' rows: four threads to a node
         const int node = tid >> 2, sub = tid & 3;
         const bool here = lives >> node & 1;
         bool kids = false;
         if (here && dense)
-            for (int j = node + 1; j < n; ++j) kids |= s_par[j] == node;
+            for (int j = node + 1 + sub; j < n; j += 4) kids |= s_par[j] == node;
+        kids = (int)kids | __shfl_xor((int)kids, 1, 64);
+        kids = (int)kids | __shfl_xor((int)kids, 2, 64);
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
             double m = -INFINITY, sum = 0.0;
             if (here && (z == 0 || kids)) {
                 const double2* st = a.stats + ((size_t)(z ? a.n_rows : 0) + r0 + node) * a.pieces;
-#pragma unroll 4
-                for (int i = sub; i < a.pieces; i += 4) m = fmax(m, st[i].x);
-                m = fmax(m, __shfl_xor(m, 1, 64));
-                m = fmax(m, __shfl_xor(m, 2, 64));
-#pragma unroll 4
-                for (int i = sub; i < a.pieces; i += 4) {
-                    const double2 x = st[i];  // of a piece of nothing but -inf (or NaN): 0 (or NaN)
-                    sum += x.x > -INFINITY ? x.y * exp2_64((x.x - m) * scale[z]) : x.y;
+                for (int i0 = 0; i0 < a.pieces; i0 += 16) {
+                    double2 x[4];
+                    double top = m;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int piece = i0 + i * 4 + sub;
+                        x[i] = piece < a.pieces ? st[piece] : make_double2(-INFINITY, 0.0);
+                        top = fmax(top, x[i].x);
+                    }
+                    // a piece of nothing but -inf has the sum 0, one with NaN the sum NaN
+                    if (m > -INFINITY) sum *= exp2_64((m - top) * scale[z]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const double e = exp2_64((x[i].x - top) * scale[z]);
+                        sum += x[i].x > -INFINITY ? x[i].y * e : x[i].y;
+                    }
+                    m = top;
                 }
-                sum += __shfl_xor(sum, 1, 64);
-                sum += __shfl_xor(sum, 2, 64);
             }
+            double top = fmax(m, __shfl_xor(m, 1, 64));
+            top = fmax(top, __shfl_xor(top, 2, 64));
+            if (m > -INFINITY) sum *= exp2_64((m - top) * scale[z]);
+            sum += __shfl_xor(sum, 1, 64);
+            sum += __shfl_xor(sum, 2, 64);
             if (sub == 0) {
-                s_m[z][node] = m * scale[z];
-                s_inv[z][node] = m < INFINITY ? 1.0 / sum : NAN;  // NaN or infinite: no distribution
+                s_m[z][node] = top * scale[z];
+                s_inv[z][node] = top < INFINITY ? 1.0 / sum : NAN;  // NaN or infinite: no distribution
             }
         }
     }
     __syncthreads();
-    // what is left of the target's probability of token i after k rejections at the current node
-    auto left = [&](float lp, float lq, int i, int cur, int k) {
-        double r = exp2_64(fma((double)lp, scale[0], -s_m[0][cur])) * s_inv[0][cur];
-        if (dense) {
-            if (k) {
-                const double q = exp2_64(fma((double)lq, scale[1], -s_m[1][cur])) * s_inv[1][cur];
-                for (int s = 1; s < k; ++s) r = fmax(r - q, 0.0) * s_z[s];
-                r = fmax(r - q, 0.0);
-            }
-        } else {
-            for (int s = 0; s < k; ++s) r = i == s_out[s] ? 0.0 : r;
+    double pj = 0.0, qj = 1.0;
+    uint64_t good_p = 0, good_q = 0;
+    if (w == 0) {
+        const int from = max(par, 0);
+        pj = exp2_64(fma((double)lp, scale[0], -s_m[0][from])) * s_inv[0][from];
+        if (dense) qj = exp2_64(fma((double)lq, scale[1], -s_m[1][from])) * s_inv[1][from];
+        good_p = __ballot(is_finite(s_inv[0][lane]));
+        good_q = __ballot(!dense || is_finite(s_inv[1][lane]));
+    }
+
+    // What is left of the target's probabilities of tokens i .. i + 3 after k rejections at node cur.
+    auto left4 = [&](float4 x, float4 y, int i, int cur, int k, double (&r)[4]) {
+        const float p[4] = {x.x, x.y, x.z, x.w};
+        const double m = -s_m[0][cur], inv = s_inv[0][cur];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = exp2_64(fma((double)p[j], scale[0], m)) * inv;
+        if (dense && k) {
+            const float d[4] = {y.x, y.y, y.z, y.w};
+            const double mq = -s_m[1][cur], invq = s_inv[1][cur];
+            double q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] = exp2_64(fma((double)d[j], scale[1], mq)) * invq;
+            for (int s = 1; s < k; ++s)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[j] = fmax(r[j] - q[j], 0.0) * s_z[s];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[j] = fmax(r[j] - q[j], 0.0);
+        } else if (!dense) {
+            for (int s = 0; s < k; ++s)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[j] = i + j == s_out[s] ? 0.0 : r[j];
         }
-        return r;
     };
-    auto target_row = [&](int cur) { return a.sm.logits + (size_t)(r0 + cur) * a.sm.logits_stride; };
-    auto draft_row = [&](int cur) { return a.sm.draft_logits + (size_t)(r0 + cur) * a.sm.draft_stride; };
-    // a piece's sum, in s_red[0] for all; by the whole workgroup
-    auto piece_sum = [&](int piece, int cur, int k) {
-        double s = 0.0;
-        float4 x[4], y[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int e = piece * kPiece + i * 1024 + tid * 4;
-            x[i] = logits4(target_row(cur), e, a.V);
-            y[i] = dense && k ? logits4(draft_row(cur), e, a.V) : x[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int e = piece * kPiece + i * 1024 + tid * 4;
-            s += left(x[i].x, y[i].x, e, cur, k) + left(x[i].y, y[i].y, e + 1, cur, k);
-            s += left(x[i].z, y[i].z, e + 2, cur, k) + left(x[i].w, y[i].w, e + 3, cur, k);
-        }
-        s = wave_all(s, [](double p, double q) { return p + q; });
-        __syncthreads();
-        if (lane == 0) s_red[w] = s;
-        __syncthreads();
-        return s_red[0] + s_red[1] + s_red[2] + s_red[3];
+    auto add = [](double x, double y) { return x + y; };
+    // s_sum's total, the same bits in every wave
+    auto total = [&]() {
+        double z = 0.0;
+        for (int i = lane; i < a.pieces; i += 64) z += s_sum[i];
+        return wave_all(z, add);
     };
 
-    // this node's token after its parent (wave 0)
-    double pj = 0.0, qj = 1.0;
-    bool bad = false;
-    if (w == 0) {
-        if (live && par >= 0) {
-            const float lp = target_row(par)[token], lq = dense ? draft_row(par)[token] : 0.f;
-            pj = exp2_64(fma((double)lp, scale[0], -s_m[0][par])) * s_inv[0][par];
-            if (dense) qj = exp2_64(fma((double)lq, scale[1], -s_m[1][par])) * s_inv[1][par];
-        }
-    }
-    int path = -1, count = 0, cur = -1, tried = -1, k = 0;
-    bool alone = !dense;
+    int path = -1, count = 0, cur = -1, tried = -1, k = 0, rejected = 0;
+    bool bad = false, alone = !dense;
     for (;;) {
         // the walk needs sums after a rejection (1), or a token (2), or is over (3)
         if (w == 0) {
             int todo = 0;
             while (!todo) {
-                const uint64_t kids = __ballot(par == cur && lane > tried && live);
-                if (cur >= 0 && (!(s_inv[0][cur] < INFINITY) || (dense && kids && !(s_inv[1][cur] < INFINITY)))) {
+                const uint64_t kids = __ballot(par == cur && lane > tried);
+                if (cur >= 0 && (!(good_p >> cur & 1) || (kids && !(good_q >> cur & 1)))) {
                     bad = true;
                     todo = 3;
                     break;
@@ -298,9 +319,10 @@ __global__ __launch_bounds__(256) void k_sample_walk(SampleArgs a) {
                 }
                 const int j = __ffsll((unsigned long long)kids) - 1;
                 tried = j;
+                const int x = __builtin_amdgcn_readlane(token, j);
                 bool yes;
                 if (cur < 0) {
-                    yes = __shfl(token, j, 64) == next;
+                    yes = x == next;
                 } else {
                     double r = pj;
                     if (dense) {
@@ -309,7 +331,7 @@ __global__ __launch_bounds__(256) void k_sample_walk(SampleArgs a) {
                         for (int s = 0; s < k; ++s) r = s_out[s] == token ? 0.0 : r;
                         if (k) r *= s_z[k];
                     }
-                    yes = __shfl((int)(u * qj < r), j, 64);
+                    yes = __ballot(u * qj < r) >> j & 1;
                 }
                 if (yes) {
                     if (lane == count) path = j;
@@ -317,10 +339,18 @@ __global__ __launch_bounds__(256) void k_sample_walk(SampleArgs a) {
                     cur = j;
                     k = 0;
                 } else if (cur >= 0) {
-                    const int x = __shfl(token, j, 64);
                     if (lane == 0) s_out[k] = x;
                     ++k;
-                    todo = 1;
+                    if (rejected < a.round) {  // an earlier round's
+                        const double z = a.left[(size_t)rejected * kTrees + t];
+                        if (!(z > 0.0))
+                            --k;
+                        else if (lane == 0)
+                            s_z[k] = 1.0 / z;
+                    } else {
+                        todo = 1;
+                    }
+                    ++rejected;
                 }
             }
             if (lane == 0) {
@@ -332,109 +362,130 @@ __global__ __launch_bounds__(256) void k_sample_walk(SampleArgs a) {
         __syncthreads();
         const int todo = s_todo, c = s_cur;
         int kk = s_k;
-        if (todo != 1 && !alone) {  // no rejection so far: every workgroup of the tree knows the same
+        if (todo != 1 && !alone) {  // every workgroup of the tree came to the same
             if (!tells) return;
             alone = true;
         }
-        if (todo == 3) break;
-        // sums at a node that nothing was rejected at, from the statistics
-        auto fresh = [&]() {
-            for (int i = tid; i < a.pieces; i += 256) {
-                const double2 x = a.stats[(size_t)(r0 + c) * a.pieces + i];
-                s_sum[i] = x.x > -INFINITY ? x.y * exp2_64(fma(x.x, scale[0], -s_m[0][c])) * s_inv[0][c] : 0.0;
+        if (todo == 3 || (todo == 2 && kk > 0)) break;  // after rejections the sums are there
+        if (todo == 1 && dense && alone && a.round + 1 < a.rounds) return;  // the next round's
+        const bool shared = todo == 1 && !alone;
+        for (bool again = true; again;) {
+            int from = 0, to = 0;
+            if (todo == 1 && kk > 0) {
+                if (!dense)  // the piece of the token that is out (or in again) now
+                    from = s_out[s_k - 1] / kPiece, to = from + 1;
+                else if (shared && kk == s_k)
+                    from = blockIdx.x, to = from + 1;
+                else
+                    to = a.pieces;
             }
-            __syncthreads();
-        };
-        auto total = [&]() {  // every thread's own, in order
-            double z = 0.0;
-            for (int i = 0; i < a.pieces; ++i) z += s_sum[i];
-            return z;
-        };
-        if (todo == 2) {
-            if (kk == 0) fresh();
-            break;
-        }
-        double z;
-        if (dense && !alone) {
-            const double own = piece_sum(blockIdx.x, c, kk);
-            if (tid == 0) {
-                __hip_atomic_store(a.rest + (size_t)t * a.pieces + blockIdx.x, own, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                s_pick[0] = __hip_atomic_fetch_add(a.arrive + t, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-            }
-            __syncthreads();
-            if (s_pick[0] != a.pieces - 1) return;
-            alone = true;
-            for (int i = tid; i < a.pieces; i += 256)
-                s_sum[i] = __hip_atomic_load(a.rest + (size_t)t * a.pieces + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __syncthreads();
-        } else if (dense) {
-            for (int i = 0; i < a.pieces; ++i) {
-                const double own = piece_sum(i, c, kk);
-                if (tid == 0) s_sum[i] = own;
-            }
-            __syncthreads();
-        } else {  // a piece without the rejected token
-            if (kk == 1) fresh();
-            const int i = s_out[kk - 1] / kPiece;
-            const double own = piece_sum(i, c, kk);
-            if (tid == 0) s_sum[i] = own;
-            __syncthreads();
-        }
-        z = total();
-        __syncthreads();
-        if (!(z > 0.0)) {  // nothing is left: the rejection does not count
-            --kk;
-            if (kk == 0) {
-                fresh();
-            } else if (dense) {
-                for (int i = 0; i < a.pieces; ++i) {
-                    const double own = piece_sum(i, c, kk);
-                    if (tid == 0) s_sum[i] = own;
+            if (kk == 0 || (!dense && kk == 1 && kk == s_k)) {  // from the statistics
+                for (int i = tid; i < a.pieces; i += 256) {
+                    const double2 x = a.stats[(size_t)(r0 + c) * a.pieces + i];
+                    s_sum[i] = x.x > -INFINITY ? x.y * exp2_64(fma(x.x, scale[0], -s_m[0][c])) * s_inv[0][c] : 0.0;
                 }
                 __syncthreads();
-            } else {
-                const int i = s_out[kk] / kPiece;
-                const double own = piece_sum(i, c, kk);
-                if (tid == 0) s_sum[i] = own;
-                __syncthreads();
             }
-        } else if (tid == 0) {
-            s_z[kk] = 1.0 / z;
+            if (from < to) {
+                const float *tp = target_row(c), *tq = dense ? draft_row(c) : tp;
+                float4 p[4], q[4];  // the next four of 1024 logits each are on their way
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    p[i] = logits4(tp, from * kPiece + i * 1024 + tid * 4, a.V);
+                    q[i] = logits4(tq, from * kPiece + i * 1024 + tid * 4, a.V);
+                }
+                for (int piece = from; piece < to; ++piece) {
+                    double s = 0.0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = piece * kPiece + i * 1024 + tid * 4;
+                        const float4 x = p[i], y = q[i];
+                        if (piece + 1 < to) {
+                            p[i] = logits4(tp, e + kPiece, a.V);
+                            q[i] = logits4(tq, e + kPiece, a.V);
+                        }
+                        double r[4];
+                        left4(x, y, e, c, kk, r);
+                        s += (r[0] + r[1]) + (r[2] + r[3]);
+                    }
+                    s = wave_all(s, add);
+                    if (lane == 0) s_part[piece * 4 + w] = s;
+                }
+                __syncthreads();
+                for (int i = from + tid; i < to; i += 256)
+                    s_sum[i] = s_part[i * 4] + s_part[i * 4 + 1] + s_part[i * 4 + 2] + s_part[i * 4 + 3];
+                __syncthreads();
+                if (shared && kk == s_k) {
+                    if (tid == 0) {
+                        __hip_atomic_store(a.rest + (size_t)t * a.pieces + from, s_sum[from], __ATOMIC_RELAXED,
+                                           __HIP_MEMORY_SCOPE_AGENT);
+                        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the sum has reached memory
+                        s_pick[0] = __hip_atomic_fetch_add(a.arrive + a.round * kTrees + t, 1, __ATOMIC_RELAXED,
+                                                           __HIP_MEMORY_SCOPE_AGENT);
+                    }
+                    __syncthreads();
+                    if (s_pick[0] != a.pieces - 1) return;
+                    alone = true;
+                    for (int i = tid; i < a.pieces; i += 256)
+                        s_sum[i] = __hip_atomic_load(a.rest + (size_t)t * a.pieces + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __syncthreads();
+                }
+            }
+            again = false;
+            if (todo == 1 && kk == s_k) {
+                const double z = total();
+                if (tid == 0 && a.round + 1 < a.rounds) a.left[(size_t)a.round * kTrees + t] = z;
+                if (z > 0.0) {
+                    if (tid == 0) s_z[kk] = 1.0 / z;
+                } else {  // nothing is left: the rejection does not count, what was there before is summed again
+                    --kk;
+                    again = true;
+                    __syncthreads();
+                }
+            }
         }
+        if (todo == 2) break;
         k = kk;
-        if (tid == 0) s_k = kk;
         __syncthreads();
     }
     if (s_todo == 2) {
-        // the piece in which the cumulated sum passes u_next, then the logit
+        // the piece in which the cumulated sum passes u_next, then the logit; u_next may be 1 to rounding: the last
+        // one with anything
         const int c = s_cur, kk = s_k;
-        double aim = 0.0;
-        for (int i = 0; i < a.pieces; ++i) aim += s_sum[i];
-        aim *= (double)a.sm.u_next[t];
-        double before = 0.0, start = 0.0;
-        int piece = -1;
-        for (int i = 0; i < a.pieces; ++i) {
-            const double own = s_sum[i];
-            if (own > 0.0) {
-                piece = i;
-                start = before;
-                if (before + own > aim) break;
+        const double aim = (double)un * total();
+        double start = 0.0, before = 0.0;
+        int piece = 0;
+        for (int i0 = 0; i0 < a.pieces; i0 += 64) {
+            const double own = i0 + lane < a.pieces ? s_sum[i0 + lane] : 0.0;
+            double v = own;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const double x = __shfl_up(v, o, 64);
+                if (lane >= o) v += x;
             }
-            before += own;
-        }  // none (u_next is 1 to rounding): the last one with anything
-        piece = piece < 0 ? 0 : piece;
+            const uint64_t hit = __ballot(before + v > aim && own > 0.0), some = __ballot(own > 0.0);
+            if (some) {
+                const int j = hit ? __ffsll((unsigned long long)hit) - 1 : 63 - __clzll((long long)some);
+                piece = i0 + j;
+                start = before + __shfl(v - own, j, 64);
+                if (hit) break;
+            }
+            before += __shfl(v, 63, 64);
+        }
         const int e = piece * kPiece + tid * 16;
-        double r[16], own = 0.0;
+        const float *tp = target_row(c), *tq = dense ? draft_row(c) : tp;
+        float4 p[4], q[4];
+        double r[4][4], own = 0.0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float4 x = logits4(target_row(c), e + i * 4, a.V), y = dense && kk ? logits4(draft_row(c), e + i * 4, a.V) : x;
-            r[i * 4] = left(x.x, y.x, e + i * 4, c, kk);
-            r[i * 4 + 1] = left(x.y, y.y, e + i * 4 + 1, c, kk);
-            r[i * 4 + 2] = left(x.z, y.z, e + i * 4 + 2, c, kk);
-            r[i * 4 + 3] = left(x.w, y.w, e + i * 4 + 3, c, kk);
+            p[i] = logits4(tp, e + i * 4, a.V);
+            q[i] = logits4(tq, e + i * 4, a.V);
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) own += r[i];
+        for (int i = 0; i < 4; ++i) {
+            left4(p[i], q[i], e + i * 4, c, kk, r[i]);
+            own += (r[i][0] + r[i][1]) + (r[i][2] + r[i][3]);
+        }
         double v = own;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -449,22 +500,25 @@ __global__ __launch_bounds__(256) void k_sample_walk(SampleArgs a) {
         int pick = 0x7fffffff, last = -1;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            run += r[i];
-            if (r[i] > 0.0) {
+            const double x = r[i >> 2][i & 3];
+            run += x;
+            if (x > 0.0) {
                 last = e + i;
-                if (run > aim && pick == 0x7fffffff) pick = e + i;
+                if (run > aim) pick = min(pick, e + i);
             }
         }
-        pick = wave_all(pick, [](int p, int q) { return min(p, q); });
-        last = wave_all(last, [](int p, int q) { return max(p, q); });
-        if (lane == 0) s_pick[w] = pick;
+        // lanes and waves are in the tokens' order
+        const uint64_t hit = __ballot(pick != 0x7fffffff), some = __ballot(last >= 0);
+        if (hit) pick = __shfl(pick, __ffsll((unsigned long long)hit) - 1, 64);
+        if (some) last = __shfl(last, 63 - __clzll((long long)some), 64);
+        if (lane == 0) {
+            s_pick[w] = pick;
+            s_pick[4 + w] = last;
+        }
         __syncthreads();
         pick = min(min(s_pick[0], s_pick[1]), min(s_pick[2], s_pick[3]));
-        __syncthreads();
-        if (lane == 0) s_pick[w] = last;
-        __syncthreads();
-        last = max(max(s_pick[0], s_pick[1]), max(s_pick[2], s_pick[3]));
-        next = pick != 0x7fffffff ? pick : last < 0 ? 0 : last;
+        last = max(max(s_pick[4], s_pick[5]), max(s_pick[6], s_pick[7]));
+        next = pick != 0x7fffffff ? pick : max(last, 0);
     }
     if (w != 0) return;
     if (bad) {
@@ -475,6 +529,7 @@ __global__ __launch_bounds__(256) void k_sample_walk(SampleArgs a) {
     if (lane == 0) {
         a.out.count[t] = count;
         a.out.next[t] = next;
+        a.done[t] = 1;
     }
 }
 
@@ -493,11 +548,15 @@ hipError_t launch_tree_sample(const cdb_model_desc& md, const cdb_drafts& d, con
     a.pieces = sample_pieces(md);
     a.stats = static_cast<double2*>(scratch);
     a.rest = reinterpret_cast<double*>(a.stats + (size_t)2 * n_rows * a.pieces);
-    a.arrive = reinterpret_cast<int*>(a.rest + (size_t)CDB_TREE_MAX_TREES * a.pieces);
+    a.left = a.rest + (size_t)kTrees * a.pieces;
+    a.arrive = reinterpret_cast<int*>(a.left + kTrees * kRounds);
+    a.done = a.arrive + kTrees * kRounds;
     a.err = err;
+    a.rounds = sm.draft_logits && n_rows > 0 && d.max_nodes > 4 ? kRounds : 1;
     if (n_rows > 0) k_sample_stats<<<dim3(a.pieces, n_rows, sm.draft_logits ? 2 : 1), 256, 0, st>>>(a);
     const int split = sm.draft_logits ? a.pieces : 1;
-    k_sample_walk<<<dim3(split, d.n_trees), 256, a.pieces * sizeof(double), st>>>(a);
+    for (a.round = 0; a.round < a.rounds; ++a.round)
+        k_sample_walk<<<dim3(split, d.n_trees), 256, 5 * a.pieces * sizeof(double), st>>>(a);
     return hipGetLastError();
 }
 

@@ -42,9 +42,10 @@ def test_workspace_serves_every_smaller_call(shape):
         assert chunk.cdb_chunk_workspace_bytes(desc, rows, chunks) == 0
     assert chunk.cdb_chunk_workspace_bytes(BAD_DESC, 1, 1) == 0
     # a tree workspace holds what sampled acceptance needs
-    pieces = (shape.vocab + 4095) // 4096
-    for rows in (1, 256):
-        assert tree.cdb_tree_workspace_bytes(desc, rows, 1) >= 256 + (2 * rows * 16 + 256 * 8) * pieces + 256 * 4
+    for rows in (0, 1, 256):
+        nb = tree.cdb_tree_workspace_bytes(desc, rows, 1)
+        assert _sample(desc=desc, n_trees=0, n_rows=rows, ls=shape.vocab, ds=shape.vocab, nb=nb) == cdb.CDB_OK
+
 
 
 def _chunks(**kw):
@@ -118,7 +119,7 @@ def test_tree_sample_refusals():
         assert _sample(**kw) == INVALID, kw
     assert _sample(desc=BAD_DESC) == UNSUPPORTED
     assert _sample(desc=cdb.make_desc(cdbgen.shrink(cdbgen.TINY, vocab=(1 << 20) + 32))) == UNSUPPORTED
-    for kw in ({"n_rows": 257}, {"nb": 256 + 2 * 8 * 16 + 256 * 8 + 256 * 4 - 1}, {"n_trees": 257}):
+    for kw in ({"n_rows": 257}, {"nb": 255}, {"n_trees": 257}):
         assert _sample(**kw) == CAPACITY, kw
     assert _sample(n_trees=0, row0=None, first=None) == cdb.CDB_OK
 
