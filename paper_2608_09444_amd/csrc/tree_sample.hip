@@ -40,37 +40,28 @@ size_t tree_sample_bytes(const cdb_model_desc& d, int rows) {
 // By its bits: a ballot of x < INFINITY was compiled to one that a NaN passes.
 __device__ __forceinline__ bool is_finite(double x) { return (__double2hiint(x) & 0x7ff00000) != 0x7ff00000; }
 
-// 2^y for y <= 0 (or a little above): 2^n 2^f with f in [-1/2, 1/2], the latter by its Taylor
-// series, whose rest is below (ln 2 / 2)^11 / 11! = 2.2e-13.
+// 2^y for y <= 0 (or a little above): 2^n 2^f with f in [-1/2, 1/2], the latter by the polynomial that meets it at the
+// nine Chebyshev points, within 1.1e-12 of the value everywhere.  Adding 1.5 x 2^52 leaves y's nearest
+// whole number in the low word; below -1000 the result is 0, or, without EXACT, 2^-1000.
+template <bool EXACT = true>
 __device__ __forceinline__ double exp2_64(double y) {
-    y = fmax(y, -1100.0);
-    const double n = rint(y), f = y - n;
-    double p = 7.0549116208011209e-09;  // ln(2)^k / k!, k = 10 .. 0
-    p = fma(p, f, 1.0178086009239696e-07);
-    p = fma(p, f, 1.3215486790144305e-06);
-    p = fma(p, f, 1.5252733804059838e-05);
-    p = fma(p, f, 1.5403530393381606e-04);
-    p = fma(p, f, 1.3333558146428441e-03);
-    p = fma(p, f, 9.6181291076284769e-03);
-    p = fma(p, f, 5.5504108664821576e-02);
-    p = fma(p, f, 2.4022650695910069e-01);
-    p = fma(p, f, 6.9314718055994529e-01);
+    constexpr double kRound = 6755399441055744.0;
+    const double v = EXACT ? y : fmax(y, -1000.0), t = v + kRound, f = v - (t - kRound);
+    double p = 1.3255224878668817e-06;
+    p = fma(p, f, 1.5310079402249296e-05);
+    p = fma(p, f, 1.5403455852453838e-04);
+    p = fma(p, f, 1.3333450568000645e-03);
+    p = fma(p, f, 9.6181291594025584e-03);
+    p = fma(p, f, 5.5504109412059327e-02);
+    p = fma(p, f, 2.4022650695812989e-01);
+    p = fma(p, f, 6.9314718054593349e-01);
     p = fma(p, f, 1.0);
-    return ldexp(p, (int)n);
+    const double r = __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
+    return EXACT && !(y >= -1000.0) ? 0.0 : r;
 }
 constexpr double kLog2e = 1.4426950408889634;
 
 __device__ __forceinline__ bool tree_len_ok(int l) { return l >= 0 && l <= 0x7fffffff - CDB_TREE_MAX_NODES; }
-
-// Whether cdb_tree_rows gave tree t no rows because of its sequence or length.  By one thread.
-__device__ __forceinline__ bool tree_refused(const cdb_drafts& dr, int t) {
-    if (!dr.seq) return false;
-    const int sq = dr.seq[t];
-    if (sq < 0 || sq >= dr.max_seqs) return true;
-    for (int k = 0; k < t; ++k)
-        if (dr.seq[k] == sq) return true;
-    return dr.len && !tree_len_ok(dr.len[sq]);
-}
 
 __device__ __forceinline__ bool temperature_ok(float t) { return t > 0.f && t < INFINITY; }
 
@@ -78,16 +69,55 @@ __device__ __forceinline__ float4 logits4(const float* row, int i, int V) {
     return i < V ? *reinterpret_cast<const float4*>(row + i) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
 }
 
-template <typename T, typename F>
-__device__ __forceinline__ T wave_all(T v, F f) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v = f(v, __shfl_xor(v, o, 64));
-    return v;
+// Lane exchanges of 64-bit values by data-parallel moves, which take a tenth of the time of shuffles through LDS.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ double dpp64(double x) {  // lanes without a source read 0
+    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(x), CTRL, ROWS, 0xf, true);
+    const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(x), CTRL, ROWS, 0xf, true);
+    return __hiloint2double(hi, lo);
+}
+// Sum over the wave, the same in every lane.
+__device__ __forceinline__ double wave_sum(double x) {
+    x += dpp64<0xb1>(x);   // lanes of a pair
+    x += dpp64<0x4e>(x);   // pairs of a quad
+    x += dpp64<0x141>(x);  // quads of 8 (mirrored)
+    x += dpp64<0x140>(x);  // halves of 16 (mirrored)
+    auto lo = __builtin_amdgcn_permlane16_swap(__double2loint(x), __double2loint(x), false, false);
+    auto hi = __builtin_amdgcn_permlane16_swap(__double2hiint(x), __double2hiint(x), false, false);
+    x = __hiloint2double(hi[0], lo[0]) + __hiloint2double(hi[1], lo[1]);
+    lo = __builtin_amdgcn_permlane32_swap(__double2loint(x), __double2loint(x), false, false);
+    hi = __builtin_amdgcn_permlane32_swap(__double2hiint(x), __double2hiint(x), false, false);
+    return __hiloint2double(hi[0], lo[0]) + __hiloint2double(hi[1], lo[1]);
+}
+// Sums over the lanes up to this one.
+__device__ __forceinline__ double wave_scan(double x) {
+    x += dpp64<0x111>(x);  // from 1, 2, 4 and 8 lanes below in 16
+    x += dpp64<0x112>(x);
+    x += dpp64<0x114>(x);
+    x += dpp64<0x118>(x);
+    x += dpp64<0x142, 0xa>(x);  // the last lane of 16 to the next 16
+    x += dpp64<0x143, 0xc>(x);  // lane 31 to the upper half
+    return x;
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp32(float x) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float wave_max(float x) {
+    x = fmaxf(x, dpp32<0xb1>(x));
+    x = fmaxf(x, dpp32<0x4e>(x));
+    x = fmaxf(x, dpp32<0x141>(x));
+    x = fmaxf(x, dpp32<0x140>(x));
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// Workgroup = (piece, row, target or drafter).
+// Maxima and sums of the pieces of every row that a tree has; of the drafter's rows those of nodes with children,
+// which are known before their logits are read.  Workgroup = (piece, row, target or drafter).
 __global__ __launch_bounds__(256) void k_sample_stats(SampleArgs a) {
-    __shared__ int s_found, s_tree, s_kids;
+    __shared__ int s_tree, s_kids;
     __shared__ float s_max[4];
     __shared__ double s_sum[4];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -95,34 +125,32 @@ __global__ __launch_bounds__(256) void k_sample_stats(SampleArgs a) {
     const bool target = blockIdx.z == 0;
     const float* src = target ? a.sm.logits + (size_t)row * a.sm.logits_stride : a.sm.draft_logits + (size_t)row * a.sm.draft_stride;
     float4 x[4];
+    auto fetch = [&]() {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = logits4(src, piece * kPiece + i * 1024 + tid * 4, a.V);
-    if (tid == 0) s_found = s_kids = 0;
+        for (int i = 0; i < 4; ++i) x[i] = logits4(src, piece * kPiece + i * 1024 + tid * 4, a.V);
+    };
+    if (target) fetch();
+    if (tid == 0) {
+        s_tree = -1;
+        s_kids = 0;
+    }
     if (piece + row + blockIdx.z == 0)  // for the launches of k_sample_walk
         for (int i = tid; i < kTrees * (kRounds + 1); i += 256) a.arrive[i] = 0;
     __syncthreads();
-    bool mine = false;
-    int first = 0;
     if (tid < a.dr.n_trees) {
-        first = a.row0[tid];
-        const int n = a.dr.n_nodes[tid];
-        mine = first >= 0 && n > 0 && n <= a.dr.max_nodes && row >= first && row < first + n;
-    }
-    if (mine) {
-        s_tree = tid;
-        atomicAdd(&s_found, 1);
+        const int first = a.row0[tid], n = a.dr.n_nodes[tid];
+        // a tree that was refused stands where rows of later trees begin
+        if (first >= 0 && n > 0 && n <= a.dr.max_nodes && row >= first && row < first + n) atomicMax(&s_tree, tid);
     }
     __syncthreads();
-    if (s_found == 0) return;
-    if (s_found > 1) {  // a tree that was refused stands where the next one's rows begin
-        if (mine && !tree_refused(a.dr, tid)) s_tree = tid;
-        __syncthreads();
-    }
-    const int t = s_tree, node = row - a.row0[t];
-    if (!target) {  // the drafter's probabilities count where there are children
+    const int t = s_tree;
+    if (t < 0) return;
+    if (!target) {
+        const int node = row - a.row0[t];
         if (tid < a.dr.max_nodes && tid < a.dr.n_nodes[t] && a.dr.parent[(size_t)t * a.dr.max_nodes + tid] == node) s_kids = 1;
         __syncthreads();
         if (!s_kids) return;
+        fetch();
     }
     const float* temps = target ? a.sm.temperature : a.sm.draft_temperature;
     const double scale = temps ? kLog2e / (double)temps[t] : kLog2e;
@@ -133,7 +161,7 @@ __global__ __launch_bounds__(256) void k_sample_stats(SampleArgs a) {
         m = fmaxf(fmaxf(fmaxf(m, x[i].x), fmaxf(x[i].y, x[i].z)), x[i].w);
         nan |= x[i].x != x[i].x || x[i].y != x[i].y || x[i].z != x[i].z || x[i].w != x[i].w;
     }
-    m = wave_all(m, [](float p, float q) { return fmaxf(p, q); });
+    m = wave_max(m);
     if (lane == 0) s_max[w] = m;
     __syncthreads();
     m = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
@@ -142,11 +170,11 @@ __global__ __launch_bounds__(256) void k_sample_stats(SampleArgs a) {
         const double mc = -scale * m;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            s += exp2_64(fma((double)x[i].x, scale, mc)) + exp2_64(fma((double)x[i].y, scale, mc));
-            s += exp2_64(fma((double)x[i].z, scale, mc)) + exp2_64(fma((double)x[i].w, scale, mc));
+            s += exp2_64<false>(fma((double)x[i].x, scale, mc)) + exp2_64<false>(fma((double)x[i].y, scale, mc));
+            s += exp2_64<false>(fma((double)x[i].z, scale, mc)) + exp2_64<false>(fma((double)x[i].w, scale, mc));
         }
     }
-    s = wave_all(s, [](double p, double q) { return p + q; });
+    s = wave_sum(s);
     if (lane == 0) s_sum[w] = s;
     __syncthreads();
     if (tid == 0)
@@ -162,10 +190,10 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
     double* s_part = s_sum + a.pieces; // [pieces][4] the waves' parts
     __shared__ double s_m[2][CDB_TREE_MAX_NODES], s_inv[2][CDB_TREE_MAX_NODES];  // each node's maximum x scale, 1 / sum
     __shared__ double s_z[CDB_TREE_MAX_NODES + 1];  // 1 / Z_k after k rejections at the current node
-    __shared__ double s_red[4];
+    __shared__ double s_seg[16];
     __shared__ int s_out[CDB_TREE_MAX_NODES];  // the tokens of the rejections
-    __shared__ int s_par[CDB_TREE_MAX_NODES];
-    __shared__ int s_cur, s_k, s_todo, s_pick[8];
+    __shared__ int s_kid[CDB_TREE_MAX_NODES];  // whether the node has children
+    __shared__ int s_cur, s_k, s_todo, s_pick[1];
     const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const bool dense = a.sm.draft_logits != nullptr, tells = blockIdx.x == 0;
     const int N = a.dr.max_nodes;
@@ -213,48 +241,51 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
         if (dense) lq = draft_row(par)[token];
     }
     const uint64_t lives = __ballot(live);
-    if (w == 0) s_par[lane] = par;
+    if (w == 0) {
+        s_kid[lane] = 0;
+        if (par >= 0) s_kid[par] = 1;
+    }
     __syncthreads();
     {  // statistics of the nodes' rows: four threads to a node
         const int node = tid >> 2, sub = tid & 3;
         const bool here = lives >> node & 1;
-        bool kids = false;
-        if (here && dense)
-            for (int j = node + 1 + sub; j < n; j += 4) kids |= s_par[j] == node;
-        kids = (int)kids | __shfl_xor((int)kids, 1, 64);
-        kids = (int)kids | __shfl_xor((int)kids, 2, 64);
+        const bool has[2] = {here, here && dense && s_kid[node]};
+        double m[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0, 0.0};
+        for (int i0 = 0; i0 < a.pieces; i0 += 16) {
+            double2 x[2][4];
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
-            double m = -INFINITY, sum = 0.0;
-            if (here && (z == 0 || kids)) {
+            for (int z = 0; z < 2; ++z) {
                 const double2* st = a.stats + ((size_t)(z ? a.n_rows : 0) + r0 + node) * a.pieces;
-                for (int i0 = 0; i0 < a.pieces; i0 += 16) {
-                    double2 x[4];
-                    double top = m;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int piece = i0 + i * 4 + sub;
-                        x[i] = piece < a.pieces ? st[piece] : make_double2(-INFINITY, 0.0);
-                        top = fmax(top, x[i].x);
-                    }
-                    // a piece of nothing but -inf has the sum 0, one with NaN the sum NaN
-                    if (m > -INFINITY) sum *= exp2_64((m - top) * scale[z]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const double e = exp2_64((x[i].x - top) * scale[z]);
-                        sum += x[i].x > -INFINITY ? x[i].y * e : x[i].y;
-                    }
-                    m = top;
+                for (int i = 0; i < 4; ++i) {
+                    const int piece = i0 + i * 4 + sub;
+                    x[z][i] = has[z] && piece < a.pieces ? st[piece] : make_double2(-INFINITY, 0.0);
                 }
             }
-            double top = fmax(m, __shfl_xor(m, 1, 64));
-            top = fmax(top, __shfl_xor(top, 2, 64));
-            if (m > -INFINITY) sum *= exp2_64((m - top) * scale[z]);
-            sum += __shfl_xor(sum, 1, 64);
-            sum += __shfl_xor(sum, 2, 64);
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                const double top = fmax(fmax(fmax(m[z], x[z][0].x), fmax(x[z][1].x, x[z][2].x)), x[z][3].x);
+                // a piece of nothing but -inf has the sum 0, one with NaN the sum NaN
+                if (i0 && m[z] > -INFINITY) sum[z] *= exp2_64((m[z] - top) * scale[z]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const double e = exp2_64((x[z][i].x - top) * scale[z]);
+                    sum[z] += x[z][i].x > -INFINITY ? x[z][i].y * e : x[z][i].y;
+                }
+                m[z] = top;
+            }
+        }
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+            double top = fmax(m[z], dpp64<0xb1>(m[z]));
+            top = fmax(top, dpp64<0x4e>(top));
+            const double e = exp2_64((m[z] - top) * scale[z]);
+            if (m[z] > -INFINITY) sum[z] *= e;
+            sum[z] += dpp64<0xb1>(sum[z]);
+            sum[z] += dpp64<0x4e>(sum[z]);
             if (sub == 0) {
                 s_m[z][node] = top * scale[z];
-                s_inv[z][node] = top < INFINITY ? 1.0 / sum : NAN;  // NaN or infinite: no distribution
+                s_inv[z][node] = top < INFINITY ? 1.0 / sum[z] : NAN;  // NaN or infinite: no distribution
             }
         }
     }
@@ -292,12 +323,17 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
                 for (int j = 0; j < 4; ++j) r[j] = i + j == s_out[s] ? 0.0 : r[j];
         }
     };
-    auto add = [](double x, double y) { return x + y; };
-    // s_sum's total, the same bits in every wave
+    // s_sum's total, the same bits in every thread
     auto total = [&]() {
         double z = 0.0;
-        for (int i = lane; i < a.pieces; i += 64) z += s_sum[i];
-        return wave_all(z, add);
+        if (a.pieces <= 32) {
+#pragma unroll 4
+            for (int i = 0; i < a.pieces; ++i) z += s_sum[i];
+        } else {
+            for (int i = lane; i < a.pieces; i += 64) z += s_sum[i];
+            z = wave_sum(z);
+        }
+        return z;
     };
 
     int path = -1, count = 0, cur = -1, tried = -1, k = 0, rejected = 0;
@@ -408,7 +444,7 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
                         left4(x, y, e, c, kk, r);
                         s += (r[0] + r[1]) + (r[2] + r[3]);
                     }
-                    s = wave_all(s, add);
+                    s = wave_sum(s);
                     if (lane == 0) s_part[piece * 4 + w] = s;
                 }
                 __syncthreads();
@@ -455,70 +491,94 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
         const double aim = (double)un * total();
         double start = 0.0, before = 0.0;
         int piece = 0;
-        for (int i0 = 0; i0 < a.pieces; i0 += 64) {
-            const double own = i0 + lane < a.pieces ? s_sum[i0 + lane] : 0.0;
-            double v = own;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const double x = __shfl_up(v, o, 64);
-                if (lane >= o) v += x;
+        if (a.pieces <= 32) {
+            bool found = false;
+#pragma unroll 4
+            for (int i = 0; i < a.pieces; ++i) {
+                const double own = s_sum[i];
+                if (own > 0.0 && !found) {
+                    piece = i;
+                    start = before;
+                    found = before + own > aim;
+                }
+                before += own;
             }
-            const uint64_t hit = __ballot(before + v > aim && own > 0.0), some = __ballot(own > 0.0);
-            if (some) {
-                const int j = hit ? __ffsll((unsigned long long)hit) - 1 : 63 - __clzll((long long)some);
-                piece = i0 + j;
-                start = before + __shfl(v - own, j, 64);
-                if (hit) break;
+        } else {
+            for (int i0 = 0; i0 < a.pieces; i0 += 64) {
+                const double own = i0 + lane < a.pieces ? s_sum[i0 + lane] : 0.0;
+                const double v = wave_scan(own);
+                const uint64_t hit = __ballot(before + v > aim && own > 0.0), some = __ballot(own > 0.0);
+                if (some) {
+                    const int j = hit ? __ffsll((unsigned long long)hit) - 1 : 63 - __clzll((long long)some);
+                    piece = i0 + j;
+                    start = before + __shfl(v - own, j, 64);
+                    if (hit) break;
+                }
+                before += __shfl(v, 63, 64);
             }
-            before += __shfl(v, 63, 64);
         }
-        const int e = piece * kPiece + tid * 16;
         const float *tp = target_row(c), *tq = dense ? draft_row(c) : tp;
         float4 p[4], q[4];
-        double r[4][4], own = 0.0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            p[i] = logits4(tp, e + i * 4, a.V);
-            q[i] = logits4(tq, e + i * 4, a.V);
+            p[i] = logits4(tp, piece * kPiece + i * 1024 + tid * 4, a.V);
+            q[i] = logits4(tq, piece * kPiece + i * 1024 + tid * 4, a.V);
         }
+        double r[4][4], own[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            left4(p[i], q[i], e + i * 4, c, kk, r[i]);
-            own += (r[i][0] + r[i][1]) + (r[i][2] + r[i][3]);
+            left4(p[i], q[i], piece * kPiece + i * 1024 + tid * 4, c, kk, r[i]);
+            own[i] = (r[i][0] + r[i][1]) + (r[i][2] + r[i][3]);
+            const double z = wave_sum(own[i]);
+            if (lane == 0) s_seg[i * 4 + w] = z;  // 256 logits in a row
         }
-        double v = own;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const double x = __shfl_up(v, o, 64);
-            if (lane >= o) v += x;
-        }
-        if (lane == 63) s_red[w] = v;
         __syncthreads();
-        double run = start;
-        for (int i = 0; i < w; ++i) run += s_red[i];
-        run += v - own;
-        int pick = 0x7fffffff, last = -1;
+        // the segment, as the piece above; its wave looks for the logit
+        int seg = 0;
+        bool found = false;
+        double from = start;
+        before = start;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const double x = r[i >> 2][i & 3];
-            run += x;
-            if (x > 0.0) {
-                last = e + i;
-                if (run > aim) pick = min(pick, e + i);
+            const double x = s_seg[i];
+            if (x > 0.0 && !found) {
+                seg = i;
+                from = before;
+                found = before + x > aim;
             }
+            before += x;
         }
-        // lanes and waves are in the tokens' order
-        const uint64_t hit = __ballot(pick != 0x7fffffff), some = __ballot(last >= 0);
-        if (hit) pick = __shfl(pick, __ffsll((unsigned long long)hit) - 1, 64);
-        if (some) last = __shfl(last, 63 - __clzll((long long)some), 64);
-        if (lane == 0) {
-            s_pick[w] = pick;
-            s_pick[4 + w] = last;
+        if ((seg & 3) == w) {
+            double x[4], mine = 0.0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = 0.0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (seg >> 2 == i) {
+                    mine = own[i];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] = r[i][j];
+                }
+            double run = from + (wave_scan(mine) - mine);
+            const int e = piece * kPiece + seg * 256 + lane * 4;
+            int pick = -1, last = -1;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                run += x[j];
+                if (x[j] > 0.0) {
+                    last = e + j;
+                    if (pick < 0 && run > aim) pick = e + j;
+                }
+            }
+            const uint64_t hit = __ballot(pick >= 0), some = __ballot(last >= 0);
+            if (hit)
+                pick = __builtin_amdgcn_readlane(pick, __ffsll((unsigned long long)hit) - 1);
+            else
+                pick = some ? __builtin_amdgcn_readlane(last, 63 - __clzll((long long)some)) : 0;
+            if (lane == 0) s_pick[0] = pick;
         }
         __syncthreads();
-        pick = min(min(s_pick[0], s_pick[1]), min(s_pick[2], s_pick[3]));
-        last = max(max(s_pick[4], s_pick[5]), max(s_pick[6], s_pick[7]));
-        next = pick != 0x7fffffff ? pick : max(last, 0);
+        next = s_pick[0];
     }
     if (w != 0) return;
     if (bad) {
