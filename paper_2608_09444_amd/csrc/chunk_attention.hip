@@ -7,6 +7,8 @@
 namespace cdb {
 
 constexpr int kTileRows = 128;  // rows of a workgroup: 32 to each of its 4 waves
+constexpr int kNoVmem = 0xf70;   // s_waitcnt: vector memory loads 0, the others any
+constexpr int kMergeRows = 16;  // rows of a workgroup that joins segments
 constexpr int kStep = 64;       // keys that a workgroup stages at a time, a page to each wave
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -133,14 +135,23 @@ __device__ __forceinline__ bool odd_words(u32x4 x) {  // an infinity or NaN amon
     return odd;
 }
 
+// Eight weights times a power of two.
+__device__ __forceinline__ bf16x8 scaled(bf16x8 p, float f) {
+    u32x4 w = __builtin_bit_cast(u32x4, p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack_bf16(bflo(w[i]) * f, bfhi(w[i]) * f);
+    return __builtin_bit_cast(bf16x8, w);
+}
+
 template <int HD, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
     constexpr int NT = HD / 16, NB = HD / 32, NL = HD / 32, CPK = HD / 8;
-    constexpr int KP = HD + 8;                      // K row pitch: consecutive keys 4 banks apart (mod 64)
-    constexpr int VP = HD == 96 ? HD : HD + 32;     // V row pitch: consecutive keys 16 banks apart (mod 64)
+    constexpr int KP = HD + 8;                   // K row pitch: consecutive keys 4 banks apart (mod 64)
+    constexpr int VP = HD == 96 ? HD : HD + 32;  // V row pitch: consecutive keys 16 banks apart (mod 64)
     __shared__ __align__(16) uint16_t sk[2][kStep * KP];
     __shared__ __align__(16) uint16_t sv[2][kStep * VP];
-    __shared__ __align__(16) int s_flag[2][4];
+    __shared__ __align__(16) int s_there[2][4];  // by page of a step: whether it is mapped
+    __shared__ __align__(16) int s_odd[2][4];    // and holds V that stage_v took out
     __shared__ ChunkTile s_tile;
     __shared__ int s_red[4];
     int head, rest;
@@ -156,44 +167,54 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
     const int segs = chunk_segments(last + 1, a.split, &seg_len);
     if (seg >= segs) return;
     const int k0 = seg * seg_len, k1 = min(last + 1, k0 + seg_len);
+    const int steps = (k1 - k0 + kStep - 1) / kStep;
     const int d = a.H * HD;
     const int my = w * 32 + c32;  // this lane's row in the tile
     const int qpos = t_pos + my;
-    const int w_last = t_pos + min(t_n, w * 32 + 32) - 1;  // the last position that the wave's rows see
-    const bool w_any = w * 32 < t_n;
-    const int32_t* pt = a.kv.page_table + ((size_t)__builtin_amdgcn_readfirstlane(s_tile.seq) * a.kv.n_planes +
-                                           __builtin_amdgcn_readfirstlane(s_tile.plane)) * a.kv.max_pages;
+    const int w_first = t_pos + w * 32;                         // position of the wave's first row
+    const int w_last = t_pos + min(t_n, w * 32 + 32) - 1;       // and of its last one
+    const int na = w * 32 < t_n && w_last >= k0 ? min(2 * steps, (w_last - k0) / 32 + 1) : -1;  // halves with keys that it sees
+    // the table by scalar loads: a page id is asked for a step before it is used, and vector loads would make its
+    // use wait for the K and V that are on their way
+    const auto* pt = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.kv.page_table + ((size_t)__builtin_amdgcn_readfirstlane(s_tile.seq) * a.kv.n_planes +
+                                           __builtin_amdgcn_readfirstlane(s_tile.plane)) * a.kv.max_pages);
 
     // staging: wave w takes page w of a step
     u32x4 kr[NL], vr[NL];
-    auto page_of = [&](int k) {  // -1: behind the segment, or not mapped
-        const int at = k + w * kPage;
-        if (at >= k1) return -2;
-        const int pid = __builtin_amdgcn_readfirstlane(pt[at / kPage]);
-        return pid >= 0 && pid < a.kv.n_pages ? pid : -1;
+    const int tables = a.kv.max_pages - 1;
+    auto entry_of = [&](int t) { return pt[min((k0 + t * kStep) / kPage + w, tables)]; };
+    auto page_of = [&](int t, int pid) {  // -2: behind the segment, -1: not mapped
+        return k0 + t * kStep + w * kPage >= k1 ? -2 : pid >= 0 && pid < a.kv.n_pages ? pid : -1;
     };
-    auto fetch = [&](int pid) {
+    const uint16_t* pool = a.kv.pool + kv_offset(a.kv.layer, 0, a.kv.n_pages, 0, head, a.H, 0, HD) + lane * 8;
+    const size_t page_len = (size_t)2 * a.H * kPage * HD, v_off = (size_t)a.H * kPage * HD;
+    auto fetch = [&](u32x4 (&r)[NL], int pid, size_t off) __attribute__((always_inline)) {
         if (pid >= 0) {
-            const uint16_t* at = a.kv.pool + kv_offset(a.kv.layer, pid, a.kv.n_pages, 0, head, a.H, 0, HD) + lane * 8;
+            const uint16_t* at = pool + pid * page_len + off;
 #pragma unroll
-            for (int i = 0; i < NL; ++i) {
-                kr[i] = *reinterpret_cast<const u32x4*>(at + i * 512);
-                vr[i] = *reinterpret_cast<const u32x4*>(at + (size_t)a.H * kPage * HD + i * 512);
-            }
+            for (int i = 0; i < NL; ++i) r[i] = *reinterpret_cast<const u32x4*>(at + i * 512);
         } else {
 #pragma unroll
-            for (int i = 0; i < NL; ++i) kr[i] = vr[i] = u32x4{0, 0, 0, 0};
+            for (int i = 0; i < NL; ++i) r[i] = u32x4{0, 0, 0, 0};
         }
     };
-    // A step whose keys not all rows see: V behind the last position becomes 0, and a V that is not finite too
+    auto stage_k = [&](int pid, int b) __attribute__((always_inline)) {
+        if (pid == -1 && lane == 0) set_err(a.err, CDB_DEV_UNMAPPED_PAGE);
+        if (lane == 0) s_there[b][w] = pid >= 0;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int f = i * 64 + lane;
+            *reinterpret_cast<u32x4*>(&sk[b][(w * kPage + f / CPK) * KP + f % CPK * 8]) = kr[i];
+        }
+    };
+    // Of a step whose keys not all rows see, V behind the last position becomes 0, and a V that is not finite too
     // (put_odd adds it to the rows that see it).
-    auto stage = [&](int k, int pid, int b) {
-        int flag = pid >= 0;
-        if (k + kStep - 1 > t_pos && pid >= 0) {
-            bool odd = false;
+    auto stage_v = [&](int t, int pid, int b) __attribute__((always_inline)) {
+        bool odd = false;
+        if (k0 + t * kStep + kStep - 1 > t_pos && pid >= 0)
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
-                const int key = k + w * kPage + (i * 64 + lane) / CPK;
+                const int key = k0 + t * kStep + w * kPage + (i * 64 + lane) / CPK;
                 const bool gone = key > last, o = !gone && odd_words(vr[i]);
                 odd |= o;
                 if (gone) vr[i] = u32x4{0, 0, 0, 0};
@@ -204,20 +225,24 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
                         if ((vr[i][x] & 0x7f800000u) == 0x7f800000u) vr[i][x] &= 0xffffu;
                     }
             }
-            if (__any(odd)) flag |= 2;
-        }
-        if (pid == -1 && lane == 0) set_err(a.err, CDB_DEV_UNMAPPED_PAGE);
-        if (lane == 0) s_flag[b][w] = flag;
+        odd = __any(odd);
+        if (lane == 0) s_odd[b][w] = odd;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int f = i * 64 + lane, key = w * kPage + f / CPK, cc = f % CPK;
-            *reinterpret_cast<u32x4*>(&sk[b][key * KP + cc * 8]) = kr[i];
-            *reinterpret_cast<u32x4*>(&sv[b][key * VP + cc * 8]) = vr[i];
+            const int f = i * 64 + lane;
+            *reinterpret_cast<u32x4*>(&sv[b][(w * kPage + f / CPK) * VP + f % CPK * 8]) = vr[i];
         }
     };
+    // bits: the step's pages whose word is set
+    auto bits = [&](const int* f) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(f);
+        return __builtin_amdgcn_readfirstlane((int)(v[0] | v[1] << 1 | v[2] << 2 | v[3] << 3));
+    };
 
-    int pid = page_of(k0), pid_next = page_of(k0 + kStep);
-    fetch(pid);
+    const int pid0 = page_of(0, entry_of(0));
+    int entry = entry_of(1);
+    fetch(kr, pid0, 0);
+    fetch(vr, pid0, v_off);
 
     // q as the B operand: dims 16 t + 8 half + e of row c32; in two parts it takes the scale along
     const float scale = 1.4426950408889634f / sqrtf((float)HD);
@@ -248,112 +273,169 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
     }
     const float s_scale = SPLIT ? 1.f : scale;
 
-    floatx16 o[NB];
+    floatx16 o[NB], s0, s1;  // s0, s1: scores of first and second halves
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+    for (int j = 0; j < 16; ++j) s0[j] = s1[j] = 0.f;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) o[b][j] = 0.f;
+    for (int x = 0; x < NB; ++x) o[x] = s0;
     float m = -INFINITY, l = 0.f;
+    bf16x8 ph[2], pl[2];  // weights of the half before
+    ph[0] = ph[1] = pl[0] = pl[1] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
 
-    stage(k0, pid, 0);
-    for (int k = k0, b = 0; k < k1; k += kStep, b ^= 1) {
-        __syncthreads();
-        const bool more = k + kStep < k1;
-        if (more) {
-            pid = pid_next;
-            fetch(pid);
-            pid_next = page_of(k + 2 * kStep);
+    const int k_at = c32 * KP + half * 8;
+    const int v_at = (4 * half + ((lane & 15) >> 2)) * VP + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
+    auto k_operand = [&](const uint16_t* k, int t) { return *reinterpret_cast<const bf16x8*>(k + k_at + t * 16); };
+    auto v_operand = [&](const uint16_t* v, int st, int x) {
+        const uint16_t* at = v + v_at + st * 16 * VP + x * 32;
+        const uint2 w0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
+        const uint2 w1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * VP)));
+        return __builtin_bit_cast(bf16x8, u32x4{w0.x, w0.y, w1.x, w1.y});
+    };
+    auto scores = [&](const uint16_t* k) __attribute__((always_inline)) {
+        floatx16 r;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) r[j] = 0.f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const bf16x8 ka = k_operand(k, t);
+            if constexpr (SPLIT) r = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, ql[t], r, 0, 0, 0);
+            r = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qh[t], r, 0, 0, 0);
         }
-        if (w_any && k <= w_last) {
-            const u32x4 fl = *reinterpret_cast<const u32x4*>(s_flag[b]);
-            const int there = __builtin_amdgcn_readfirstlane((fl[0] & 1) | (fl[1] & 1) << 1 | (fl[2] & 1) << 2 | (fl[3] & 1) << 3);
-            const bool odd = __builtin_amdgcn_readfirstlane((fl[0] | fl[1] | fl[2] | fl[3]) & 2);
-            const bool masked = k + kStep - 1 > t_pos + w * 32 || there != 15;
-            floatx16 s[2];
+        return r;
+    };
+    auto product = [&](const uint16_t* v, int st, int x, const bf16x8 (&h)[2], const bf16x8 (&lo)[2]) __attribute__((always_inline)) {
+        const bf16x8 va = v_operand(v, st, x);
+        if constexpr (SPLIT) o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, lo[st], o[x], 0, 0, 0);
+        o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, h[st], o[x], 0, 0, 0);
+    };
+    auto products = [&](const uint16_t* v) __attribute__((always_inline)) {
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+        for (int st = 0; st < 2; ++st)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) s[kb][j] = 0.f;
+            for (int x = 0; x < NB; ++x) product(v, st, x, ph, pl);
+    };
+    auto put_odd = [&](int from) __attribute__((always_inline)) {  // V of keys from .. from + 31 that stage_v took out
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+        for (int x = 0; x < NB; ++x) {
+            floatx16 more;
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const bf16x8 ka = *reinterpret_cast<const bf16x8*>(&sk[b][(kb * 32 + c32) * KP + t * 16 + half * 8]);
-                    if constexpr (SPLIT) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, ql[t], s[kb], 0, 0, 0);
-                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qh[t], s[kb], 0, 0, 0);
-                }
-            if (masked)
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const int key = k + kb * 32 + (j >> 2) * 8 + half * 4 + (j & 3);
-                        if (key > qpos || !(there >> (kb * 2 + (j >> 3)) & 1)) s[kb][j] = -INFINITY;
-                    }
-            float mx = fmaxf(s[0][0], s[1][0]);
-#pragma unroll
-            for (int j = 1; j < 16; ++j) mx = fmaxf(fmaxf(mx, s[0][j]), s[1][j]);
-            {
-                const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-                mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * s_scale;
-            }
-            const bool up = mx > m + 8.f;
-            if (__any(up)) {
-                const float corr = up ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
-                m = up ? mx : m;
-                l *= corr;
-#pragma unroll
-                for (int x = 0; x < NB; ++x)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) o[x][j] *= corr;
-            }
-            const float mref = m == -INFINITY ? 0.f : m;  // nothing seen yet: every weight 0
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    uint32_t hw[4], lw[4];
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kb][st * 8 + e], s_scale, -mref));
-                        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[kb][st * 8 + e + 1], s_scale, -mref));
-                        l += p0 + p1;
-                        hw[e / 2] = pack_bf16(p0, p1);
-                        if constexpr (SPLIT) lw[e / 2] = pack_bf16(p0 - bflo(hw[e / 2]), p1 - bfhi(hw[e / 2]));
-                    }
-                    const bf16x8 ph = __builtin_bit_cast(bf16x8, u32x4{hw[0], hw[1], hw[2], hw[3]});
-                    bf16x8 pl = ph;
-                    if constexpr (SPLIT) pl = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], lw[2], lw[3]});
-                    const int g = lane >> 4, c = lane & 15;
-                    const uint16_t* vb = &sv[b][(kb * 32 + st * 16 + 4 * half + (c >> 2)) * VP + (g & 1) * 16 + (c & 3) * 4];
-#pragma unroll
-                    for (int x = 0; x < NB; ++x) {
-                        const uint2 w0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                                                       (__attribute__((address_space(3))) s16x4*)(vb + x * 32)));
-                        const uint2 w1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                                                       (__attribute__((address_space(3))) s16x4*)(vb + 8 * VP + x * 32)));
-                        const bf16x8 va = __builtin_bit_cast(bf16x8, u32x4{w0.x, w0.y, w1.x, w1.y});
-                        if constexpr (SPLIT) o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pl, o[x], 0, 0, 0);
-                        o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, ph, o[x], 0, 0, 0);
-                    }
-                }
-            if (odd) {  // rare: values taken out by stage, to the rows that see them
+            for (int j = 0; j < 16; ++j) more[j] = 0.f;
 #pragma unroll 1
-                for (int key = k; key < min(k + kStep, last + 1); ++key) {
-                    const int id = pt[key / kPage];
-                    if (id < 0 || id >= a.kv.n_pages) continue;
-                    const uint16_t* at = a.kv.pool + kv_offset(a.kv.layer, id, a.kv.n_pages, 1, head, a.H, key % kPage, HD) + half * 4;
+            for (int key = from; key < min(from + 32, last + 1); ++key) {
+                const int id = pt[key / kPage];
+                if (id < 0 || id >= a.kv.n_pages) continue;
+                const uint16_t* at = a.kv.pool + kv_offset(a.kv.layer, id, a.kv.n_pages, 1, head, a.H, key % kPage, HD) + half * 4;
 #pragma unroll
-                    for (int x = 0; x < NB; ++x)
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const uint16_t v = at[x * 32 + (j >> 2) * 8 + (j & 3)];
-                            if ((v & 0x7f80) == 0x7f80 && key <= qpos) o[x][j] += bf2f(v);
-                        }
+                for (int j = 0; j < 16; ++j) {
+                    const uint16_t v = at[x * 32 + (j >> 2) * 8 + (j & 3)];
+                    if ((v & 0x7f80) == 0x7f80 && key <= qpos) more[j] += bf2f(v);
                 }
             }
+            o[x] += more;
         }
-        if (more) stage(k + kStep, pid, b ^ 1);
+    };
+    // Half i (32 keys from k, scores in s): scores of the next one, weights of this one, products of the one before, which
+    // do not depend on one another.  there: this half's two pages; odd: whether put_odd has to run for the one before.
+    auto run_half = [&](int i, int k, floatx16& s, floatx16& next, const uint16_t* k_next, const uint16_t* v_before, int there,
+                        bool odd) __attribute__((always_inline)) {
+        if (i > na) return;  // half na: nothing of it is seen
+        if (k + 31 > w_first || there != 3)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (k + (j >> 2) * 8 + half * 4 + (j & 3) > qpos || !(there >> (j >> 3) & 1)) s[j] = -INFINITY;
+        // The maximum that a row's weights are taken against is a whole number (of powers of two) and follows the
+        // row's own once that is 8 above: what is scaled then, the weights at hand among it, stays exact.
+        float mx = fmaxf(s[0], s[1]);
+#pragma unroll
+        for (int j = 2; j < 16; ++j) mx = fmaxf(mx, s[j]);
+        {
+            const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+            mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * s_scale;
+        }
+        const bool up = mx > m + 8.f;
+        if (__any(up)) {
+            const float now = up ? ceilf(mx) : m;
+            const float corr = up ? __builtin_amdgcn_exp2f(m - now) : 1.f;
+            m = now;
+            l *= corr;
+#pragma unroll
+            for (int x = 0; x < NB; ++x)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[x][j] *= corr;
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                ph[st] = scaled(ph[st], corr);
+                if constexpr (SPLIT) pl[st] = scaled(pl[st], corr);
+            }
+        }
+        const float m0 = m == -INFINITY ? 0.f : m;  // nothing seen yet: every weight 0
+        const bf16x8 h[2] = {ph[0], ph[1]}, lo[2] = {pl[0], pl[1]};
+#pragma unroll
+        for (int j = 0; j < 16; ++j) next[j] = 0.f;
+        uint32_t hw[8], lw[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            if (t < NT) {
+                const bf16x8 ka = k_operand(k_next, t);
+                if constexpr (SPLIT) next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, ql[t], next, 0, 0, 0);
+                next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qh[t], next, 0, 0, 0);
+                product(v_before, t / NB, t % NB, h, lo);
+            }
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[2 * t], s_scale, -m0));
+            const float p1 = __builtin_amdgcn_exp2f(fmaf(s[2 * t + 1], s_scale, -m0));
+            l += p0 + p1;
+            hw[t] = pack_bf16(p0, p1);
+            if constexpr (SPLIT) lw[t] = pack_bf16(p0 - bflo(hw[t]), p1 - bfhi(hw[t]));
+        }
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            ph[st] = __builtin_bit_cast(bf16x8, u32x4{hw[st * 4], hw[st * 4 + 1], hw[st * 4 + 2], hw[st * 4 + 3]});
+            if constexpr (SPLIT) pl[st] = __builtin_bit_cast(bf16x8, u32x4{lw[st * 4], lw[st * 4 + 1], lw[st * 4 + 2], lw[st * 4 + 3]});
+        }
+        if (odd) put_odd(k - 32);
+    };
+
+    // V of the half before the first: zeros
+    for (int i = tid; i < 32 * VP / 8; i += 256) *reinterpret_cast<u32x4*>(&sv[1][32 * VP + i * 8]) = u32x4{0, 0, 0, 0};
+    stage_k(pid0, 0);
+    stage_v(0, pid0, 0);
+    // nothing is on its way here (q among it), so that no use of q in the loop waits for later loads
+    __builtin_amdgcn_s_waitcnt(kNoVmem);
+    int pid_k = page_of(1, entry), pid_v = pid_k;
+    entry = entry_of(2);
+    fetch(kr, pid_k, 0);
+    fetch(vr, pid_v, v_off);
+    __syncthreads();
+    if (na >= 0) s0 = scores(sk[0]);
+    int there = bits(s_there[0]), odd = 0;  // odd: of the step before
+    for (int t = 0, b = 0; t < steps; ++t, b ^= 1) {
+        const int k = k0 + t * kStep;
+        const bool more = t + 1 < steps;
+        // first half; the next step's K
+        const int pid_next = page_of(t + 2, entry);
+        if (more) {
+            stage_k(pid_k, b ^ 1);
+            pid_k = pid_next;
+            fetch(kr, pid_k, 0);
+        }
+        entry = entry_of(t + 3);
+        run_half(2 * t, k, s0, s1, sk[b] + 32 * KP, sv[b ^ 1] + 32 * VP, there & 3, odd >> 2 & 3);
+        odd = bits(s_odd[b]);
+        __syncthreads();
+        // second half; the next step's V
+        const int there_next = bits(s_there[b ^ 1]);
+        if (more) {
+            stage_v(t + 1, pid_v, b ^ 1);
+            pid_v = pid_next;
+            fetch(vr, pid_v, v_off);
+        }
+        run_half(2 * t + 1, k + 32, s1, s0, sk[b ^ 1], sv[b], there >> 2, odd & 3);
+        there = there_next;
+        __syncthreads();
+    }
+    if (na == 2 * steps) {
+        products(sv[(steps - 1) & 1] + 32 * VP);
+        if (odd >> 2) put_odd(k0 + steps * kStep - 32);
     }
 
     {
@@ -385,20 +467,20 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
                 make_float4(o[x][j], o[x][j + 1], o[x][j + 2], o[x][j + 3]);
 }
 
-// Segments of a tile's rows joined, in order.  Workgroup = (head, tile).
+// Segments of a tile's rows joined, in order.  Workgroup = (head, kMergeRows rows, tile).
 template <int HD>
 __global__ __launch_bounds__(256) void k_chunk_merge(ChunkAttnArgs a) {
     __shared__ ChunkTile s_tile;
     __shared__ int s_red[4];
-    const int head = blockIdx.x % a.H;
-    if (!chunk_tile(a, blockIdx.x / a.H, &s_tile, s_red, false)) return;
+    const int head = blockIdx.x, part = blockIdx.y * kMergeRows;
+    if (!chunk_tile(a, blockIdx.z, &s_tile, s_red, false)) return;
     const ChunkTile t = s_tile;
     int seg_len;
     const int segs = chunk_segments(t.pos + t.n, a.split, &seg_len);
     if (segs == 1) return;
     constexpr int CPR = HD / 8;  // threads of a row
-    for (int i = threadIdx.x; i < t.n * CPR; i += 256) {
-        const int row = t.row + i / CPR, c = i % CPR;
+    for (int i = threadIdx.x; i < min(t.n - part, kMergeRows) * CPR; i += 256) {
+        const int row = t.row + part + i / CPR, c = i % CPR;
         const size_t rec = ((size_t)row * a.H + head) * a.split.most;
         float top = -INFINITY;
         for (int s = 0; s < segs; ++s) top = fmaxf(top, a.ml[rec + s].x);
@@ -428,7 +510,7 @@ static void launch_hd(const ChunkAttnArgs& a, bool split, int groups, int tiles,
         k_chunk_attn<HD, true><<<groups, 256, 0, st>>>(a);
     else
         k_chunk_attn<HD, false><<<groups, 256, 0, st>>>(a);
-    if (a.split.most > 1) k_chunk_merge<HD><<<tiles * a.H, 256, 0, st>>>(a);
+    if (a.split.most > 1) k_chunk_merge<HD><<<dim3(a.H, kTileRows / kMergeRows, tiles), 256, 0, st>>>(a);
 }
 
 hipError_t launch_chunk_attention(const cdb_chunks& ch, const KvTarget& kv, const void* q, int q_type, int H, int hd,
