@@ -1,6 +1,7 @@
 // Causal attention of chunks of new tokens (several sequences, one to thousands of
 // rows each) over the paged, depth-indexed KV cache.
 #include <algorithm>
+#include <type_traits>
 
 #include "cdb_internal.h"
 
@@ -188,23 +189,35 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
     };
     const uint16_t* pool = a.kv.pool + kv_offset(a.kv.layer, 0, a.kv.n_pages, 0, head, a.H, 0, HD) + lane * 8;
     const size_t page_len = (size_t)2 * a.H * kPage * HD, v_off = (size_t)a.H * kPage * HD;
+    auto fetch_page = [&](u32x4 (&r)[NL], int pid, size_t off) __attribute__((always_inline)) {
+        const uint16_t* at = pool + pid * page_len + off;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) r[i] = *reinterpret_cast<const u32x4*>(at + i * 512);
+    };
     auto fetch = [&](u32x4 (&r)[NL], int pid, size_t off) __attribute__((always_inline)) {
         if (pid >= 0) {
-            const uint16_t* at = pool + pid * page_len + off;
-#pragma unroll
-            for (int i = 0; i < NL; ++i) r[i] = *reinterpret_cast<const u32x4*>(at + i * 512);
+            fetch_page(r, pid, off);
         } else {
 #pragma unroll
             for (int i = 0; i < NL; ++i) r[i] = u32x4{0, 0, 0, 0};
         }
     };
-    auto stage_k = [&](int pid, int b) __attribute__((always_inline)) {
-        if (pid == -1 && lane == 0) set_err(a.err, CDB_DEV_UNMAPPED_PAGE);
-        if (lane == 0) s_there[b][w] = pid >= 0;
+    auto put_k = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int f = i * 64 + lane;
             *reinterpret_cast<u32x4*>(&sk[b][(w * kPage + f / CPK) * KP + f % CPK * 8]) = kr[i];
+        }
+    };
+    auto stage_k = [&](int pid, int b) __attribute__((always_inline)) {
+        if (lane == 0) s_there[b][w] = pid >= 0;
+        put_k(b);
+    };
+    auto put_v = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int f = i * 64 + lane;
+            *reinterpret_cast<u32x4*>(&sv[b][(w * kPage + f / CPK) * VP + f % CPK * 8]) = vr[i];
         }
     };
     // Of a step whose keys not all rows see, V behind the last position becomes 0, and a V that is not finite too
@@ -227,11 +240,7 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
             }
         odd = __any(odd);
         if (lane == 0) s_odd[b][w] = odd;
-#pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            const int f = i * 64 + lane;
-            *reinterpret_cast<u32x4*>(&sv[b][(w * kPage + f / CPK) * VP + f % CPK * 8]) = vr[i];
-        }
+        put_v(b);
     };
     // bits: the step's pages whose word is set
     auto bits = [&](const int* f) {
@@ -239,6 +248,13 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
         return __builtin_amdgcn_readfirstlane((int)(v[0] | v[1] << 1 | v[2] << 2 | v[3] << 3));
     };
 
+    // whether every page of the segment is mapped
+    bool hole = false;
+    for (int i = tid; i < (k1 - k0 + kPage - 1) / kPage; i += 256) {
+        const int id = pt[k0 / kPage + i];
+        hole |= id < 0 || id >= a.kv.n_pages;
+    }
+    if (hole) set_err(a.err, CDB_DEV_UNMAPPED_PAGE);
     const int pid0 = page_of(0, entry_of(0));
     int entry = entry_of(1);
     fetch(kr, pid0, 0);
@@ -336,10 +352,12 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
     };
     // Half i (32 keys from k, scores in s): scores of the next one, weights of this one, products of the one before, which
     // do not depend on one another.  there: this half's two pages; odd: whether put_odd has to run for the one before.
-    auto run_half = [&](int i, int k, floatx16& s, floatx16& next, const uint16_t* k_next, const uint16_t* v_before, int there,
-                        bool odd) __attribute__((always_inline)) {
-        if (i > na) return;  // half na: nothing of it is seen
-        if (k + 31 > w_first || there != 3)
+    // PLAIN: every row sees all of this half and of the one before.
+    auto run_half = [&](auto plain, int i, int k, floatx16& s, floatx16& next, const uint16_t* k_next, const uint16_t* v_before,
+                        int there, bool odd) __attribute__((always_inline)) {
+        constexpr bool PLAIN = decltype(plain)::value;
+        if (PLAIN ? na < 0 : i > na) return;  // half na: nothing of it is seen
+        if (!PLAIN && (k + 31 > w_first || there != 3))
 #pragma unroll
             for (int j = 0; j < 16; ++j)
                 if (k + (j >> 2) * 8 + half * 4 + (j & 3) > qpos || !(there >> (j >> 3) & 1)) s[j] = -INFINITY;
@@ -368,7 +386,7 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
                 if constexpr (SPLIT) pl[st] = scaled(pl[st], corr);
             }
         }
-        const float m0 = m == -INFINITY ? 0.f : m;  // nothing seen yet: every weight 0
+        const float m0 = !PLAIN && m == -INFINITY ? 0.f : m;  // nothing seen yet: every weight 0
         const bf16x8 h[2] = {ph[0], ph[1]}, lo[2] = {pl[0], pl[1]};
 #pragma unroll
         for (int j = 0; j < 16; ++j) next[j] = 0.f;
@@ -392,7 +410,10 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
             ph[st] = __builtin_bit_cast(bf16x8, u32x4{hw[st * 4], hw[st * 4 + 1], hw[st * 4 + 2], hw[st * 4 + 3]});
             if constexpr (SPLIT) pl[st] = __builtin_bit_cast(bf16x8, u32x4{lw[st * 4], lw[st * 4 + 1], lw[st * 4 + 2], lw[st * 4 + 3]});
         }
-        if (odd) put_odd(k - 32);
+        // here, next to the products, and not sunk to where the weights are used
+        asm volatile("" : "+v"(ph[0]), "+v"(ph[1]), "+v"(l));
+        if constexpr (SPLIT) asm volatile("" : "+v"(pl[0]), "+v"(pl[1]));
+        if (!PLAIN && odd) put_odd(k - 32);
     };
 
     // V of the half before the first: zeros
@@ -405,33 +426,59 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
     entry = entry_of(2);
     fetch(kr, pid_k, 0);
     fetch(vr, pid_v, v_off);
-    __syncthreads();
+    const bool all_there = !__syncthreads_or(hole);
     if (na >= 0) s0 = scores(sk[0]);
-    int there = bits(s_there[0]), odd = 0;  // odd: of the step before
-    for (int t = 0, b = 0; t < steps; ++t, b ^= 1) {
-        const int k = k0 + t * kStep;
+    // A step's first half needs nothing that was staged since the last barrier, and its barrier stands before the
+    // second half, which needs K of the next step and V of this one.
+    int t = 0;
+    // steps that every row sees, with another such one behind them (its V is staged here) and two whole ones
+    const int plain = all_there ? min(steps - 3, (t_pos + 1 - k0) / kStep - 1) : 0;
+    auto plain_step = [&](auto buffer) __attribute__((always_inline)) {
+        constexpr int b = decltype(buffer)::value;
+        const std::true_type yes;
+        const int pid_next = entry;  // of step t + 2
+        entry = entry_of(t + 3);
+        put_k(b ^ 1);
+        fetch_page(kr, pid_next, 0);
+        run_half(yes, 2 * t, 0, s0, s1, sk[b] + 32 * KP, sv[b ^ 1] + 32 * VP, 3, false);
+        __syncthreads();
+        put_v(b ^ 1);
+        fetch_page(vr, pid_next, v_off);
+        run_half(yes, 2 * t + 1, 0, s1, s0, sk[b ^ 1], sv[b], 3, false);
+        ++t;
+    };
+    while (t + 2 <= plain) {
+        plain_step(std::integral_constant<int, 0>{});
+        plain_step(std::integral_constant<int, 1>{});
+    }
+    const int t_first = t;
+    int there = 15, odd = 0;  // odd: of the step before
+    if (t_first > 0)
+        pid_k = pid_v = 0;  // mapped, whichever it is
+    else
+        there = bits(s_there[0]);
+    for (; t < steps; ++t) {
+        const int k = k0 + t * kStep, b = t & 1;
         const bool more = t + 1 < steps;
-        // first half; the next step's K
+        const std::false_type no;
         const int pid_next = page_of(t + 2, entry);
+        entry = entry_of(t + 3);
         if (more) {
             stage_k(pid_k, b ^ 1);
             pid_k = pid_next;
             fetch(kr, pid_k, 0);
         }
-        entry = entry_of(t + 3);
-        run_half(2 * t, k, s0, s1, sk[b] + 32 * KP, sv[b ^ 1] + 32 * VP, there & 3, odd >> 2 & 3);
-        odd = bits(s_odd[b]);
+        run_half(no, 2 * t, k, s0, s1, sk[b] + 32 * KP, sv[b ^ 1] + 32 * VP, there & 3, odd >> 2 & 3);
         __syncthreads();
-        // second half; the next step's V
         const int there_next = bits(s_there[b ^ 1]);
+        odd = t == t_first && t > 0 ? 0 : bits(s_odd[b]);
         if (more) {
             stage_v(t + 1, pid_v, b ^ 1);
             pid_v = pid_next;
             fetch(vr, pid_v, v_off);
         }
-        run_half(2 * t + 1, k + 32, s1, s0, sk[b ^ 1], sv[b], there >> 2, odd & 3);
+        run_half(no, 2 * t + 1, k + 32, s1, s0, sk[b ^ 1], sv[b], there >> 2, odd & 3);
         there = there_next;
-        __syncthreads();
     }
     if (na == 2 * steps) {
         products(sv[(steps - 1) & 1] + 32 * VP);
