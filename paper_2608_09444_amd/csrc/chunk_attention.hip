@@ -391,6 +391,7 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) next[j] = 0.f;
         uint32_t hw[8], lw[8];
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
             if (t < NT) {
@@ -410,6 +411,7 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
             ph[st] = __builtin_bit_cast(bf16x8, u32x4{hw[st * 4], hw[st * 4 + 1], hw[st * 4 + 2], hw[st * 4 + 3]});
             if constexpr (SPLIT) pl[st] = __builtin_bit_cast(bf16x8, u32x4{lw[st * 4], lw[st * 4 + 1], lw[st * 4 + 2], lw[st * 4 + 3]});
         }
+        __builtin_amdgcn_s_setprio(0);
         // here, next to the products, and not sunk to where the weights are used
         asm volatile("" : "+v"(ph[0]), "+v"(ph[1]), "+v"(l));
         if constexpr (SPLIT) asm volatile("" : "+v"(pl[0]), "+v"(pl[1]));
