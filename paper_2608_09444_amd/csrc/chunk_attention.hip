@@ -9,16 +9,16 @@ namespace cdb {
 
 constexpr int kTileRows = 128;  // rows of a workgroup: 32 to each of its 4 waves
 constexpr int kNoVmem = 0xf70;   // s_waitcnt: vector memory loads 0, the others any
-constexpr int kMergeRows = 16;  // rows of a workgroup that joins segments
+constexpr int kFill = 64;       // positions of the shortest segments
 constexpr int kStep = 64;       // keys that a workgroup stages at a time, a page to each wave
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // Segments that a context of `keys` positions is cut into: as many as the launch wants to fill the
-// GPU (of 256 positions at least), and none longer than 2048 positions, as far as
+// GPU (of kFill positions at least), and none longer than 2048 positions, as far as
 // there are records for them.
 __host__ __device__ __forceinline__ int chunk_segments(int keys, const ChunkSplit& s, int* len) {
-    const int fill = (keys + 255) / 256;
+    const int fill = (keys + kFill - 1) / kFill;
     int n = (keys + 2047) / 2048;
     if (n < (fill < s.want ? fill : s.want)) n = fill < s.want ? fill : s.want;
     if (n > s.most) n = s.most;
@@ -32,7 +32,7 @@ ChunkSplit chunk_split(int H, int n_chunks, int n_rows, int max_pages) {
     s.want = std::max(1, (512 + tiles * H - 1) / std::max(1, tiles * H));
     s.most = std::max(1, std::min(kChunkSegments, kChunkRecordRows / std::max(1, n_rows)));
     const int64_t longest = (int64_t)max_pages * kPage;
-    if (longest <= 256 || (s.want == 1 && longest <= 2048)) s.most = 1;
+    if (longest <= kFill || (s.want == 1 && longest <= 2048)) s.most = 1;
     return s;
 }
 
@@ -60,6 +60,12 @@ struct ChunkTile {
     int seq, plane;
     int found;
 };
+
+// Whether a chunk of n rows is in range.
+__device__ __forceinline__ bool chunk_ok(const KvTarget& kv, int seq, int pos, int c, int n) {
+    return seq >= 0 && seq < kv.max_seqs && pos >= 0 && pos <= kv.max_pages * kPage - n &&
+           (!kv.c_row || (c >= 0 && c < kv.n_planes - 2));
+}
 
 // The from_last-th tile from the end (later tiles of a chunk see longer contexts,
 // so they come first).  Run by all 256 threads, thread = chunk; false: there is no
@@ -101,8 +107,7 @@ __device__ __forceinline__ bool chunk_tile(const ChunkAttnArgs& a, int from_last
     if (tile >= first && tile < first + nt) {
         const int n = r1 - r0, skip = (tile - first) * kTileRows;
         const int plane = a.kv.c_row ? c + 1 : a.kv.plane_fixed;
-        const bool ok = seq >= 0 && seq < a.kv.max_seqs && pos >= 0 && pos <= a.kv.max_pages * kPage - n &&
-                        (!a.kv.c_row || (c >= 0 && c < a.kv.n_planes - 2));
+        const bool ok = chunk_ok(a.kv, seq, pos, c, n);
         if (!ok) set_err(a.err, CDB_DEV_BAD_INDEX);
         *s_tile = ChunkTile{r0 + skip, min(kTileRows, n - skip), pos + skip, seq, plane, ok};
     }
@@ -152,7 +157,7 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
     __shared__ __align__(16) uint16_t sk[2][kStep * KP];
     __shared__ __align__(16) uint16_t sv[2][kStep * VP];
     __shared__ __align__(16) int s_there[2][4];  // by page of a step: whether it is mapped
-    __shared__ __align__(16) int s_odd[2][4];    // and holds V that stage_v took out
+    __shared__ int s_odd;                        // whether stage_v took something out
     __shared__ ChunkTile s_tile;
     __shared__ int s_red[4];
     int head, rest;
@@ -221,7 +226,7 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
         }
     };
     // Of a step whose keys not all rows see, V behind the last position becomes 0, and a V that is not finite too
-    // (put_odd adds it to the rows that see it).
+    // (at the end it is added to the rows that see it).
     auto stage_v = [&](int t, int pid, int b) __attribute__((always_inline)) {
         bool odd = false;
         if (k0 + t * kStep + kStep - 1 > t_pos && pid >= 0)
@@ -238,8 +243,7 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
                         if ((vr[i][x] & 0x7f800000u) == 0x7f800000u) vr[i][x] &= 0xffffu;
                     }
             }
-        odd = __any(odd);
-        if (lane == 0) s_odd[b][w] = odd;
+        if (odd) s_odd = 1;
         put_v(b);
     };
     // bits: the step's pages whose word is set
@@ -330,31 +334,11 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
 #pragma unroll
             for (int x = 0; x < NB; ++x) product(v, st, x, ph, pl);
     };
-    auto put_odd = [&](int from) __attribute__((always_inline)) {  // V of keys from .. from + 31 that stage_v took out
-#pragma unroll
-        for (int x = 0; x < NB; ++x) {
-            floatx16 more;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) more[j] = 0.f;
-#pragma unroll 1
-            for (int key = from; key < min(from + 32, last + 1); ++key) {
-                const int id = pt[key / kPage];
-                if (id < 0 || id >= a.kv.n_pages) continue;
-                const uint16_t* at = a.kv.pool + kv_offset(a.kv.layer, id, a.kv.n_pages, 1, head, a.H, key % kPage, HD) + half * 4;
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const uint16_t v = at[x * 32 + (j >> 2) * 8 + (j & 3)];
-                    if ((v & 0x7f80) == 0x7f80 && key <= qpos) more[j] += bf2f(v);
-                }
-            }
-            o[x] += more;
-        }
-    };
     // Half i (32 keys from k, scores in s): scores of the next one, weights of this one, products of the one before, which
-    // do not depend on one another.  there: this half's two pages; odd: whether put_odd has to run for the one before.
+    // do not depend on one another.  there: this half's two pages.
     // PLAIN: every row sees all of this half and of the one before.
     auto run_half = [&](auto plain, int i, int k, floatx16& s, floatx16& next, const uint16_t* k_next, const uint16_t* v_before,
-                        int there, bool odd) __attribute__((always_inline)) {
+                        int there) __attribute__((always_inline)) {
         constexpr bool PLAIN = decltype(plain)::value;
         if (PLAIN ? na < 0 : i > na) return;  // half na: nothing of it is seen
         if (!PLAIN && (k + 31 > w_first || there != 3))
@@ -415,9 +399,10 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
         // here, next to the products, and not sunk to where the weights are used
         asm volatile("" : "+v"(ph[0]), "+v"(ph[1]), "+v"(l));
         if constexpr (SPLIT) asm volatile("" : "+v"(pl[0]), "+v"(pl[1]));
-        if (!PLAIN && odd) put_odd(k - 32);
     };
 
+    if (tid == 0) s_odd = 0;
+    __syncthreads();
     // V of the half before the first: zeros
     for (int i = tid; i < 32 * VP / 8; i += 256) *reinterpret_cast<u32x4*>(&sv[1][32 * VP + i * 8]) = u32x4{0, 0, 0, 0};
     stage_k(pid0, 0);
@@ -442,11 +427,11 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
         entry = entry_of(t + 3);
         put_k(b ^ 1);
         fetch_page(kr, pid_next, 0);
-        run_half(yes, 2 * t, 0, s0, s1, sk[b] + 32 * KP, sv[b ^ 1] + 32 * VP, 3, false);
+        run_half(yes, 2 * t, 0, s0, s1, sk[b] + 32 * KP, sv[b ^ 1] + 32 * VP, 3);
         __syncthreads();
         put_v(b ^ 1);
         fetch_page(vr, pid_next, v_off);
-        run_half(yes, 2 * t + 1, 0, s1, s0, sk[b ^ 1], sv[b], 3, false);
+        run_half(yes, 2 * t + 1, 0, s1, s0, sk[b ^ 1], sv[b], 3);
         ++t;
     };
     while (t + 2 <= plain) {
@@ -454,7 +439,7 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
         plain_step(std::integral_constant<int, 1>{});
     }
     const int t_first = t;
-    int there = 15, odd = 0;  // odd: of the step before
+    int there = 15;
     if (t_first > 0)
         pid_k = pid_v = 0;  // mapped, whichever it is
     else
@@ -470,28 +455,47 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
             pid_k = pid_next;
             fetch(kr, pid_k, 0);
         }
-        run_half(no, 2 * t, k, s0, s1, sk[b] + 32 * KP, sv[b ^ 1] + 32 * VP, there & 3, odd >> 2 & 3);
+        run_half(no, 2 * t, k, s0, s1, sk[b] + 32 * KP, sv[b ^ 1] + 32 * VP, there & 3);
         __syncthreads();
         const int there_next = bits(s_there[b ^ 1]);
-        odd = t == t_first && t > 0 ? 0 : bits(s_odd[b]);
         if (more) {
             stage_v(t + 1, pid_v, b ^ 1);
             pid_v = pid_next;
             fetch(vr, pid_v, v_off);
         }
-        run_half(no, 2 * t + 1, k + 32, s1, s0, sk[b ^ 1], sv[b], there >> 2, odd & 3);
+        run_half(no, 2 * t + 1, k + 32, s1, s0, sk[b ^ 1], sv[b], there >> 2);
         there = there_next;
     }
     if (na == 2 * steps) {
         products(sv[(steps - 1) & 1] + 32 * VP);
-        if (odd >> 2) put_odd(k0 + steps * kStep - 32);
     }
 
     {
         const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
         l = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
+    __syncthreads();
     if (my >= t_n) return;
+    if (s_odd) {  // rare
+#pragma unroll
+        for (int x = 0; x < NB; ++x) {
+            floatx16 more;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) more[j] = 0.f;
+#pragma unroll 1
+            for (int key = max(k0, t_pos + 1 - kStep); key < k1; ++key) {
+                const int id = pt[key / kPage];
+                if (id < 0 || id >= a.kv.n_pages) continue;
+                const uint16_t* at = a.kv.pool + kv_offset(a.kv.layer, id, a.kv.n_pages, 1, head, a.H, key % kPage, HD) + half * 4;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const uint16_t v = at[x * 32 + (j >> 2) * 8 + (j & 3)];
+                    if ((v & 0x7f80) == 0x7f80 && key <= qpos) more[j] += bf2f(v);
+                }
+            }
+            o[x] += more;
+        }
+    }
     const int row = t_row + my;
     if (segs == 1) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -516,30 +520,41 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
                 make_float4(o[x][j], o[x][j + 1], o[x][j + 2], o[x][j + 3]);
 }
 
-// Segments of a tile's rows joined, in order.  Workgroup = (head, kMergeRows rows, tile).
+// Segments of a row joined, in order.  Workgroup = row; its threads take eight values of a head each.
 template <int HD>
 __global__ __launch_bounds__(256) void k_chunk_merge(ChunkAttnArgs a) {
-    __shared__ ChunkTile s_tile;
-    __shared__ int s_red[4];
-    const int head = blockIdx.x, part = blockIdx.y * kMergeRows;
-    if (!chunk_tile(a, blockIdx.z, &s_tile, s_red, false)) return;
-    const ChunkTile t = s_tile;
+    __shared__ int s_last;
+    const int tid = threadIdx.x, row = blockIdx.x;
+    if (tid == 0) s_last = -1;
+    int r0 = 0, r1 = 0;
+    if (tid < a.ch.n_chunks) {
+        r0 = a.ch.row0[tid];
+        r1 = a.ch.row0[tid + 1];
+    }
+    if (__syncthreads_or(r0 < 0 || r1 < r0 || r1 > a.ch.n_rows)) return;
+    if (row >= r0 && row < r1) {
+        const int seq = a.ch.seq[tid], pos = a.ch.pos0[tid], c = a.kv.c_row ? a.kv.c_row[tid] : 0, n = r1 - r0;
+        if (chunk_ok(a.kv, seq, pos, c, n)) s_last = pos + min(n, ((row - r0) / kTileRows + 1) * kTileRows) - 1;
+    }
+    __syncthreads();
+    if (s_last < 0) return;
     int seg_len;
-    const int segs = chunk_segments(t.pos + t.n, a.split, &seg_len);
+    const int segs = chunk_segments(s_last + 1, a.split, &seg_len);
     if (segs == 1) return;
-    constexpr int CPR = HD / 8;  // threads of a row
-    for (int i = threadIdx.x; i < min(t.n - part, kMergeRows) * CPR; i += 256) {
-        const int row = t.row + part + i / CPR, c = i % CPR;
-        const size_t rec = ((size_t)row * a.H + head) * a.split.most;
+    const int d = a.H * HD;
+    for (int i = tid; i < d / 8; i += 256) {
+        const size_t rec = ((size_t)row * a.H + i / (HD / 8)) * a.split.most;
+        const float* part = a.part + rec * HD + i % (HD / 8) * 8;
         float top = -INFINITY;
         for (int s = 0; s < segs; ++s) top = fmaxf(top, a.ml[rec + s].x);
         float num[8] = {}, den = 0.f;
         if (top > -INFINITY)
+#pragma unroll 4
             for (int s = 0; s < segs; ++s) {
                 const float2 x = a.ml[rec + s];
                 const float f = __builtin_amdgcn_exp2f(x.x - top);
                 den += f * x.y;
-                const float4* p = reinterpret_cast<const float4*>(a.part + (rec + s) * HD + c * 8);
+                const float4* p = reinterpret_cast<const float4*>(part + s * HD);
                 const float4 u = p[0], v = p[1];
                 const float y[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -549,17 +564,17 @@ __global__ __launch_bounds__(256) void k_chunk_merge(ChunkAttnArgs a) {
         u32x4 out;
 #pragma unroll
         for (int e = 0; e < 4; ++e) out[e] = pack_bf16(num[2 * e] * inv, num[2 * e + 1] * inv);
-        *reinterpret_cast<u32x4*>(chunk_out(a, row, head * HD + c * 8, a.H * HD)) = out;
+        *reinterpret_cast<u32x4*>(chunk_out(a, row, i * 8, d)) = out;
     }
 }
 
 template <int HD>
-static void launch_hd(const ChunkAttnArgs& a, bool split, int groups, int tiles, hipStream_t st) {
+static void launch_hd(const ChunkAttnArgs& a, bool split, int groups, hipStream_t st) {
     if (split)
         k_chunk_attn<HD, true><<<groups, 256, 0, st>>>(a);
     else
         k_chunk_attn<HD, false><<<groups, 256, 0, st>>>(a);
-    if (a.split.most > 1) k_chunk_merge<HD><<<dim3(a.H, kTileRows / kMergeRows, tiles), 256, 0, st>>>(a);
+    if (a.split.most > 1) k_chunk_merge<HD><<<a.ch.n_rows, 256, 0, st>>>(a);
 }
 
 hipError_t launch_chunk_attention(const cdb_chunks& ch, const KvTarget& kv, const void* q, int q_type, int H, int hd,
@@ -581,9 +596,9 @@ hipError_t launch_chunk_attention(const cdb_chunks& ch, const KvTarget& kv, cons
     const int tiles = std::min(ch.n_chunks, ch.n_rows) + ch.n_rows / kTileRows;
     const int groups = (a.xcd_heads ? a.xcd_heads * 8 : H) * tiles * a.split.most;
     switch (hd) {
-        case 64: launch_hd<64>(a, q_type == CDB_F32, groups, tiles, st); break;
-        case 96: launch_hd<96>(a, q_type == CDB_F32, groups, tiles, st); break;
-        case 128: launch_hd<128>(a, q_type == CDB_F32, groups, tiles, st); break;
+        case 64: launch_hd<64>(a, q_type == CDB_F32, groups, st); break;
+        case 96: launch_hd<96>(a, q_type == CDB_F32, groups, st); break;
+        case 128: launch_hd<128>(a, q_type == CDB_F32, groups, st); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
