@@ -10,16 +10,18 @@ namespace cdb {
 constexpr int kTileRows = 128;  // rows of a workgroup: 32 to each of its 4 waves
 constexpr int kNoVmem = 0xf70;   // s_waitcnt: vector memory loads 0, the others any
 constexpr int kFill = 64;       // positions of the shortest segments
+constexpr int kLong = 8192, kLongFew = 1536, kFewRows = 32;
+constexpr int kWant = 256;      // (tile, head, segment) triples that fill the GPU
 constexpr int kStep = 64;       // keys that a workgroup stages at a time, a page to each wave
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// Segments that a context of `keys` positions is cut into: as many as the launch wants to fill the
-// GPU (of kFill positions at least), and none longer than 2048 positions, as far as
-// there are records for them.
-__host__ __device__ __forceinline__ int chunk_segments(int keys, const ChunkSplit& s, int* len) {
-    const int fill = (keys + kFill - 1) / kFill;
-    int n = (keys + 2047) / 2048;
+// Segments that a chunk's context of `keys` positions is cut into: as many as the launch wants to fill the GPU (of kFill
+// positions at least), and none longer than kLong positions, or kLongFew where few rows make records
+// that cost little; as far as there are records for them.
+__host__ __device__ __forceinline__ int chunk_segments(int keys, int rows, const ChunkSplit& s, int* len) {
+    const int longest = rows <= kFewRows ? kLongFew : kLong, fill = (keys + kFill - 1) / kFill;
+    int n = (keys + longest - 1) / longest;
     if (n < (fill < s.want ? fill : s.want)) n = fill < s.want ? fill : s.want;
     if (n > s.most) n = s.most;
     *len = ((keys + n - 1) / n + kStep - 1) / kStep * kStep;
@@ -29,10 +31,11 @@ __host__ __device__ __forceinline__ int chunk_segments(int keys, const ChunkSpli
 ChunkSplit chunk_split(int H, int n_chunks, int n_rows, int max_pages) {
     ChunkSplit s{1, 1};
     const int tiles = std::max(n_chunks, (n_rows + kTileRows - 1) / kTileRows);
-    s.want = std::max(1, (512 + tiles * H - 1) / std::max(1, tiles * H));
+    s.want = std::max(1, (kWant + tiles * H - 1) / std::max(1, tiles * H));
     s.most = std::max(1, std::min(kChunkSegments, kChunkRecordRows / std::max(1, n_rows)));
-    const int64_t longest = (int64_t)max_pages * kPage;
-    if (longest <= kFill || (s.want == 1 && longest <= 2048)) s.most = 1;
+    // no more than the longest context that the tables hold is cut into: the grid has a workgroup for each
+    int len;
+    s.most = std::min(s.most, chunk_segments(std::max(1, max_pages * kPage), 1, s, &len));
     return s;
 }
 
@@ -53,11 +56,12 @@ struct ChunkAttnArgs {
     int* err;
 };
 
-// A tile of one chunk's rows.
+// A tile of one chunk's rows, and a segment of its context.
 struct ChunkTile {
     int row, n;     // first row in the call's buffers, rows
     int pos;        // position of the first row
     int seq, plane;
+    int seg, seg_len;
     int found;
 };
 
@@ -67,10 +71,10 @@ __device__ __forceinline__ bool chunk_ok(const KvTarget& kv, int seq, int pos, i
            (!kv.c_row || (c >= 0 && c < kv.n_planes - 2));
 }
 
-// The from_last-th tile from the end (later tiles of a chunk see longer contexts,
-// so they come first).  Run by all 256 threads, thread = chunk; false: there is no
-// such tile, or nothing is to be done for it.
-__device__ __forceinline__ bool chunk_tile(const ChunkAttnArgs& a, int from_last, ChunkTile* s_tile, int* s_red, bool tells) {
+// The work-th (tile, segment) pair from the end (later tiles of a chunk see longer contexts, so they come first).
+// Run by all 256 threads, thread = chunk; false: there is no such pair.  Workgroups without one come
+// last, when others have all of the work.
+__device__ __forceinline__ bool chunk_tile(const ChunkAttnArgs& a, int work, ChunkTile* s_tile, int* s_red, bool tells) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     int r0 = 0, r1 = 0, seq = -1, pos = 0, c = 0;
     if (tid < a.ch.n_chunks) {
@@ -81,15 +85,19 @@ __device__ __forceinline__ bool chunk_tile(const ChunkAttnArgs& a, int from_last
         if (a.kv.c_row) c = a.kv.c_row[tid];
     }
     const bool bad = r0 < 0 || r1 < r0 || r1 > a.ch.n_rows;
-    const int nt = bad ? 0 : (r1 - r0 + kTileRows - 1) / kTileRows;
-    int v = nt;
+    const int n = r1 - r0;
+    const bool ok = !bad && n > 0 && chunk_ok(a.kv, seq, pos, c, n);
+    if (tells && !bad && n > 0 && !ok) set_err(a.err, CDB_DEV_BAD_INDEX);
+    int len = 0;
+    const int segs = ok ? chunk_segments(pos + n, n, a.split, &len) : 0, works = ok ? (n + kTileRows - 1) / kTileRows * segs : 0;
+    int v = works;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const int u = __shfl_up(v, o, 64);
         if (lane >= o) v += u;
     }
     const bool any_bad = __any(bad);
-    if (lane == 63) s_red[w] = any_bad ? 1 << 20 : v;
+    if (lane == 63) s_red[w] = any_bad ? 1 << 24 : v;
     if (tid == 0) s_tile->found = 0;
     __syncthreads();
     int total = 0, before = 0;
@@ -98,18 +106,16 @@ __device__ __forceinline__ bool chunk_tile(const ChunkAttnArgs& a, int from_last
         if (i < w) before += s_red[i];
         total += s_red[i];
     }
-    if (total >= 1 << 20) {
+    if (total >= 1 << 24) {
         if (tells && tid == 0) set_err(a.err, CDB_DEV_BAD_INDEX);
         return false;
     }
-    const int tile = total - 1 - from_last, first = before + v - nt;
-    if (tile < 0) return false;
-    if (tile >= first && tile < first + nt) {
-        const int n = r1 - r0, skip = (tile - first) * kTileRows;
-        const int plane = a.kv.c_row ? c + 1 : a.kv.plane_fixed;
-        const bool ok = chunk_ok(a.kv, seq, pos, c, n);
-        if (!ok) set_err(a.err, CDB_DEV_BAD_INDEX);
-        *s_tile = ChunkTile{r0 + skip, min(kTileRows, n - skip), pos + skip, seq, plane, ok};
+    const int at = total - 1 - work, first = before + v - works;
+    if (at < 0) return false;
+    if (at >= first && at < first + works) {
+        const int tile = (at - first) / segs, skip = tile * kTileRows;
+        *s_tile = ChunkTile{r0 + skip, min(kTileRows, n - skip), pos + skip, seq, a.kv.c_row ? c + 1 : a.kv.plane_fixed,
+                            at - first - tile * segs, len, 1};
     }
     __syncthreads();
     return s_tile->found;
@@ -162,15 +168,14 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
     __shared__ int s_red[4];
     int head, rest;
     if (!chunk_head(a, blockIdx.x, &head, &rest)) return;
-    const int seg = rest % a.split.most;
-    if (!chunk_tile(a, rest / a.split.most, &s_tile, s_red, blockIdx.x == 0)) return;
+    if (!chunk_tile(a, rest, &s_tile, s_red, blockIdx.x == 0)) return;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int t_row = __builtin_amdgcn_readfirstlane(s_tile.row), t_n = __builtin_amdgcn_readfirstlane(s_tile.n);
     const int t_pos = __builtin_amdgcn_readfirstlane(s_tile.pos);
     const int last = t_pos + t_n - 1;  // the last position that any row sees
-    int seg_len;
-    const int segs = chunk_segments(last + 1, a.split, &seg_len);
+    const int seg = __builtin_amdgcn_readfirstlane(s_tile.seg), seg_len = __builtin_amdgcn_readfirstlane(s_tile.seg_len);
+    const int segs = (last + seg_len) / seg_len;  // of this tile
     if (seg >= segs) return;
     const int k0 = seg * seg_len, k1 = min(last + 1, k0 + seg_len);
     const int steps = (k1 - k0 + kStep - 1) / kStep;
@@ -523,9 +528,9 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
 // Segments of a row joined, in order.  Workgroup = row; its threads take eight values of a head each.
 template <int HD>
 __global__ __launch_bounds__(256) void k_chunk_merge(ChunkAttnArgs a) {
-    __shared__ int s_last;
+    __shared__ int s_segs;
     const int tid = threadIdx.x, row = blockIdx.x;
-    if (tid == 0) s_last = -1;
+    if (tid == 0) s_segs = 1;
     int r0 = 0, r1 = 0;
     if (tid < a.ch.n_chunks) {
         r0 = a.ch.row0[tid];
@@ -534,12 +539,14 @@ __global__ __launch_bounds__(256) void k_chunk_merge(ChunkAttnArgs a) {
     if (__syncthreads_or(r0 < 0 || r1 < r0 || r1 > a.ch.n_rows)) return;
     if (row >= r0 && row < r1) {
         const int seq = a.ch.seq[tid], pos = a.ch.pos0[tid], c = a.kv.c_row ? a.kv.c_row[tid] : 0, n = r1 - r0;
-        if (chunk_ok(a.kv, seq, pos, c, n)) s_last = pos + min(n, ((row - r0) / kTileRows + 1) * kTileRows) - 1;
+        if (chunk_ok(a.kv, seq, pos, c, n)) {
+            int len;
+            chunk_segments(pos + n, n, a.split, &len);
+            s_segs = (pos + min(n, ((row - r0) / kTileRows + 1) * kTileRows) + len - 1) / len;
+        }
     }
     __syncthreads();
-    if (s_last < 0) return;
-    int seg_len;
-    const int segs = chunk_segments(s_last + 1, a.split, &seg_len);
+    const int segs = s_segs;
     if (segs == 1) return;
     const int d = a.H * HD;
     for (int i = tid; i < d / 8; i += 256) {
