@@ -10,8 +10,8 @@ import ctypes as C
 
 import torch
 
-from . import CDB_ERR_CAPACITY, CdbError, _check, _ptr, cdb_kv, cdb_model_desc, cdb_workspace_init, lib as _lib
-from .tree import _flat, _held, _need, _stream, _tensor
+from . import CDB_ERR_CAPACITY, CDB_ERR_INVALID_ARG, CdbError, _check, _ptr, cdb_kv, cdb_model_desc, cdb_workspace_init, lib as _lib
+from .tree import _held, _need, _stream, _tensor
 
 EXPORTED = ("cdb_chunk_workspace_bytes", "cdb_chunk_qkv", "cdb_chunk_attention")
 
@@ -56,33 +56,34 @@ def cdb_chunk_workspace_bytes(desc: cdb_model_desc, max_rows: int, max_chunks: i
     return lib().cdb_chunk_workspace_bytes(C.byref(desc), max_rows, max_chunks)
 
 
-def _q_type(fn, t) -> int:
-    _need(fn, t.dtype in _TYPES)
-    return _TYPES[t.dtype]
+def _rows(fn, t, dtype, least) -> int:
+    """The address of a contiguous device tensor of this type (None: fp32 or bf16) with at least so many values."""
+    if not ((t.dtype is dtype if dtype else t.dtype in _TYPES) and t.is_cuda and t.numel() >= least and t.is_contiguous()):
+        raise CdbError(fn, CDB_ERR_INVALID_ARG)
+    return t.data_ptr()
 
 
 def cdb_chunk_qkv(desc: cdb_model_desc, kv: cdb_kv, chunks: cdb_chunks, stage: int, layer: int, qkv: cdb_qkv, q_out, ws,
                   stream=None):
     """q_out: device fp32 or bf16 [n_rows][d]."""
-    fn = "cdb_chunk_qkv"
-    _need(fn, getattr(qkv, "rows", chunks.n_rows) >= chunks.n_rows and getattr(qkv, "width", desc.d) == desc.d and
-          getattr(qkv, "head_dim", desc.head_dim) == desc.head_dim)
-    t = _q_type(fn, q_out)
-    at = _flat(fn, q_out, q_out.dtype, chunks.n_rows * desc.d)
-    _check(fn, lib().cdb_chunk_qkv(C.byref(desc), C.byref(kv), C.byref(chunks), stage, layer, C.byref(qkv), at, t,
-                                   ws.data_ptr(), ws.numel(), _stream(fn, stream, ws)))
+    fn, n, d = "cdb_chunk_qkv", chunks.n_rows, desc.d
+    rows, heads, head_dim = getattr(qkv, "shape", (n, desc.n_heads, desc.head_dim))  # structs made by hand are taken as they are
+    if rows < n or heads != desc.n_heads or head_dim != desc.head_dim:
+        raise CdbError(fn, CDB_ERR_INVALID_ARG)
+    to = _rows(fn, q_out, None, n * d)
+    _check(fn, lib().cdb_chunk_qkv(C.byref(desc), C.byref(kv), C.byref(chunks), stage, layer, C.byref(qkv), to,
+                                   _TYPES[q_out.dtype], ws.data_ptr(), ws.numel(), _stream(fn, stream, ws)))
 
 
 def cdb_chunk_attention(desc: cdb_model_desc, kv: cdb_kv, chunks: cdb_chunks, stage: int, layer: int, q, out, ws,
                         stream=None, order: int = CDB_ORDER_ROWS):
     """q: device fp32 or bf16 [n_rows][d]; out: device bf16 [n_rows][d], or, in CDB_ORDER_FRAGMENTS, of n_rows rounded up to
     32 rows."""
-    fn, n = "cdb_chunk_attention", chunks.n_rows
-    t = _q_type(fn, q)
-    qp = _flat(fn, q, q.dtype, n * desc.d)
-    op = _flat(fn, out, torch.bfloat16, (n if order == CDB_ORDER_ROWS else (n + 31) // 32 * 32) * desc.d)
-    _check(fn, lib().cdb_chunk_attention(C.byref(desc), C.byref(kv), C.byref(chunks), stage, layer, qp, t, op, order,
-                                         ws.data_ptr(), ws.numel(), _stream(fn, stream, ws)))
+    fn, n, d = "cdb_chunk_attention", chunks.n_rows, desc.d
+    at = _rows(fn, q, None, n * d)
+    to = _rows(fn, out, torch.bfloat16, (n if order == CDB_ORDER_ROWS else (n + 31) // 32 * 32) * d)
+    _check(fn, lib().cdb_chunk_attention(C.byref(desc), C.byref(kv), C.byref(chunks), stage, layer, at, _TYPES[q.dtype], to,
+                                         order, ws.data_ptr(), ws.numel(), _stream(fn, stream, ws)))
 
 
 # ---------------------------------------------------------------- device-memory holders (torch)
@@ -128,5 +129,4 @@ class QKV:
         strides = [t.stride(0) if n > 1 else H * hd for t in (q, k, v)]  # of one row any
         self.q, self.k, self.v, self.q_gain, self.k_gain, self.rope_pos = q, k, v, q_gain, k_gain, rope_pos
         self.c = _held(cdb_qkv(_ptr(q), _ptr(k), _ptr(v), _TYPES[q.dtype], int(bool(norm)), *strides, _ptr(q_gain),
-                               _ptr(k_gain), _ptr(rope_pos)), q, k, v, q_gain, k_gain, rope_pos, rows=n, width=H * hd,
-                       head_dim=hd)
+                               _ptr(k_gain), _ptr(rope_pos)), q, k, v, q_gain, k_gain, rope_pos, shape=(n, H, hd))
