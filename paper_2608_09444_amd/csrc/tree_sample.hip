@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256) void k_sample_stats(SampleArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         m = fmaxf(fmaxf(fmaxf(m, x[i].x), fmaxf(x[i].y, x[i].z)), x[i].w);
-        nan |= x[i].x != x[i].x || x[i].y != x[i].y || x[i].z != x[i].z || x[i].w != x[i].w;
+        nan |= __builtin_isunordered(x[i].x, x[i].y) || __builtin_isunordered(x[i].z, x[i].w);
     }
     m = wave_max(m);
     if (lane == 0) s_max[w] = m;
@@ -191,15 +191,17 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
     __shared__ double s_m[2][CDB_TREE_MAX_NODES], s_inv[2][CDB_TREE_MAX_NODES];  // each node's maximum x scale, 1 / sum
     __shared__ double s_z[CDB_TREE_MAX_NODES + 1];  // 1 / Z_k after k rejections at the current node
     __shared__ double s_seg[16];
-    __shared__ int s_out[CDB_TREE_MAX_NODES];  // the tokens of the rejections
+    __shared__ int s_out[CDB_TREE_MAX_NODES];       // the tokens of the rejections
+    __shared__ double s_drop[CDB_TREE_MAX_NODES];   // and, of a sure drafter, what each took out of r
+    __shared__ int s_exact;                         // whether s_sum is what the last of them left
     __shared__ int s_kid[CDB_TREE_MAX_NODES];  // whether the node has children
     __shared__ int s_cur, s_k, s_todo, s_pick[1];
     const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    if (a.round > 0 && a.done[t]) return;
     const bool dense = a.sm.draft_logits != nullptr, tells = blockIdx.x == 0;
     const int N = a.dr.max_nodes;
     const size_t at = (size_t)t * N + lane;
     // all that does not depend on another load
-    const int done = a.round > 0 ? a.done[t] : 0;
     const int r0 = a.row0[t];
     int n = a.dr.n_nodes[t], next = a.first_ids[t];
     const float temp = a.sm.temperature ? a.sm.temperature[t] : 1.f;
@@ -214,7 +216,6 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
         refused |= sq < 0 || sq >= a.dr.max_seqs;
         if (a.dr.len && !__any(refused)) refused = !tree_len_ok(a.dr.len[sq]);
     }
-    if (done) return;
     refused = __any(refused);
     const double scale[2] = {kLog2e / (double)temp, kLog2e / (double)dtemp};
     auto target_row = [&](int node) { return a.sm.logits + (size_t)(r0 + node) * a.sm.logits_stride; };
@@ -337,7 +338,8 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
     };
 
     int path = -1, count = 0, cur = -1, tried = -1, k = 0, rejected = 0;
-    bool bad = false, alone = !dense;
+    double mass = 1.0;  // what a sure drafter's rejections left of p
+    bool bad = false, alone = !dense, exact = dense;
     for (;;) {
         // the walk needs sums after a rejection (1), or a token (2), or is over (3)
         if (w == 0) {
@@ -357,23 +359,23 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
                 tried = j;
                 const int x = __builtin_amdgcn_readlane(token, j);
                 bool yes;
+                double r = pj;
                 if (cur < 0) {
                     yes = x == next;
                 } else {
-                    double r = pj;
                     if (dense) {
                         for (int s = 1; s <= k; ++s) r = fmax(r - qj, 0.0) * s_z[s];
                     } else {
                         for (int s = 0; s < k; ++s) r = s_out[s] == token ? 0.0 : r;
-                        if (k) r *= s_z[k];
                     }
-                    yes = __ballot(u * qj < r) >> j & 1;
+                    yes = __ballot(u * qj < (dense || !k ? r : r * s_z[k])) >> j & 1;
                 }
                 if (yes) {
                     if (lane == count) path = j;
                     ++count;
                     cur = j;
                     k = 0;
+                    mass = 1.0;
                 } else if (cur >= 0) {
                     if (lane == 0) s_out[k] = x;
                     ++k;
@@ -383,8 +385,19 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
                             --k;
                         else if (lane == 0)
                             s_z[k] = 1.0 / z;
-                    } else {
+                    } else if (dense) {
                         todo = 1;
+                    } else {
+                        const double gone = __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(r), j),
+                                                             __builtin_amdgcn_readlane(__double2loint(r), j));
+                        mass -= gone;
+                        // the difference keeps 40 bits as long as enough is left, else the rest is summed
+                        exact = mass < 1e-3;
+                        todo = exact;
+                        if (lane == 0) {
+                            s_drop[k - 1] = gone;
+                            if (!exact) s_z[k] = 1.0 / mass;
+                        }
                     }
                     ++rejected;
                 }
@@ -393,6 +406,7 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
                 s_cur = cur;
                 s_k = k;
                 s_todo = todo;
+                s_exact = exact;
             }
         }
         __syncthreads();
@@ -402,25 +416,28 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
             if (!tells) return;
             alone = true;
         }
-        if (todo == 3 || (todo == 2 && kk > 0)) break;  // after rejections the sums are there
+        if (todo == 3 || (todo == 2 && kk > 0 && s_exact)) break;  // the sums are there
         if (todo == 1 && dense && alone && a.round + 1 < a.rounds) return;  // the next round's
         const bool shared = todo == 1 && !alone;
         for (bool again = true; again;) {
             int from = 0, to = 0;
             if (todo == 1 && kk > 0) {
-                if (!dense)  // the piece of the token that is out (or in again) now
-                    from = s_out[s_k - 1] / kPiece, to = from + 1;
-                else if (shared && kk == s_k)
+                if (shared && kk == s_k)
                     from = blockIdx.x, to = from + 1;
                 else
                     to = a.pieces;
             }
-            if (kk == 0 || (!dense && kk == 1 && kk == s_k)) {  // from the statistics
+            if (todo == 2 || kk == 0) {  // from the statistics
                 for (int i = tid; i < a.pieces; i += 256) {
                     const double2 x = a.stats[(size_t)(r0 + c) * a.pieces + i];
                     s_sum[i] = x.x > -INFINITY ? x.y * exp2_64(fma(x.x, scale[0], -s_m[0][c])) * s_inv[0][c] : 0.0;
                 }
                 __syncthreads();
+                if (kk > 0) {  // without the tokens that are out
+                    if (tid == 0)
+                        for (int s = 0; s < kk; ++s) s_sum[s_out[s] / kPiece] -= s_drop[s];
+                    __syncthreads();
+                }
             }
             if (from < to) {
                 const float *tp = target_row(c), *tq = dense ? draft_row(c) : tp;
@@ -468,8 +485,9 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
                 }
             }
             again = false;
+            if (todo == 1) mass = total();
             if (todo == 1 && kk == s_k) {
-                const double z = total();
+                const double z = mass;
                 if (tid == 0 && a.round + 1 < a.rounds) a.left[(size_t)a.round * kTrees + t] = z;
                 if (z > 0.0) {
                     if (tid == 0) s_z[kk] = 1.0 / z;
