@@ -59,6 +59,10 @@ __device__ __forceinline__ double exp2_64(double y) {
     const double r = __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
     return EXACT && !(y >= -1000.0) ? 0.0 : r;
 }
+// With the denormal results too: a drafted token of the smallest probability is still a possible one.
+__device__ __forceinline__ double exp2_64_tail(double y) {
+    return y < -900.0 ? exp2_64(y + 200.0) * 0x1p-200 : exp2_64(y);
+}
 constexpr double kLog2e = 1.4426950408889634;
 
 __device__ __forceinline__ bool tree_len_ok(int l) { return l >= 0 && l <= 0x7fffffff - CDB_TREE_MAX_NODES; }
@@ -167,11 +171,12 @@ __global__ __launch_bounds__(256) void k_sample_stats(SampleArgs a) {
     m = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
     double s = nan || m == INFINITY ? NAN : 0.0;
     if (m > -INFINITY) {
-        const double mc = -scale * m;
+        // The difference first: the product of a mask's lowest value, or of a low temperature, is rounded in its whole places.
+        const double top = m;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            s += exp2_64<false>(fma((double)x[i].x, scale, mc)) + exp2_64<false>(fma((double)x[i].y, scale, mc));
-            s += exp2_64<false>(fma((double)x[i].z, scale, mc)) + exp2_64<false>(fma((double)x[i].w, scale, mc));
+            s += exp2_64<false>(((double)x[i].x - top) * scale) + exp2_64<false>(((double)x[i].y - top) * scale);
+            s += exp2_64<false>(((double)x[i].z - top) * scale) + exp2_64<false>(((double)x[i].w - top) * scale);
         }
     }
     s = wave_sum(s);
@@ -188,7 +193,7 @@ __global__ __launch_bounds__(256) void k_sample_stats(SampleArgs a) {
 __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
     extern __shared__ double s_sum[];  // [pieces] what is left of the target's probabilities at the current node
     double* s_part = s_sum + a.pieces; // [pieces][4] the waves' parts
-    __shared__ double s_m[2][CDB_TREE_MAX_NODES], s_inv[2][CDB_TREE_MAX_NODES];  // each node's maximum x scale, 1 / sum
+    __shared__ double s_m[2][CDB_TREE_MAX_NODES], s_inv[2][CDB_TREE_MAX_NODES];  // each node's maximum, 1 / sum
     __shared__ double s_z[CDB_TREE_MAX_NODES + 1];  // 1 / Z_k after k rejections at the current node
     __shared__ double s_seg[16];
     __shared__ int s_out[CDB_TREE_MAX_NODES];       // the tokens of the rejections
@@ -285,7 +290,7 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
             sum[z] += dpp64<0xb1>(sum[z]);
             sum[z] += dpp64<0x4e>(sum[z]);
             if (sub == 0) {
-                s_m[z][node] = top * scale[z];
+                s_m[z][node] = top;
                 s_inv[z][node] = top < INFINITY ? 1.0 / sum[z] : NAN;  // NaN or infinite: no distribution
             }
         }
@@ -295,8 +300,8 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
     uint64_t good_p = 0, good_q = 0;
     if (w == 0) {
         const int from = max(par, 0);
-        pj = exp2_64(fma((double)lp, scale[0], -s_m[0][from])) * s_inv[0][from];
-        if (dense) qj = exp2_64(fma((double)lq, scale[1], -s_m[1][from])) * s_inv[1][from];
+        pj = exp2_64_tail(((double)lp - s_m[0][from]) * scale[0]) * s_inv[0][from];
+        if (dense) qj = exp2_64_tail(((double)lq - s_m[1][from]) * scale[1]) * s_inv[1][from];
         good_p = __ballot(is_finite(s_inv[0][lane]));
         good_q = __ballot(!dense || is_finite(s_inv[1][lane]));
     }
@@ -304,15 +309,15 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
     // What is left of the target's probabilities of tokens i .. i + 3 after k rejections at node cur.
     auto left4 = [&](float4 x, float4 y, int i, int cur, int k, double (&r)[4]) {
         const float p[4] = {x.x, x.y, x.z, x.w};
-        const double m = -s_m[0][cur], inv = s_inv[0][cur];
+        const double m = s_m[0][cur], inv = s_inv[0][cur];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = exp2_64(fma((double)p[j], scale[0], m)) * inv;
+        for (int j = 0; j < 4; ++j) r[j] = exp2_64(((double)p[j] - m) * scale[0]) * inv;
         if (dense && k) {
             const float d[4] = {y.x, y.y, y.z, y.w};
-            const double mq = -s_m[1][cur], invq = s_inv[1][cur];
+            const double mq = s_m[1][cur], invq = s_inv[1][cur];
             double q[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) q[j] = exp2_64(fma((double)d[j], scale[1], mq)) * invq;
+            for (int j = 0; j < 4; ++j) q[j] = exp2_64(((double)d[j] - mq) * scale[1]) * invq;
             for (int s = 1; s < k; ++s)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) r[j] = fmax(r[j] - q[j], 0.0) * s_z[s];
@@ -391,8 +396,9 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
                         const double gone = __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(r), j),
                                                              __builtin_amdgcn_readlane(__double2loint(r), j));
                         mass -= gone;
-                        // the difference keeps 40 bits as long as enough is left, else the rest is summed
-                        exact = mass < 1e-3;
+                        // Probabilities are within 1.1e-12 of their values, the difference within 2^-33 of its own as
+                        // long as this much is left; else the rest is summed.
+                        exact = mass < 1.0 / 64;
                         todo = exact;
                         if (lane == 0) {
                             s_drop[k - 1] = gone;
@@ -430,13 +436,18 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
             if (todo == 2 || kk == 0) {  // from the statistics
                 for (int i = tid; i < a.pieces; i += 256) {
                     const double2 x = a.stats[(size_t)(r0 + c) * a.pieces + i];
-                    s_sum[i] = x.x > -INFINITY ? x.y * exp2_64(fma(x.x, scale[0], -s_m[0][c])) * s_inv[0][c] : 0.0;
+                    s_sum[i] = x.x > -INFINITY ? x.y * exp2_64((x.x - s_m[0][c]) * scale[0]) * s_inv[0][c] : 0.0;
                 }
                 __syncthreads();
                 if (kk > 0) {  // without the tokens that are out
-                    if (tid == 0)
+                    if (tid == 0) {
+                        bool thin = false;
                         for (int s = 0; s < kk; ++s) s_sum[s_out[s] / kPiece] -= s_drop[s];
+                        for (int s = 0; s < kk; ++s) thin |= s_sum[s_out[s] / kPiece] < 1e-9;
+                        s_exact = thin;
+                    }
                     __syncthreads();
+                    if (s_exact) to = a.pieces;  // what is left of a piece may be the rounding alone
                 }
             }
             if (from < to) {

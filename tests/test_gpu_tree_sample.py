@@ -234,6 +234,85 @@ def test_masked_logits_and_equal_distributions():
         assert not bad and c.code() == 0
 
 
+@pytest.mark.parametrize("dense", [True, False])
+def test_masks_of_the_lowest_value_and_low_temperatures(dense):
+    """Tokens masked with the lowest value of fp32 instead of -inf, whole stretches of the vocabulary among them, rows of
+    nothing else (the same for every token), temperatures from the smallest one up, and large logits."""
+    _say(f"lowest value dense={dense}")
+    lowest = np.finfo(np.float32).min
+    for seed in range(3):
+        c = Case(12320, 8, 7, 40 + seed, dense)
+        for x in (c.logits, c.draft) if dense else (c.logits,):
+            x[:, 4096:8192] = lowest
+            x[:, 12288:] = lowest
+        c.logits[-1] = lowest
+        c.tokens[:, 1:] = np.where((c.tokens[:, 1:] >= 4096) & (c.tokens[:, 1:] < 8192), 5, c.tokens[:, 1:]) % 12288
+        c.device()
+        c.run()
+        _, bad = c.check()
+        assert not bad and c.code() == 0
+        c.temp[:] = [2.0 ** -149, 1e-38, 1e-30, 1e-20, 1e-10, 1e-5, 1e-3, 1e30]
+        if dense:
+            c.dtemp[:] = c.temp[::-1]
+        c.device()
+        c.run()
+        _, bad = c.check()
+        assert not bad and c.code() == 0
+        c = Case(4128, 8, 7, 50 + seed, dense)
+        c.logits *= 1e30
+        c.device()
+        c.run()
+        _, bad = c.check()
+        assert not bad and c.code() == 0
+
+
+def test_sure_drafter_leaves_nothing_of_a_piece():
+    """Both possible tokens of the first 4096 are rejected; the smallest random number then falls on the first possible
+    token behind them, and so does none of what the differences of their probabilities leave by rounding."""
+    _say("nothing of a piece")
+    for seed in range(4):
+        c = Case(8192, 64, 3, 60 + seed, dense=False)
+        r = np.random.default_rng(seed)
+        c.n[:] = 3
+        c.row0 = (3 * np.arange(64)).astype(np.int32)
+        c.parent[:, 1:] = 0
+        c.M = 192
+        c.logits = r.normal(0, 2, (192, 8192)).astype(np.float32)
+        c.logits[:, 0:4200] = -np.inf
+        c.tokens[:, 1:] = r.permuted(np.tile(np.arange(4096), (64, 1)), axis=1)[:, :2]
+        for t in range(64):
+            c.logits[3 * t, c.tokens[t, 1:]] = 5 + r.normal(0, 1, 2)
+        c.first = c.tokens[:, 0].copy()
+        c.u_node[:] = 1 - 2.0 ** -24
+        c.u_next[:] = 0
+        c.device()
+        c.run()
+        count, bad = c.check()
+        assert not bad and (count == 1).all() and (c.acc.next.cpu().numpy() == 4200).all()
+
+
+def test_sure_drafter_with_little_left():
+    """Rejected tokens hold all but 1e-2 to 1e-9 of the probabilities."""
+    _say("little left")
+    for seed in range(6):
+        c = Case(8192, 28, 9, 70 + seed, dense=False, temps=False)
+        r = np.random.default_rng(seed)
+        c.n[:] = 9
+        c.row0 = (9 * np.arange(28)).astype(np.int32)
+        c.parent[:, 1:] = 0
+        c.M = 252
+        c.logits = r.normal(0, 1, (252, 8192)).astype(np.float32)
+        c.tokens[:, 1:] = r.integers(0, 8192, (28, 8))
+        for t in range(28):
+            c.logits[9 * t, c.tokens[t, 1:]] = r.uniform(12, 30, 8)
+        c.first = c.tokens[:, 0].copy()
+        c.u_node = r.uniform(1 - 2.0 ** -seed * 1e-2, 1, (28, 9)).astype(np.float32)
+        c.u_node = np.minimum(c.u_node, np.float32(1 - 2.0 ** -24))
+        c.device()
+        c.run()
+        c.check()
+
+
 def test_random_numbers_at_the_ends():
     _say("ends")
     for u in (0.0, 1 - 2.0 ** -24, 1.0):
