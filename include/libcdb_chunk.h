@@ -91,7 +91,8 @@ typedef struct {
  * rounded to bf16 and written to the cache at the row's position, in its plane of
  * stage `stage` (0 prelude, 1 core -> plane c + 1, 2 coda), layer `layer`; q written
  * to q_out [n_rows][d] as q_type (CDB_F32, CDB_BF16), which may be in->q itself where
- * types and strides (d) are the same.  Arithmetic and norms are in 32 bits, angles in
+ * types and strides (d) are the same, and otherwise lies apart from q, k and v
+ * (CDB_ERR_INVALID_ARG).  Arithmetic and norms are in 32 bits, angles in
  * 64.  A position of a plane belongs to one row of the call.  A row whose page is
  * not mapped writes q only (CDB_DEV_UNMAPPED_PAGE). */
 cdb_status cdb_chunk_qkv(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_chunks* chunks, int32_t stage,
@@ -101,8 +102,8 @@ cdb_status cdb_chunk_qkv(const cdb_model_desc* desc, const cdb_kv* kv, const cdb
 /* Causal attention: the row at position p of a chunk attends to positions 0..p of its
  * sequence in the chunk's plane,
  *   out[i][h] = softmax_s(q[i][h] . K_s / sqrt(head_dim)) V_s,
- * rounded to bf16.  q: [n_rows][d] of q_type; out: in the given order, rows outside every
- * (good) chunk left as they were.  Reads the cache only; the rows' own K/V must be in it.
+ * rounded to bf16.  q: [n_rows][d] of q_type; out: in the given order, apart from q, rows outside
+ * every (good) chunk left as they were.  Reads the cache only; the rows' own K/V must be in it.
  * With CDB_BF16 queries the weights are rounded to bf16 for the product with V; with
  * CDB_F32 both are taken in two bf16 parts (about 16 bits).  Sums and statistics are in 32
  * bits.
@@ -111,8 +112,9 @@ cdb_status cdb_chunk_qkv(const cdb_model_desc* desc, const cdb_kv* kv, const cdb
  * see them get no number or an infinity, and no other row changes.  An unmapped page is
  * left out (CDB_DEV_UNMAPPED_PAGE); a row that sees nothing gets zeros.  The stage's pool has
  * at least one page, however few are mapped.
- * A chunk's result does not depend on the other chunks; n_rows and n_chunks choose how
- * contexts are split, so roundings may differ between calls of different ones. */
+ * A chunk's result does not depend on the other chunks; n_rows, n_chunks and the table's
+ * max_pages choose how contexts are split, so roundings may differ between calls of
+ * different ones.  The same call gives the same bits. */
 cdb_status cdb_chunk_attention(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_chunks* chunks, int32_t stage,
                                int32_t layer, const void* q, int32_t q_type, void* out, int32_t out_order, void* ws,
                                size_t ws_bytes, hipStream_t stream);

@@ -236,7 +236,7 @@ typedef struct {
  * When no child is left, next is the first token whose cumulated r, from token 0 on, is above
  * u_next times the sum of r.  Probabilities and sums are in 64 bits.
  * The trees, row0, n_rows (at most 256 here) and `out` are as for cdb_tree_accept, with the
- * same refusals; a drafted token outside [0, vocab) is not accepted (CDB_DEV_BAD_INDEX).
+ * same refusals; no row belongs to two trees; a drafted token outside [0, vocab) is not accepted (CDB_DEV_BAD_INDEX).
  * A walk that comes to logits that are no distribution ends there, next = -1
  * (CDB_DEV_BAD_VALUE); a tree with a bad temperature accepts nothing (the same code). */
 cdb_status cdb_tree_sample(const cdb_model_desc* desc, const cdb_drafts* drafts, const int32_t* row0, int32_t n_rows,

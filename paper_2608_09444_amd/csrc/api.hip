@@ -802,6 +802,11 @@ size_t cdb_chunk_workspace_bytes(const cdb_model_desc* desc, int32_t max_rows, i
     return 256 + chunk_scratch_bytes(*desc, max_rows);
 }
 
+static bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + b_bytes && y < x + a_bytes;
+}
+
 // What both calls check; *t: the layer's cache.  *nothing: there are no rows.
 static cdb_status check_chunks(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_chunks* ch, int32_t stage,
                                int32_t layer, int32_t q_type, const void* ws, KvTarget* t, bool* nothing) {
@@ -841,6 +846,13 @@ cdb_status cdb_chunk_qkv(const cdb_model_desc* desc, const cdb_kv* kv, const cdb
         if (n < desc->d || n % per16) return CDB_ERR_INVALID_ARG;
     for (const void* p : {in->q, in->k, in->v, static_cast<const void*>(q_out), in->q_gain, in->k_gain})
         if (!aligned16(p)) return CDB_ERR_INVALID_ARG;
+    // q_out is in->q itself, row upon row, or lies apart from all three
+    const size_t bytes = in->type == CDB_F32 ? 4 : 2, n = (size_t)chunks->n_rows, to_bytes = n * desc->d * (q_type == CDB_F32 ? 4 : 2);
+    if (!(q_out == in->q && q_type == in->type && (in->q_stride == desc->d || n == 1)))
+        if (overlap(q_out, to_bytes, in->q, ((n - 1) * in->q_stride + desc->d) * bytes)) return CDB_ERR_INVALID_ARG;
+    if (overlap(q_out, to_bytes, in->k, ((n - 1) * in->k_stride + desc->d) * bytes) ||
+        overlap(q_out, to_bytes, in->v, ((n - 1) * in->v_stride + desc->d) * bytes))
+        return CDB_ERR_INVALID_ARG;
     HIPCHK(launch_chunk_qkv(*desc, *chunks, t, *in, q_out, q_type, static_cast<int*>(ws), st));
     return CDB_OK;
 }
@@ -856,6 +868,8 @@ cdb_status cdb_chunk_attention(const cdb_model_desc* desc, const cdb_kv* kv, con
     if (ws_bytes < 256 + chunk_scratch_bytes(*desc, chunks->n_rows)) return CDB_ERR_CAPACITY;
     if (nothing) return CDB_OK;
     if (!q || !out || !aligned16(q) || !aligned16(out)) return CDB_ERR_INVALID_ARG;
+    const size_t n = (size_t)chunks->n_rows, to_rows = out_order == CDB_ORDER_ROWS ? n : (n + 31) / 32 * 32;
+    if (overlap(out, to_rows * desc->d * 2, q, n * desc->d * (q_type == CDB_F32 ? 4 : 2))) return CDB_ERR_INVALID_ARG;
     HIPCHK(launch_chunk_attention(*chunks, t, q, q_type, desc->n_heads, desc->head_dim,
                                   static_cast<unsigned char*>(ws) + 256, static_cast<uint16_t*>(out), out_order,
                                   static_cast<int*>(ws), st));

@@ -55,7 +55,7 @@ def _chunks(**kw):
 
 
 def _qkv(**kw):
-    a = dict(q=16, k=16, v=16, type=1, norm=1, q_stride=256, k_stride=256, v_stride=256, q_gain=None, k_gain=None, rope=None)
+    a = dict(q=1 << 20, k=2 << 20, v=3 << 20, type=1, norm=1, q_stride=256, k_stride=256, v_stride=256, q_gain=None, k_gain=None, rope=None)
     a.update(kw)
     return chunk.cdb_qkv(*a.values())
 
@@ -64,7 +64,7 @@ def _write(desc=DESC, kv=KV, ch=_chunks(), stage=1, layer=0, qkv=_qkv(), q=16, q
     return _status("cdb_chunk_qkv", desc, kv, ch, stage, layer, qkv, q, q_type, ws, nb, None)
 
 
-def _attend(desc=DESC, kv=KV, ch=_chunks(), stage=1, layer=0, q=16, q_type=1, out=16, order=1, ws=16, nb=BIG):
+def _attend(desc=DESC, kv=KV, ch=_chunks(), stage=1, layer=0, q=16, q_type=1, out=1 << 20, order=1, ws=16, nb=BIG):
     return _status("cdb_chunk_attention", desc, kv, ch, stage, layer, q, q_type, out, order, ws, nb, None)
 
 
@@ -92,6 +92,11 @@ def test_qkv_refusals():
         assert _write(qkv=_qkv(**kw)) == INVALID, kw
     assert _write(qkv=_qkv(type=0, q_stride=258)) == INVALID
     assert _write(qkv=None) == INVALID
+    # q_out in part of what is read: 8 rows of 256 bf16 values are 4096 bytes
+    for q, kw in ((2 << 20, {}), ((2 << 20) + 4080, {}), ((3 << 20) - 4080, {}), ((1 << 20) + 16, {}), (1 << 20, {"q_stride": 768}),
+                  (1 << 20, {"type": 0}), ((3 << 20) + 7 * 1536 + 496, {"v_stride": 768}), (4096, {"q": 4096 + 4080})):
+        assert _write(q=q, qkv=_qkv(**kw)) == INVALID, (q, kw)
+    assert _write(q=1 << 20, q_type=0) == INVALID
 
 
 def test_attention_refusals():
@@ -99,6 +104,8 @@ def test_attention_refusals():
     for kw in ({"out": None}, {"out": 24}, {"order": 2}, {"order": -1}):
         assert _attend(**kw) == INVALID, kw
     assert _attend(nb=need - 1) == CAPACITY
+    for kw in ({"out": 16}, {"out": 4096}, {"out": 8192, "q_type": 0}, {"out": 1 << 20, "q": (1 << 20) + 16384 - 16, "order": 0}):
+        assert _attend(**kw) == INVALID, kw
 
 
 def _sample(desc=DESC, n_trees=2, n_rows=8, row0=16, first=16, out=tree.cdb_accepted(16, 16, 16), ws=16, nb=BIG, sm=True,
