@@ -332,14 +332,8 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
     // s_sum's total, the same bits in every thread
     auto total = [&]() {
         double z = 0.0;
-        if (a.pieces <= 32) {
-#pragma unroll 4
-            for (int i = 0; i < a.pieces; ++i) z += s_sum[i];
-        } else {
-            for (int i = lane; i < a.pieces; i += 64) z += s_sum[i];
-            z = wave_sum(z);
-        }
-        return z;
+        for (int i = lane; i < a.pieces; i += 64) z += s_sum[i];
+        return wave_sum(z);
     };
 
     int path = -1, count = 0, cur = -1, tried = -1, k = 0, rejected = 0;
@@ -520,31 +514,17 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
         const double aim = (double)un * total();
         double start = 0.0, before = 0.0;
         int piece = 0;
-        if (a.pieces <= 32) {
-            bool found = false;
-#pragma unroll 4
-            for (int i = 0; i < a.pieces; ++i) {
-                const double own = s_sum[i];
-                if (own > 0.0 && !found) {
-                    piece = i;
-                    start = before;
-                    found = before + own > aim;
-                }
-                before += own;
+        for (int i0 = 0; i0 < a.pieces; i0 += 64) {
+            const double own = i0 + lane < a.pieces ? s_sum[i0 + lane] : 0.0;
+            const double v = wave_scan(own);
+            const uint64_t hit = __ballot(before + v > aim && own > 0.0), some = __ballot(own > 0.0);
+            if (some) {
+                const int j = hit ? __ffsll((unsigned long long)hit) - 1 : 63 - __clzll((long long)some);
+                piece = i0 + j;
+                start = before + __shfl(v - own, j, 64);
+                if (hit) break;
             }
-        } else {
-            for (int i0 = 0; i0 < a.pieces; i0 += 64) {
-                const double own = i0 + lane < a.pieces ? s_sum[i0 + lane] : 0.0;
-                const double v = wave_scan(own);
-                const uint64_t hit = __ballot(before + v > aim && own > 0.0), some = __ballot(own > 0.0);
-                if (some) {
-                    const int j = hit ? __ffsll((unsigned long long)hit) - 1 : 63 - __clzll((long long)some);
-                    piece = i0 + j;
-                    start = before + __shfl(v - own, j, 64);
-                    if (hit) break;
-                }
-                before += __shfl(v, 63, 64);
-            }
+            before += __shfl(v, 63, 64);
         }
         const float *tp = target_row(c), *tq = dense ? draft_row(c) : tp;
         float4 p[4], q[4];
