@@ -529,19 +529,23 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
 }
 
 // Segments of a row joined, in order.  Workgroup = row; its threads take eight values of a head each.
+constexpr int kBatch = 8;  // records on their way at a time
 template <int HD>
 __global__ __launch_bounds__(256) void k_chunk_merge(ChunkAttnArgs a) {
     __shared__ int s_segs;
     const int tid = threadIdx.x, row = blockIdx.x;
     if (tid == 0) s_segs = 1;
-    int r0 = 0, r1 = 0;
+    int r0 = 0, r1 = 0, seq = -1, pos = 0, c = 0;
     if (tid < a.ch.n_chunks) {
         r0 = a.ch.row0[tid];
         r1 = a.ch.row0[tid + 1];
+        seq = a.ch.seq[tid];
+        pos = a.ch.pos0[tid];
+        if (a.kv.c_row) c = a.kv.c_row[tid];
     }
     if (__syncthreads_or(r0 < 0 || r1 < r0 || r1 > a.ch.n_rows)) return;
     if (row >= r0 && row < r1) {
-        const int seq = a.ch.seq[tid], pos = a.ch.pos0[tid], c = a.kv.c_row ? a.kv.c_row[tid] : 0, n = r1 - r0;
+        const int n = r1 - r0;
         if (chunk_ok(a.kv, seq, pos, c, n)) {
             int len;
             chunk_segments(pos + n, n, a.split, &len);
@@ -555,21 +559,36 @@ __global__ __launch_bounds__(256) void k_chunk_merge(ChunkAttnArgs a) {
     for (int i = tid; i < d / 8; i += 256) {
         const size_t rec = ((size_t)row * a.H + i / (HD / 8)) * a.split.most;
         const float* part = a.part + rec * HD + i % (HD / 8) * 8;
-        float top = -INFINITY;
-        for (int s = 0; s < segs; ++s) top = fmaxf(top, a.ml[rec + s].x);
-        float num[8] = {}, den = 0.f;
-        if (top > -INFINITY)
-#pragma unroll 4
-            for (int s = 0; s < segs; ++s) {
-                const float2 x = a.ml[rec + s];
-                const float f = __builtin_amdgcn_exp2f(x.x - top);
-                den += f * x.y;
-                const float4* p = reinterpret_cast<const float4*>(part + s * HD);
-                const float4 u = p[0], v = p[1];
-                const float y[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+        // every record is asked for before the first one is used: the kernel is a chain of memory latencies
+        float2 ml[kChunkSegments];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) num[e] += f * y[e];
-            }
+        for (int s = 0; s < kChunkSegments; ++s) ml[s] = s < segs ? a.ml[rec + s] : make_float2(-INFINITY, 0.f);
+        float num[8] = {}, den = 0.f, top = -INFINITY;
+#pragma unroll
+        for (int s0 = 0; s0 < kChunkSegments; s0 += kBatch) {
+            if (s0 >= segs) break;
+            float4 u[kBatch], v[kBatch];
+#pragma unroll
+            for (int s = 0; s < kBatch; ++s)
+                if (s0 + s < segs) {
+                    const float4* p = reinterpret_cast<const float4*>(part + (s0 + s) * HD);
+                    u[s] = p[0];
+                    v[s] = p[1];
+                }
+            if (s0 == 0)
+#pragma unroll
+                for (int s = 0; s < kChunkSegments; ++s) top = fmaxf(top, ml[s].x);
+            if (top == -INFINITY) break;
+#pragma unroll
+            for (int s = 0; s < kBatch; ++s)
+                if (s0 + s < segs) {
+                    const float f = __builtin_amdgcn_exp2f(ml[s0 + s].x - top);
+                    den += f * ml[s0 + s].y;
+                    const float y[8] = {u[s].x, u[s].y, u[s].z, u[s].w, v[s].x, v[s].y, v[s].z, v[s].w};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) num[e] += f * y[e];
+                }
+        }
         const float inv = den == 0.f ? 0.f : 1.f / den;
         u32x4 out;
 #pragma unroll
