@@ -1,5 +1,28 @@
 // Causal attention of chunks of new tokens (several sequences, one to thousands of
 // rows each) over the paged, depth-indexed KV cache.
+//
+//   out[i] = sum_{s <= p_i} 2^(x_is - m_i) V_s / sum_{s <= p_i} 2^(x_is - m_i),
+//   x_is = q_i . K_s log2(e) / sqrt(hd),
+//
+// in one pass over the keys, with a running m_i and both sums scaled as it grows.
+//
+// Bound: 4 hd operations per (row, key, head) at the matrix rate where chunks are
+// long, K and V once per chunk at the memory rate where they are short, and a chain of
+// latencies (chunk, page id, K, scores, weights, V, join) where there is little of either.
+// Workgroup = (head, tile of 128 rows, segment of the context), a wave to 32 rows: K and V
+// are staged in LDS once for four waves, and with 32x32x16 products an operand read from
+// LDS serves 32 rows.  S^T = K q^T leaves a row's scores in two lanes, so that maxima and sums
+// need one exchange, and in the registers that the second product takes its weights from.
+// The three parts of a half step (scores of the next 32 keys, weights of these, products
+// of the ones before) do not depend on one another and stand interleaved in one block: a
+// wave's exponentials run under its own products.  One barrier per 64 keys.
+//
+// Measured (bf16 q; us, with the join of segments): 4 chunks of 2048 rows behind 4096
+// positions, 16 x 128 heads: 346-365, 940-990 TFLOP/s (a large library product reaches 1220
+// here; the instructions of a half alone take 690 cycles, of which the products 512); 62 single rows
+// and 2 chunks of 700-1000 behind 2048-4100: 302-306, 5.6 TB/s of K and V; 9 chunks of
+// 33-333 behind up to 2047, 55 x 96 heads: 92-98, 510-540 TFLOP/s; 13 rows behind 700: 13-13.5,
+// latency; fp32 q, 512 rows behind 512: 29-34.
 #include <algorithm>
 #include <type_traits>
 
@@ -8,11 +31,21 @@
 namespace cdb {
 
 constexpr int kTileRows = 128;  // rows of a workgroup: 32 to each of its 4 waves
-constexpr int kNoVmem = 0xf70;   // s_waitcnt: vector memory loads 0, the others any
-constexpr int kFill = 64;       // positions of the shortest segments
-constexpr int kLong = 8192, kLongFew = 1536, kFewRows = 32;
-constexpr int kWant = 256;      // (tile, head, segment) triples that fill the GPU
+constexpr int kNoVmem = 0xf70;  // s_waitcnt: vector memory loads 0, the others any
 constexpr int kStep = 64;       // keys that a workgroup stages at a time, a page to each wave
+
+// How contexts are cut (us; 16 x 128 heads where nothing else is said).
+// Enough segments that there are kWant (tile, head, segment) triples, one to a compute unit: none against 256
+// against 1024 of them, 13 rows behind 700 21.3 / 13.5 / 13.9, 512 fp32 rows behind 512 46.5 / 33.4 / 36.9, 2
+// chunks of 700-1000 rows behind 2048-4100 89.4 / 71.9 / 75.4, 9 chunks of 33-333, 55 x 96 heads
+// 97 / 97 / 114, 2 of 1024 behind 2048, 55 x 96 heads 153 / 149 / 182.  Segments of kFill positions at least: of 512
+// the first two take 18.8 and 39.6.
+// Longer segments than kLong positions are cut whatever the launch's size, so that one long context does not
+// outlast the others; at 1536 the records cost long chunks more than that gives (62 rows and 2 chunks 347 against
+// 305, the last case above 187 against 149).  A chunk of kFewRows rows or fewer, one wave's, writes little of
+// them: 64 single rows behind 3000-4000 take 332 with kLongFew, 360 without.
+constexpr int kWant = 256, kFill = 64;
+constexpr int kLong = 8192, kLongFew = 1536, kFewRows = 32;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
@@ -123,7 +156,8 @@ __device__ __forceinline__ bool chunk_tile(const ChunkAttnArgs& a, int work, Chu
 
 // (head, rest) of a workgroup.  Workgroups go round the 8 XCDs by their index, so
 // with xcd_heads a head stays on one of them, whose L2 then holds its K and V for
-// all tiles.
+// all tiles (55 x 96 heads: 149 against 160 us for 2 chunks of 1024, 97 against 102 for 9 of
+// 33-333).  Taken while rounding the heads up to eights leaves at most an eighth of the workgroups idle.
 __device__ __forceinline__ bool chunk_head(const ChunkAttnArgs& a, int id, int* head, int* rest) {
     if (!a.xcd_heads) {
         *head = id % a.H;
@@ -426,7 +460,9 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
     // A step's first half needs nothing that was staged since the last barrier, and its barrier stands before the
     // second half, which needs K of the next step and V of this one.
     int t = 0;
-    // steps that every row sees, with another such one behind them (its V is staged here) and two whole ones
+    // Steps that every row sees, with another such one behind them (its V is staged here) and two whole ones: they
+    // need neither masks nor flags, and the buffers of two of them are constants (4 chunks of 2048 rows behind
+    // 4096: 360 us against 397 with the general steps alone).
     const int plain = all_there ? min(steps - 3, (t_pos + 1 - k0) / kStep - 1) : 0;
     auto plain_step = [&](auto buffer) __attribute__((always_inline)) {
         constexpr int b = decltype(buffer)::value;
@@ -528,7 +564,9 @@ __global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
                 make_float4(o[x][j], o[x][j + 1], o[x][j + 2], o[x][j + 3]);
 }
 
-// Segments of a row joined, in order.  Workgroup = row; its threads take eight values of a head each.
+// Segments of a row joined, in order: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  Workgroup = row; its threads
+// take eight values of a head each.  A launch of its own, 4.7-5.5 us for small calls of which 2 are its launch; a
+// join by the last workgroup of each (tile, head) was slower (13 rows behind 700: 14.3 against 13.1).
 constexpr int kBatch = 8;  // records on their way at a time
 template <int HD>
 __global__ __launch_bounds__(256) void k_chunk_merge(ChunkAttnArgs a) {
