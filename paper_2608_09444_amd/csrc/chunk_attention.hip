@@ -189,8 +189,13 @@ __device__ __forceinline__ bf16x8 scaled(bf16x8 p, float f) {
     return __builtin_bit_cast(bf16x8, w);
 }
 
-template <int HD, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void k_chunk_attn(ChunkAttnArgs a) {
+// PER_CU: workgroups that a compute unit can hold.  Two leave a wave 256 registers, 17 too few for heads of 128 with q in two
+// parts; one leaves it all it needs.  fp32 q, one against two (us; 16 heads): 2048 rows 74 / 91, 1024 behind 4096 96 / 114, 2
+// of 2048 behind 2048 214 / 234, 1024 rows 37 / 38, but 512 behind 512 35 / 34, 12 chunks of 100-300 94 / 84, 65 single
+// rows 363 / 340, where loads and starts are to be covered.  So long chunks take one (kLongChunk rows each on average).
+constexpr int kLongChunk = 1024;
+template <int HD, bool SPLIT, int PER_CU>
+__global__ __launch_bounds__(256, PER_CU) void k_chunk_attn(ChunkAttnArgs a) {
     constexpr int NT = HD / 16, NB = HD / 32, NL = HD / 32, CPK = HD / 8;
     constexpr int KP = HD + 8;                   // K row pitch: consecutive keys 4 banks apart (mod 64)
     constexpr int VP = HD == 96 ? HD : HD + 32;  // V row pitch: consecutive keys 16 banks apart (mod 64)
@@ -637,10 +642,12 @@ __global__ __launch_bounds__(256) void k_chunk_merge(ChunkAttnArgs a) {
 
 template <int HD>
 static void launch_hd(const ChunkAttnArgs& a, bool split, int groups, hipStream_t st) {
-    if (split)
-        k_chunk_attn<HD, true><<<groups, 256, 0, st>>>(a);
+    if (!split)
+        k_chunk_attn<HD, false, 2><<<groups, 256, 0, st>>>(a);
+    else if (HD == 128 && a.ch.n_rows / kLongChunk >= a.ch.n_chunks)
+        k_chunk_attn<HD, true, HD == 128 ? 1 : 2><<<groups, 256, 0, st>>>(a);
     else
-        k_chunk_attn<HD, false><<<groups, 256, 0, st>>>(a);
+        k_chunk_attn<HD, true, 2><<<groups, 256, 0, st>>>(a);
     if (a.split.most > 1) k_chunk_merge<HD><<<a.ch.n_rows, 256, 0, st>>>(a);
 }
 

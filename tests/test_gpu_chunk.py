@@ -261,6 +261,32 @@ def test_what_masked_places_hold_does_not_matter(dtype):
                 assert torch.isnan(hit).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_long_chunks(dtype):
+    """Steps that every row of a tile sees, among them keys that are no numbers and pages that are not mapped."""
+    _say(f"long chunks {dtype}")
+    chunks = _ragged((1100, 333), (1024, 0))
+    for H, hd in ((2, 128), (3, 96), (4, 64)):
+        c = Case(H, hd, chunks, seed=8, spare_rows=3).device()
+        clean, q = c.attend(dtype)
+        assert c.code() == 0 and (clean[-3:] == 77).all()
+        c.check(clean, q)
+        p, bad = 333, 700
+        for value in (math.nan, math.inf):
+            d = Case(H, hd, chunks, seed=8, spare_rows=3)
+            d.pool[1, d.table[0, 1, (p + bad) // PAGE], 1, :, (p + bad) % PAGE, 5] = value
+            got, _ = d.device().attend(dtype)
+            assert torch.equal(got[:bad], clean[:bad]) and torch.equal(got[1100:], clean[1100:])
+            hit = got[bad:1100].view(1100 - bad, H, hd)
+            assert not torch.isfinite(hit[:, :, 5]).any()
+            assert torch.isfinite(hit[:, :, [j for j in range(hd) if j != 5]]).all()
+        c.table[1, 2, 9] = -1
+        c.device()
+        got, q = c.attend(dtype)
+        assert c.code() == cdb.CDB_DEV_UNMAPPED_PAGE
+        c.check(got, q)
+
+
 def test_unmapped_pages_are_left_out():
     _say("unmapped pages")
     chunks = _ragged((5, 200), (1, 700), (140, 10), (2, 30))
