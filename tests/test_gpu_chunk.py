@@ -373,6 +373,39 @@ def test_offsets_past_32_bits():
     del big
 
 
+def test_most_rows_and_chunks():
+    _say("65536 rows")
+    r = np.random.default_rng(12)
+    c = Case(2, 64, [(256, int(p), i, i % 3) for i, p in enumerate(r.integers(0, 60, 256))], seed=12).device()
+    for dtype in (torch.bfloat16, torch.float32):
+        got, q = c.attend(dtype)
+        assert c.code() == 0
+        c.check(got, q, skip=[i for i in range(256) if i % 37 not in (0, 36)])
+
+
+def test_graphs_that_share_a_workspace():
+    """Two captured calls whose segments lie in one workspace, replayed in turn."""
+    _say("two graphs")
+    cases = [Case(H, hd, chunks, seed=13).device() for H, hd, chunks in
+             ((4, 64, _ragged((13, 700), (1, 300))), (2, 128, _ragged((3, 2000), (60, 5))))]
+    ws = max((c.ws for c in cases), key=lambda w: w.buf.numel())
+    clean, graphs, outs = [], [], []
+    for c in cases:
+        c.ws = ws
+        clean.append(c.attend()[0])
+        c.check(clean[-1], c.q.to(torch.bfloat16))
+        outs.append(torch.zeros((c.M, c.H * c.hd), dtype=torch.bfloat16, device="cuda"))
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            chunk.cdb_chunk_attention(c.desc, c.kv, c.c.c, c.stage, c.layer, c.d_q, outs[-1], ws.buf)
+    for _ in range(3):
+        for g, out, want in zip(graphs, outs, clean):
+            out.zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out.cpu(), want)
+
+
 def test_another_stream_and_a_captured_call():
     """A call on a side stream; a captured call replayed with other chunks of the same capacity, twice each."""
     _say("streams and graphs")

@@ -430,6 +430,37 @@ def test_streams_and_graphs():
         c.check()
 
 
+def test_graphs_that_share_a_workspace():
+    """Two captured calls, of a dense and of a sure drafter, on one workspace, replayed in turn with an eager one between."""
+    _say("two graphs")
+    cases = [Case(V, T, N, 23 + N, dense).device() for V, T, N, dense in ((8224, 9, 12, True), (4128, 20, 9, False),
+                                                                            (8224, 5, 4, True))]
+    for c in cases:
+        c.ws = cases[0].ws
+    graphs = []
+    for c in cases[:2]:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            c.run()
+    for _ in range(3):
+        for g, c in zip(graphs, cases):
+            c.acc.path.fill_(7)
+            c.acc.count.fill_(7)
+            g.replay()
+            c.check()
+        cases[2].run()
+        cases[2].check()
+
+
+@pytest.mark.parametrize("dense", [True, False])
+def test_largest_vocabulary(dense):
+    _say(f"largest vocabulary dense={dense}")
+    c = Case(1 << 20, 2, 5, 3, dense, near=1.5).device()
+    c.run()
+    _, bad = c.check()
+    assert not bad and c.code() == 0
+
+
 def test_tokens_are_distributed_as_the_target():
     """The token that follows a root, accepted or drawn, over 256 trees and 40 seeds against the target's probabilities:
     each of 32 counts of 10240 draws within 5 standard deviations.  The drafter is far off, with three guesses a tree."""
