@@ -47,6 +47,9 @@ constexpr int kStep = 64;       // keys that a workgroup stages at a time, a pag
 constexpr int kWant = 256, kFill = 64;
 constexpr int kLong = 8192, kLongFew = 1536, kFewRows = 32;
 
+// From here on a scaled score's last place is worth 64 and more.
+constexpr float kFar = 1073741824.f;
+
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // Segments that a chunk's context of `keys` positions is cut into: as many as the launch wants to fill the GPU (of kFill
@@ -343,6 +346,10 @@ __global__ __launch_bounds__(256, PER_CU) void k_chunk_attn(ChunkAttnArgs a) {
 #pragma unroll
     for (int x = 0; x < NB; ++x) o[x] = s0;
     float m = -INFINITY, l = 0.f;
+    // bf16 queries: m follows a score that is above lim; rows at kFar or beyond (far: which of the wave) have their maximum in
+    // lim, scores less it, and m = 0
+    float lim = -INFINITY;
+    uint64_t far = 0;
     bf16x8 ph[2], pl[2];  // weights of the half before
     ph[0] = ph[1] = pl[0] = pl[1] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
 
@@ -394,14 +401,30 @@ __global__ __launch_bounds__(256, PER_CU) void k_chunk_attn(ChunkAttnArgs a) {
         float mx = fmaxf(s[0], s[1]);
 #pragma unroll
         for (int j = 2; j < 16; ++j) mx = fmaxf(mx, s[j]);
+        float top;
         {
             const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-            mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * s_scale;
+            top = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
         }
-        const bool up = mx > m + 8.f;
-        if (__any(up)) {
-            const float now = up ? ceilf(mx) : m;
-            const float corr = up ? __builtin_amdgcn_exp2f(m - now) : 1.f;
+        mx = top * s_scale;
+        bool up = mx > (SPLIT ? m + 8.f : lim);
+        if ((__ballot(up) | far) != 0) {
+            const float limit = lim;
+            float was = m;
+            // A bf16 row's scores are scaled with the subtraction of the maximum, in one rounding, and against a maximum that was
+            // rounded itself the largest weight may be any 2^(half its last place).  So from kFar on a row's maximum is a
+            // quarter of its largest score, unscaled and exact: above (below, if negative) every other row's kind of maximum,
+            // and in the scores' own order.  Different scores are 64 powers of two apart there, so that only equal ones
+            // count, as many as there are, in one segment and where segments are joined.
+            if constexpr (!SPLIT) {
+                if (__builtin_expect((far | __ballot(fabsf(mx) >= kFar)) != 0, 0)) {
+                    was = fabsf(limit) >= kFar ? limit : was;
+                    mx = fabsf(mx) >= kFar ? top * 0.25f : mx;
+                    up = mx > limit;
+                }
+            }
+            const float now = up ? ceilf(mx) : was;
+            const float corr = up ? __builtin_amdgcn_exp2f(was - now) : 1.f;
             m = now;
             l *= corr;
 #pragma unroll
@@ -412,6 +435,16 @@ __global__ __launch_bounds__(256, PER_CU) void k_chunk_attn(ChunkAttnArgs a) {
             for (int st = 0; st < 2; ++st) {
                 ph[st] = scaled(ph[st], corr);
                 if constexpr (SPLIT) pl[st] = scaled(pl[st], corr);
+            }
+            if constexpr (!SPLIT) {
+                lim = now + 8.f;  // now itself from kFar on
+                const bool mine = fabsf(now) >= kFar && now > -INFINITY;
+                far = __ballot(mine);
+                if (__builtin_expect(far != 0, 0)) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) s[j] = mine ? fmaf(-4.f, now, s[j]) : s[j];
+                    m = mine ? 0.f : now;
+                }
             }
         }
         const float m0 = !PLAIN && m == -INFINITY ? 0.f : m;  // nothing seen yet: every weight 0
@@ -560,7 +593,7 @@ __global__ __launch_bounds__(256, PER_CU) void k_chunk_attn(ChunkAttnArgs a) {
         return;
     }
     const size_t rec = ((size_t)row * a.H + head) * a.split.most + seg;
-    if (half == 0) a.ml[rec] = make_float2(m, l);
+    if (half == 0) a.ml[rec] = make_float2(!SPLIT && fabsf(lim) >= kFar ? lim : m, l);
 #pragma unroll
     for (int x = 0; x < NB; ++x)
 #pragma unroll
