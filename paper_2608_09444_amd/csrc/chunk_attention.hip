@@ -654,11 +654,11 @@ __global__ __launch_bounds__(256) void k_chunk_merge(ChunkAttnArgs a) {
             if (s0 == 0)
 #pragma unroll
                 for (int s = 0; s < kChunkSegments; ++s) top = fmaxf(top, ml[s].x);
-            if (top == -INFINITY) break;
 #pragma unroll
             for (int s = 0; s < kBatch; ++s)
                 if (s0 + s < segs) {
-                    const float f = __builtin_amdgcn_exp2f(ml[s0 + s].x - top);
+                    // 1 where no segment has a score above -inf: sums are 0, or NaN where scores were
+                    const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[s0 + s].x - top);
                     den += f * ml[s0 + s].y;
                     const float y[8] = {u[s].x, u[s].y, u[s].z, u[s].w, v[s].x, v[s].y, v[s].z, v[s].w};
 #pragma unroll

@@ -103,3 +103,35 @@ def test_large_scores_leave_other_rows():
         got, _ = c.attend(q=big)
         assert torch.equal(got[~rows], clean[~rows])
         assert torch.isfinite(got).all()
+
+
+# one segment, and several that are joined
+@pytest.mark.parametrize("chunks", [_ragged((13, 0)), _ragged((13, 700)), _ragged((200, 300), (1, 500))], ids=str)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_query_that_is_no_number(dtype, chunks):
+    """Every score of the row is NaN, and so is the row, in however many segments; the others keep their bits."""
+    _say(f"NaN query {dtype} {chunks}")
+    for H, hd in ((4, 64), (3, 96), (2, 128)):
+        c = Case(H, hd, chunks, seed=45)
+        clean, _ = c.device().attend(dtype)
+        q = c.q.clone()
+        bad = torch.zeros(c.M, dtype=torch.bool)
+        bad[[5, c.M - 1]] = True
+        q.view(c.M, H, hd)[bad, :, 7] = math.nan
+        got, _ = c.attend(dtype, q=q)
+        assert c.code() == 0
+        assert torch.isnan(got[bad]).all()
+        assert torch.equal(got[~bad], clean[~bad])
+
+
+@pytest.mark.parametrize("n", [13, 128, 300])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_first_key_that_is_no_number(dtype, n):
+    """Every row sees it, the first one nothing else; 128 rows and more are cut into segments."""
+    _say(f"NaN key {dtype} {n}")
+    for H, hd in ((4, 64), (3, 96), (2, 128)):
+        c = Case(H, hd, [(n, 0, 0, 1)], seed=46)
+        c.pool[1, c.table[0, 2, 0], 0, :, 0, 5] = math.nan
+        got, _ = c.device().attend(dtype)
+        assert c.code() == 0
+        assert torch.isnan(got).all()
