@@ -251,7 +251,7 @@ __global__ __launch_bounds__(256, 3) void k_sample_walk(SampleArgs a) {
         live = false;
     }
     live = live && par < lane;
-    if (live && par >= 0 && (token < 0 || token >= a.V)) {
+    if (live && (token < 0 || token >= a.V)) {
         if (tells && w == 0) set_err(a.err, CDB_DEV_BAD_INDEX);
         live = false;
     }

@@ -496,3 +496,37 @@ def test_tokens_are_distributed_as_the_target():
         n = got.sum()
         assert n == 10240
         assert (np.abs(got - n * p) <= 5 * np.sqrt(n * p * (1 - p))).all()
+
+
+def test_roots_outside_the_vocabulary():
+    """A root's token outside [0, vocab) is not accepted, and told, also where the token already drawn is the same; a
+    good root behind it is taken."""
+    _say("roots")
+    for dense in (True, False):
+        for token in (-1, 256, 2 ** 31 - 1, -2 ** 31):
+            c = Case(256, 4, 6, 27, dense)
+            c.n[:] = 6
+            c.row0 = (6 * np.arange(4)).astype(np.int32)
+            c.M = 24
+            r = np.random.default_rng(27)
+            c.logits = r.normal(0, 2.5, (24, 256)).astype(np.float32)
+            c.draft = (c.logits + r.normal(0, 0.5, c.logits.shape)).astype(np.float32) if dense else None
+            c.first = c.tokens[:, 0].copy()
+            c.tokens[2, 0] = c.first[2] = token
+            c.device()
+            c.run()
+            torch.cuda.synchronize()
+            assert c.code() == cdb.CDB_DEV_BAD_INDEX
+            got = [x.cpu().numpy() for x in (c.acc.path, c.acc.count, c.acc.next)]
+            path, count, nxt, _ = c.want(refused=(2,))
+            assert nxt[2] == token and count[2] == 0
+            for a, b in zip(got, (path, count, nxt)):
+                assert np.array_equal(a, b)
+            # a second root
+            c.first[2] = 7
+            c.parent[2, 1] = -1
+            c.tokens[2, 1] = 7
+            c.device()
+            c.run()
+            c.check()
+            assert c.code() == cdb.CDB_DEV_BAD_INDEX
