@@ -52,16 +52,16 @@ constexpr float kFar = 1073741824.f;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// Segments that a chunk's context of `keys` positions is cut into: as many as the launch wants to fill the GPU (of kFill
-// positions at least), and none longer than kLong positions, or kLongFew where few rows make records
-// that cost little; as far as there are records for them.
-__host__ __device__ __forceinline__ int chunk_segments(int keys, int rows, const ChunkSplit& s, int* len) {
-    const int longest = rows <= kFewRows ? kLongFew : kLong, fill = (keys + kFill - 1) / kFill;
-    int n = (keys + longest - 1) / longest;
+// Segments that a chunk's context of `keys` positions (1 or more, up to 2^31 - 1) is cut into: as many as the launch wants to
+// fill the GPU (of kFill positions at least), and none longer than kLong positions, or kLongFew where few rows make records
+// that cost little; as far as there are records for them.  *len: positions of a segment, up to 2^31 of them.
+__host__ __device__ __forceinline__ int chunk_segments(int keys, int rows, const ChunkSplit& s, uint32_t* len) {
+    const int last = keys - 1, fill = last / kFill + 1;
+    int n = last / (rows <= kFewRows ? kLongFew : kLong) + 1;
     if (n < (fill < s.want ? fill : s.want)) n = fill < s.want ? fill : s.want;
     if (n > s.most) n = s.most;
-    *len = ((keys + n - 1) / n + kStep - 1) / kStep * kStep;
-    return (keys + *len - 1) / *len;
+    *len = ((uint32_t)(last / n) / kStep + 1) * kStep;
+    return (uint32_t)last / *len + 1;
 }
 
 ChunkSplit chunk_split(int H, int n_chunks, int n_rows, int max_pages) {
@@ -70,7 +70,7 @@ ChunkSplit chunk_split(int H, int n_chunks, int n_rows, int max_pages) {
     s.want = std::max(1, (kWant + tiles * H - 1) / std::max(1, tiles * H));
     s.most = std::max(1, std::min(kChunkSegments, kChunkRecordRows / std::max(1, n_rows)));
     // no more than the longest context that the tables hold is cut into: the grid has a workgroup for each
-    int len;
+    uint32_t len;
     s.most = std::min(s.most, chunk_segments(std::max(1, max_pages * kPage), 1, s, &len));
     return s;
 }
@@ -97,7 +97,8 @@ struct ChunkTile {
     int row, n;     // first row in the call's buffers, rows
     int pos;        // position of the first row
     int seq, plane;
-    int seg, seg_len;
+    int seg;
+    uint32_t seg_len;
     int found;
 };
 
@@ -124,7 +125,7 @@ __device__ __forceinline__ bool chunk_tile(const ChunkAttnArgs& a, int work, Chu
     const int n = r1 - r0;
     const bool ok = !bad && n > 0 && chunk_ok(a.kv, seq, pos, c, n);
     if (tells && !bad && n > 0 && !ok) set_err(a.err, CDB_DEV_BAD_INDEX);
-    int len = 0;
+    uint32_t len = 0;
     const int segs = ok ? chunk_segments(pos + n, n, a.split, &len) : 0, works = ok ? (n + kTileRows - 1) / kTileRows * segs : 0;
     int v = works;
 #pragma unroll
@@ -216,15 +217,17 @@ __global__ __launch_bounds__(256, PER_CU) void k_chunk_attn(ChunkAttnArgs a) {
     const int t_row = __builtin_amdgcn_readfirstlane(s_tile.row), t_n = __builtin_amdgcn_readfirstlane(s_tile.n);
     const int t_pos = __builtin_amdgcn_readfirstlane(s_tile.pos);
     const int last = t_pos + t_n - 1;  // the last position that any row sees
-    const int seg = __builtin_amdgcn_readfirstlane(s_tile.seg), seg_len = __builtin_amdgcn_readfirstlane(s_tile.seg_len);
-    const int segs = (last + seg_len) / seg_len;  // of this tile
+    const int seg = __builtin_amdgcn_readfirstlane(s_tile.seg);
+    const uint32_t seg_len = __builtin_amdgcn_readfirstlane(s_tile.seg_len);
+    const int segs = (uint32_t)last / seg_len + 1;  // of this tile
     if (seg >= segs) return;
-    const int k0 = seg * seg_len, k1 = min(last + 1, k0 + seg_len);
+    // positions reach 2^31 - 81, so that a step behind them does not pass 32 bits, and two do
+    const int k0 = seg * seg_len, k1 = min(last + 1u, k0 + seg_len);
     const int steps = (k1 - k0 + kStep - 1) / kStep;
     const int d = a.H * HD;
     const int my = w * 32 + c32;  // this lane's row in the tile
-    const int qpos = t_pos + my;
-    const int w_first = t_pos + w * 32;                         // position of the wave's first row
+    const int qpos = t_pos + min(my, t_n - 1);
+    const int w_first = t_pos + min(w * 32, t_n - 1);           // position of the wave's first row
     const int w_last = t_pos + min(t_n, w * 32 + 32) - 1;       // and of its last one
     const int na = w * 32 < t_n && w_last >= k0 ? min(2 * steps, (w_last - k0) / 32 + 1) : -1;  // halves with keys that it sees
     // the table by scalar loads: a page id is asked for a step before it is used, and vector loads would make its
@@ -235,9 +238,10 @@ __global__ __launch_bounds__(256, PER_CU) void k_chunk_attn(ChunkAttnArgs a) {
     // staging: wave w takes page w of a step
     u32x4 kr[NL], vr[NL];
     const int tables = a.kv.max_pages - 1;
-    auto entry_of = [&](int t) { return pt[min((k0 + t * kStep) / kPage + w, tables)]; };
+    const int page0 = k0 / kPage + w;
+    auto entry_of = [&](int t) { return pt[min(page0 + t * (kStep / kPage), tables)]; };
     auto page_of = [&](int t, int pid) {  // -2: behind the segment, -1: not mapped
-        return k0 + t * kStep + w * kPage >= k1 ? -2 : pid >= 0 && pid < a.kv.n_pages ? pid : -1;
+        return page0 + t * (kStep / kPage) > (k1 - 1) / kPage ? -2 : pid >= 0 && pid < a.kv.n_pages ? pid : -1;
     };
     const uint16_t* pool = a.kv.pool + kv_offset(a.kv.layer, 0, a.kv.n_pages, 0, head, a.H, 0, HD) + lane * 8;
     const size_t page_len = (size_t)2 * a.H * kPage * HD, v_off = (size_t)a.H * kPage * HD;
@@ -623,9 +627,9 @@ __global__ __launch_bounds__(256) void k_chunk_merge(ChunkAttnArgs a) {
     if (row >= r0 && row < r1) {
         const int n = r1 - r0;
         if (chunk_ok(a.kv, seq, pos, c, n)) {
-            int len;
+            uint32_t len;
             chunk_segments(pos + n, n, a.split, &len);
-            s_segs = (pos + min(n, ((row - r0) / kTileRows + 1) * kTileRows) + len - 1) / len;
+            s_segs = (uint32_t)(pos + min(n, ((row - r0) / kTileRows + 1) * kTileRows) - 1) / len + 1;
         }
     }
     __syncthreads();
