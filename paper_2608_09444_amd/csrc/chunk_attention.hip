@@ -52,14 +52,19 @@ constexpr float kFar = 1073741824.f;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// Segments that a chunk's context of `keys` positions (1 or more, up to 2^31 - 1) is cut into: as many as the launch wants to
+// Segments that a context of `keys` positions (1 or more, up to 2^31 - 1) is to be cut into: as many as the launch wants to
 // fill the GPU (of kFill positions at least), and none longer than kLong positions, or kLongFew where few rows make records
-// that cost little; as far as there are records for them.  *len: positions of a segment, up to 2^31 of them.
-__host__ __device__ __forceinline__ int chunk_segments(int keys, int rows, const ChunkSplit& s, uint32_t* len) {
+// that cost little.  Not fewer for a longer context or for fewer rows.
+__host__ __device__ __forceinline__ int segments_wanted(int keys, int rows, const ChunkSplit& s) {
     const int last = keys - 1, fill = last / kFill + 1;
-    int n = last / (rows <= kFewRows ? kLongFew : kLong) + 1;
-    if (n < (fill < s.want ? fill : s.want)) n = fill < s.want ? fill : s.want;
-    if (n > s.most) n = s.most;
+    const int n = last / (rows <= kFewRows ? kLongFew : kLong) + 1, filling = fill < s.want ? fill : s.want;
+    return n < filling ? filling : n;
+}
+
+// Segments that a chunk's context is cut into, as far as there are records for them.  *len: positions of a segment, whole
+// steps, up to 2^31 of them.
+__device__ __forceinline__ int chunk_segments(int keys, int rows, const ChunkSplit& s, uint32_t* len) {
+    const int last = keys - 1, n = min(segments_wanted(keys, rows, s), s.most);
     *len = ((uint32_t)(last / n) / kStep + 1) * kStep;
     return (uint32_t)last / *len + 1;
 }
@@ -69,9 +74,8 @@ ChunkSplit chunk_split(int H, int n_chunks, int n_rows, int max_pages) {
     const int tiles = std::max(n_chunks, (n_rows + kTileRows - 1) / kTileRows);
     s.want = std::max(1, (kWant + tiles * H - 1) / std::max(1, tiles * H));
     s.most = std::max(1, std::min(kChunkSegments, kChunkRecordRows / std::max(1, n_rows)));
-    // no more than the longest context that the tables hold is cut into: the grid has a workgroup for each
-    uint32_t len;
-    s.most = std::min(s.most, chunk_segments(std::max(1, max_pages * kPage), 1, s, &len));
+    // no more than the longest context that the tables hold may be cut into: the grid has a workgroup for each
+    s.most = std::min(s.most, segments_wanted(std::max(1, max_pages * kPage), 1, s));
     return s;
 }
 

@@ -32,3 +32,10 @@ def test_every_table_has_segments_that_records_hold(heads, chunks, rows):
         want, most = split(heads, chunks, rows, pages)
         assert 1 <= want and 1 <= most <= MOST_SEGMENTS, pages
         assert most == 1 or most * rows <= RECORD_ROWS, pages
+
+
+@pytest.mark.parametrize("heads,chunks,rows", CALLS)
+def test_a_wider_table_has_no_fewer_segments(heads, chunks, rows):
+    """What a table could hold takes no segments from shorter contexts in it."""
+    most = [split(heads, chunks, rows, pages)[1] for pages in (*range(1, 4000), *range(4000, 20000, 37), *FAR)]
+    assert all(b >= a for a, b in zip(most, most[1:]))
