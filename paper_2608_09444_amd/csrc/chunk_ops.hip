@@ -46,8 +46,9 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
 }
 
 // Workgroup = (row, kTasks of its 3 H heads of q, k and v).  Eight lanes (four for heads of 64) take one head: a
-// lane 8 values of its first half and the 8 that are rotated with them.  The values are asked for first, so
-// that they come while the row's chunk, its page and its angles are found.  Two heads to a group of lanes: the angles
+// lane 8 values of its first half and the 8 that are rotated with them.  Chunks follow one another, so the ends of
+// row0 tell by scalar loads whether any has the row; then its values are asked for, so that they come
+// while its chunk, its page and its angles are found.  Two heads to a group of lanes: the angles
 // (in 64 bits: a position of 10^5 keeps 2^-24 of a turn) and the search are paid once for 64 heads of 128, and enough
 // workgroups are left.  1, 2, 4 heads: 8 rows 7.3, 6.8, 7.2 us; 7 ragged chunks 18.7, 17.1, 17.5; 16 prompts 33.0, 31.6, 36.4.
 constexpr int kTasks = 2;
@@ -59,6 +60,9 @@ __global__ __launch_bounds__(256) void k_chunk_qkv(QkvArgs a) {
     __shared__ float2 s_cs[HALF];
     const int tid = threadIdx.x, row = blockIdx.x, e = tid % G;
     const bool on = e * 16 < HD;  // heads of 96 leave two of eight lanes idle
+    const auto* ends = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)a.ch.row0;
+    const bool outside = row < ends[0] || row >= ends[a.ch.n_chunks];
+    if (outside && blockIdx.x + blockIdx.y != 0) return;  // the first workgroup tells what is wrong with row0
     if (tid == 0) s_pos = -1;
     int r0 = 0, r1 = 0, seq = -1, pos = 0, c = 0;
     if (tid < a.ch.n_chunks) {
@@ -74,7 +78,7 @@ __global__ __launch_bounds__(256) void k_chunk_qkv(QkvArgs a) {
         const int i = (blockIdx.y * kTasks + t) * NG + tid / G, head = i % a.H, part = i / a.H;
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[t][k] = y[t][k] = 0.f;
-        if (on && part < 3) {
+        if (on && part < 3 && !outside) {
             const int64_t stride = part == 0 ? a.in.q_stride : part == 1 ? a.in.k_stride : a.in.v_stride;
             const IN* src = static_cast<const IN*>(part == 0 ? a.in.q : part == 1 ? a.in.k : a.in.v) + row * stride + head * HD + e * 8;
             load8(src, x[t]);

@@ -1,10 +1,12 @@
-"""GPU: calls over chunks with page tables of the largest size, and at the last positions that those have."""
+"""GPU: calls over chunks with page tables of the largest size, at the last positions that those have, and with buffers of
+many more rows than chunks."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2608_09444_amd as cdb
-from test_gpu_chunk import PAGE, Case, Write, _say
+from paper_2608_09444_amd import chunk
+from test_gpu_chunk import PAGE, Case, Write, _dev, _say
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +59,33 @@ def test_the_last_positions_of_the_widest_table(dtype):
     w.run()
     assert c.code() == 0
     w.check()
+
+
+def test_rows_outside_chunks_are_not_read():
+    """65536 rows of three parts, 16 x 128 values of 4 bytes each, are 1.6 GB: 0.2 ms at the 8 TB/s that this memory cannot
+    exceed.  A call in which chunks have 13 of the rows takes less than 0.6 of that, from its first rows to its last."""
+    _say("rows that nobody has")
+    H, hd, n, M = 16, 128, 13, 65536
+    c = Case(H, hd, [(n, 40, 0, 0)], seed=63).device()
+    x = torch.randn((M, 3, H, hd), device="cuda")
+    qkv = chunk.QKV(*x.unbind(1), norm=True)
+    q_out = torch.zeros((M, H * hd), device="cuda")
+    for first in (0, 1000, M - n):
+        c.c = chunk.Chunks(M, _dev([first, first + n]), c.c.seq, c.c.pos0, c.c.cc)
+        q_out.fill_(77.0)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for _ in range(4):
+                chunk.cdb_chunk_qkv(c.desc, c.kv, c.c.c, 1, 1, qkv.c, q_out, c.ws.buf)
+        took = []
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            graph.replay()
+            b.record()
+            torch.cuda.synchronize()
+            took.append(a.elapsed_time(b) / 4)
+        assert c.code() == 0
+        assert (q_out[first:first + n] != 77).all()
+        assert (q_out[:first] == 77).all() and (q_out[first + n:] == 77).all()
+        assert min(took) < 0.6 * x.numel() * 4 / 8e12 * 1e3, took
