@@ -91,8 +91,8 @@ typedef struct {
  * rounded to bf16 and written to the cache at the row's position, in its plane of
  * stage `stage` (0 prelude, 1 core -> plane c + 1, 2 coda), layer `layer`; q written
  * to q_out [n_rows][d] as q_type (CDB_F32, CDB_BF16), which may be in->q itself where
- * types and strides (d) are the same, and otherwise lies apart from q, k and v
- * (CDB_ERR_INVALID_ARG).  Arithmetic and norms are in 32 bits, angles in
+ * types and strides (d) are the same, and otherwise lies apart from q, k and v; all of
+ * them lie apart from the stage's pool (CDB_ERR_INVALID_ARG).  Arithmetic and norms are in 32 bits, angles in
  * 64.  A position of a plane belongs to one row of the call.  A row whose page is
  * not mapped writes q only (CDB_DEV_UNMAPPED_PAGE). */
 cdb_status cdb_chunk_qkv(const cdb_model_desc* desc, const cdb_kv* kv, const cdb_chunks* chunks, int32_t stage,
@@ -102,7 +102,7 @@ cdb_status cdb_chunk_qkv(const cdb_model_desc* desc, const cdb_kv* kv, const cdb
 /* Causal attention: the row at position p of a chunk attends to positions 0..p of its
  * sequence in the chunk's plane,
  *   out[i][h] = softmax_s(q[i][h] . K_s / sqrt(head_dim)) V_s,
- * rounded to bf16.  q: [n_rows][d] of q_type; out: in the given order, apart from q, rows outside
+ * rounded to bf16.  q: [n_rows][d] of q_type; out: in the given order, apart from q and the stage's pool, rows outside
  * every (good) chunk left as they were.  Reads the cache only; the rows' own K/V must be in it.
  * With CDB_BF16 queries the weights are rounded to bf16 for the product with V; with
  * CDB_F32 both are taken in two bf16 parts (about 16 bits).  Sums and statistics are in 32

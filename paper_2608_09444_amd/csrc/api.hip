@@ -846,13 +846,20 @@ cdb_status cdb_chunk_qkv(const cdb_model_desc* desc, const cdb_kv* kv, const cdb
         if (n < desc->d || n % per16) return CDB_ERR_INVALID_ARG;
     for (const void* p : {in->q, in->k, in->v, static_cast<const void*>(q_out), in->q_gain, in->k_gain})
         if (!aligned16(p)) return CDB_ERR_INVALID_ARG;
-    // q_out is in->q itself, row upon row, or lies apart from all three
+    // q_out is in->q itself, row upon row, or lies apart from all three; the cache lies apart from all four
     const size_t bytes = in->type == CDB_F32 ? 4 : 2, n = (size_t)chunks->n_rows, to_bytes = n * desc->d * (q_type == CDB_F32 ? 4 : 2);
-    if (!(q_out == in->q && q_type == in->type && (in->q_stride == desc->d || n == 1)))
-        if (overlap(q_out, to_bytes, in->q, ((n - 1) * in->q_stride + desc->d) * bytes)) return CDB_ERR_INVALID_ARG;
-    if (overlap(q_out, to_bytes, in->k, ((n - 1) * in->k_stride + desc->d) * bytes) ||
-        overlap(q_out, to_bytes, in->v, ((n - 1) * in->v_stride + desc->d) * bytes))
-        return CDB_ERR_INVALID_ARG;
+    const size_t cache = t.n_pages * cdb_kv_page_bytes(desc, stage);
+    const bool in_place = q_out == in->q && q_type == in->type && (in->q_stride == desc->d || n == 1);
+    const struct {
+        const void* at;
+        int64_t stride;
+    } parts[3] = {{in->q, in->q_stride}, {in->k, in->k_stride}, {in->v, in->v_stride}};
+    for (int i = 0; i < 3; ++i) {
+        const size_t part = ((n - 1) * parts[i].stride + desc->d) * bytes;
+        if (!(i == 0 && in_place) && overlap(q_out, to_bytes, parts[i].at, part)) return CDB_ERR_INVALID_ARG;
+        if (overlap(t.pool, cache, parts[i].at, part)) return CDB_ERR_INVALID_ARG;
+    }
+    if (overlap(t.pool, cache, q_out, to_bytes)) return CDB_ERR_INVALID_ARG;
     HIPCHK(launch_chunk_qkv(*desc, *chunks, t, *in, q_out, q_type, static_cast<int*>(ws), st));
     return CDB_OK;
 }
@@ -869,7 +876,9 @@ cdb_status cdb_chunk_attention(const cdb_model_desc* desc, const cdb_kv* kv, con
     if (nothing) return CDB_OK;
     if (!q || !out || !aligned16(q) || !aligned16(out)) return CDB_ERR_INVALID_ARG;
     const size_t n = (size_t)chunks->n_rows, to_rows = out_order == CDB_ORDER_ROWS ? n : (n + 31) / 32 * 32;
-    if (overlap(out, to_rows * desc->d * 2, q, n * desc->d * (q_type == CDB_F32 ? 4 : 2))) return CDB_ERR_INVALID_ARG;
+    if (overlap(out, to_rows * desc->d * 2, q, n * desc->d * (q_type == CDB_F32 ? 4 : 2)) ||
+        overlap(out, to_rows * desc->d * 2, t.pool, t.n_pages * cdb_kv_page_bytes(desc, stage)))
+        return CDB_ERR_INVALID_ARG;
     HIPCHK(launch_chunk_attention(*chunks, t, q, q_type, desc->n_heads, desc->head_dim,
                                   static_cast<unsigned char*>(ws) + 256, static_cast<uint16_t*>(out), out_order,
                                   static_cast<int*>(ws), st));
