@@ -189,13 +189,17 @@ def cdb_tree_accept(drafts: cdb_drafts, row0, next_ids, first_ids, out: cdb_acce
 
 
 def cdb_tree_sample(desc: cdb_model_desc, drafts: cdb_drafts, row0, first_ids, sampling: cdb_sampling, out: cdb_accepted,
-                    ws, stream=None):
-    """row0, first_ids: device int32 [n_trees].  drafts: as for cdb_tree_accept."""
+                    ws, stream=None, n_rows: int | None = None):
+    """row0, first_ids: device int32 [n_trees].  drafts: as for cdb_tree_accept.  n_rows: rows of the logits, None: those of
+    Sampling's (a cdb_sampling made by hand does not know them)."""
     _trees_fit("cdb_tree_sample", drafts, out)
     _trees_fit("cdb_tree_sample", drafts, sampling)
     _need("cdb_tree_sample", getattr(sampling, "vocab", desc.vocab) == desc.vocab)
+    rows = getattr(sampling, "n_rows", n_rows)
+    n = rows if n_rows is None else n_rows
+    _need("cdb_tree_sample", n is not None and n <= rows)
     at, first = (_flat("cdb_tree_sample", t, torch.int32, drafts.n_trees) for t in (row0, first_ids))
-    _check("cdb_tree_sample", lib().cdb_tree_sample(C.byref(desc), C.byref(drafts), at, sampling.n_rows, first,
+    _check("cdb_tree_sample", lib().cdb_tree_sample(C.byref(desc), C.byref(drafts), at, n, first,
                                                     C.byref(sampling), C.byref(out), ws.data_ptr(), ws.numel(),
                                                     _stream("cdb_tree_sample", stream, ws)))
 
