@@ -11,7 +11,7 @@ import ctypes as C
 import torch
 
 from . import CDB_ERR_CAPACITY, CDB_ERR_INVALID_ARG, CdbError, _check, _ptr, cdb_kv, cdb_model_desc, cdb_workspace_init, lib as _lib
-from .tree import _held, _need, _stream, _tensor
+from .tree import _held, _here, _need, _stream, _tensor
 
 EXPORTED = ("cdb_chunk_workspace_bytes", "cdb_chunk_qkv", "cdb_chunk_attention")
 
@@ -56,9 +56,10 @@ def cdb_chunk_workspace_bytes(desc: cdb_model_desc, max_rows: int, max_chunks: i
     return lib().cdb_chunk_workspace_bytes(C.byref(desc), max_rows, max_chunks)
 
 
-def _rows(fn, t, dtype, least) -> int:
-    """The address of a contiguous device tensor of this type (None: fp32 or bf16) with at least so many values."""
-    if not ((t.dtype is dtype if dtype else t.dtype in _TYPES) and t.is_cuda and t.numel() >= least and t.is_contiguous()):
+def _rows(fn, t, dtype, least, here) -> int:
+    """The address of a contiguous tensor of device `here`, of this type (None: fp32 or bf16) with at least so many values."""
+    if not ((t.dtype is dtype if dtype else t.dtype in _TYPES) and t.is_cuda and t.get_device() == here and
+            t.numel() >= least and t.is_contiguous()):
         raise CdbError(fn, CDB_ERR_INVALID_ARG)
     return t.data_ptr()
 
@@ -67,10 +68,10 @@ def cdb_chunk_qkv(desc: cdb_model_desc, kv: cdb_kv, chunks: cdb_chunks, stage: i
                   stream=None):
     """q_out: device fp32 or bf16 [n_rows][d]."""
     fn, n, d = "cdb_chunk_qkv", chunks.n_rows, desc.d
-    rows, heads, head_dim = getattr(qkv, "shape", (n, desc.n_heads, desc.head_dim))  # structs made by hand are taken as they are
-    if rows < n or heads != desc.n_heads or head_dim != desc.head_dim:
+    shape = getattr(qkv, "shape", None)  # structs made by hand are taken as they are
+    if shape is not None and (shape[0] < n or shape[1] != desc.n_heads or shape[2] != desc.head_dim):
         raise CdbError(fn, CDB_ERR_INVALID_ARG)
-    to = _rows(fn, q_out, None, n * d)
+    to = _rows(fn, q_out, None, n * d, _here(fn, ws, chunks, qkv))
     _check(fn, lib().cdb_chunk_qkv(C.byref(desc), C.byref(kv), C.byref(chunks), stage, layer, C.byref(qkv), to,
                                    _TYPES[q_out.dtype], ws.data_ptr(), ws.numel(), _stream(fn, stream, ws)))
 
@@ -80,8 +81,9 @@ def cdb_chunk_attention(desc: cdb_model_desc, kv: cdb_kv, chunks: cdb_chunks, st
     """q: device fp32 or bf16 [n_rows][d]; out: device bf16 [n_rows][d], or, in CDB_ORDER_FRAGMENTS, of n_rows rounded up to
     32 rows."""
     fn, n, d = "cdb_chunk_attention", chunks.n_rows, desc.d
-    at = _rows(fn, q, None, n * d)
-    to = _rows(fn, out, torch.bfloat16, (n if order == CDB_ORDER_ROWS else (n + 31) // 32 * 32) * d)
+    here = _here(fn, ws, chunks)
+    at = _rows(fn, q, None, n * d, here)
+    to = _rows(fn, out, torch.bfloat16, (n if order == CDB_ORDER_ROWS else (n + 31) // 32 * 32) * d, here)
     _check(fn, lib().cdb_chunk_attention(C.byref(desc), C.byref(kv), C.byref(chunks), stage, layer, at, _TYPES[q.dtype], to,
                                          order, ws.data_ptr(), ws.numel(), _stream(fn, stream, ws)))
 

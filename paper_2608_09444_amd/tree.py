@@ -131,6 +131,15 @@ def _trees_fit(fn, drafts, holder):
     _need(fn, getattr(holder, "nodes", drafts.max_nodes) == drafts.max_nodes)
 
 
+def _here(fn, ws, *held) -> int:
+    """The workspace's device, which tensors that structs hold are of too (a struct made by hand tells none)."""
+    here = ws.get_device()
+    for c in held:
+        if getattr(c, "device", here) != here:
+            raise CdbError(fn, CDB_ERR_INVALID_ARG)
+    return here
+
+
 def _rows_fit(fn, rows, tree):
     _need(fn, getattr(tree, "n_rows", rows.n_rows) >= rows.n_rows)
 
@@ -194,6 +203,8 @@ def cdb_tree_sample(desc: cdb_model_desc, drafts: cdb_drafts, row0, first_ids, s
     Sampling's (a cdb_sampling made by hand does not know them)."""
     _trees_fit("cdb_tree_sample", drafts, out)
     _trees_fit("cdb_tree_sample", drafts, sampling)
+    here = _here("cdb_tree_sample", ws, drafts, sampling, out)
+    _need("cdb_tree_sample", row0.get_device() == here and first_ids.get_device() == here)
     _need("cdb_tree_sample", getattr(sampling, "vocab", desc.vocab) == desc.vocab)
     rows = getattr(sampling, "n_rows", n_rows)
     n = rows if n_rows is None else n_rows
@@ -213,7 +224,11 @@ def cdb_tree_commit(desc: cdb_model_desc, kv: cdb_kv, drafts: cdb_drafts, accept
 # ---------------------------------------------------------------- device-memory holders (torch)
 
 def _held(c, *tensors, **sizes):
-    """The struct with its tensors, which live as long as it does, and their sizes, which the calls check."""
+    """The struct with its tensors, which live as long as it does and are of one device, and their sizes; the calls check both."""
+    devices = {t.get_device() for t in tensors if t is not None}
+    _need(type(c).__name__, len(devices) <= 1)
+    if devices:
+        c.device = devices.pop()
     c.keep = tensors
     for k, v in sizes.items():
         setattr(c, k, v)

@@ -18,6 +18,9 @@ class OnDevice:
     def __init__(self, dtype, n, index=0):
         self.dtype, self.n, self.is_cuda, self.device = dtype, n, True, types.SimpleNamespace(index=index)
 
+    def get_device(self):
+        return self.device.index
+
     def numel(self):
         return self.n
 
