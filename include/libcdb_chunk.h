@@ -107,9 +107,10 @@ cdb_status cdb_chunk_qkv(const cdb_model_desc* desc, const cdb_kv* kv, const cdb
  * With CDB_BF16 queries the weights are rounded to bf16 for the product with V; with
  * CDB_F32 both are taken in two bf16 parts (about 16 bits).  Sums and statistics are in 32
  * bits.
- * What a row may not see (NaN included) does not reach it.  K and V that rows see are
- * finite, and so are their scores and sums in 32 bits; where they are not, the rows that
- * see them get no number or an infinity, and no other row changes.  An unmapped page is
+ * What a row may not see (NaN included) does not reach it.  q and the K and V that rows see
+ * are finite, and so are their scores and sums in 32 bits; where they are not, the rows that
+ * see them get no number or an infinity, and no other row changes.  Only a score of -inf
+ * may also count as that of a key that is not there.  An unmapped page is
  * left out (CDB_DEV_UNMAPPED_PAGE); a row that sees nothing gets zeros.  The stage's pool has
  * at least one page, however few are mapped.
  * A chunk's result does not depend on the other chunks; n_rows, n_chunks and the table's

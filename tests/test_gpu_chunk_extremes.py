@@ -135,3 +135,40 @@ def test_a_first_key_that_is_no_number(dtype, n):
         got, _ = c.device().attend(dtype)
         assert c.code() == 0
         assert torch.isnan(got).all()
+
+
+@pytest.mark.parametrize("chunks", [_ragged((40, 30)), _ragged((13, 700)), _ragged((300, 900))], ids=str)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_infinite_keys(dtype, chunks):
+    """A key with an infinite value: where it makes a score of +inf or NaN the row is no number; where it makes one of -inf
+    the row is no number either, or what it is without the key.  Rows that do not see it keep their bits."""
+    _say(f"infinite keys {dtype} {chunks}")
+    (n, p, s, loop), = chunks
+    for H, hd in ((4, 64), (3, 96), (2, 128)):
+        for value in (math.inf, -math.inf):
+            for t in (3, p + 7):
+                c = Case(H, hd, chunks, seed=47)
+                clean, q = c.device().attend(dtype)
+                at = c.table[s, c.plane(loop), t // PAGE], t % PAGE
+                K, V = c.pool[1, at[0], 0, :, at[1]], c.pool[1, at[0], 1, :, at[1]]
+                K[:, 5] = value
+                got, _ = c.device().attend(dtype)
+                assert c.code() == 0
+                first = max(0, t - p)
+                assert torch.equal(got[:first], clean[:first])
+                # without the key, and the tolerance that the other tests take
+                (x, there), (v, _) = c.cache(0, 0), c.cache(0, 1)
+                sc = q.double().view(n, H, hd).transpose(0, 1) @ torch.nan_to_num(x, 0, 0, 0).transpose(1, 2) / math.sqrt(hd)
+                hide = torch.arange(p + n)[None, :] > torch.arange(p, p + n)[:, None]
+                hide = hide | (torch.arange(p + n) == t)[None, :]
+                w = torch.softmax(sc.masked_fill(hide, -math.inf), -1)
+                want, A = w @ v, w @ v.abs()
+                S = q.double().abs().view(n, H, hd).transpose(0, 1) @ torch.nan_to_num(x, 0, 0, 0).abs().transpose(1, 2)
+                S = (S / math.sqrt(hd)).masked_fill(hide, 0).amax(-1, keepdim=True)
+                keys = (~hide).sum(-1)[None, :, None].double()
+                rounded = 2 ** -16 + S * 2 ** -15 if dtype == torch.float32 else 2 ** -8 + S * 2 ** -16
+                tol = want.abs() * 2 ** -8 + A * (rounded + 2 ** -19 + keys * 2 ** -23)
+                near = ((got.view(n, H, hd).double() - want.transpose(0, 1)).abs() <= tol.transpose(0, 1)).all(-1)
+                none = ~torch.isfinite(got.view(n, H, hd)).any(-1)
+                minus = q.view(n, H, hd)[:, :, 5].float() * value == -math.inf
+                assert (none | (near & minus))[first:].all(), (H, hd, value, t)
