@@ -196,7 +196,7 @@ cdb_status cdb_tree_accept(const cdb_drafts* drafts, const int32_t* row0, const 
                            hipStream_t stream);
 
 /* Device error code beside those above: logits that are no distribution (a NaN, an infinity
- * that is not -inf, or nothing else than -inf), or a temperature that is not above 0. */
+ * that is not -inf, or nothing else than -inf), or a temperature that is not above 0 and finite. */
 enum { CDB_DEV_BAD_VALUE = 5 };
 
 #define CDB_SAMPLE_MAX_VOCAB (1 << 20)
@@ -209,7 +209,7 @@ enum { CDB_DEV_BAD_VALUE = 5 };
  *                  token that it guessed (probability 1)
  *   *_stride       in values, at least the model's vocab, a multiple of 4; the logits'
  *                  addresses are multiples of 16
- *   temperature, draft_temperature   fp32 [n_trees], above 0: the probabilities are
+ *   temperature, draft_temperature   fp32 [n_trees], above 0 and finite: the probabilities are
  *                  softmax(logits / temperature); NULL: 1
  *   u_node         fp32 [n_trees][max_nodes] random numbers, even in [0, 1), one per node
  *   u_next         fp32 [n_trees] one per tree, for the token that follows
