@@ -17,11 +17,11 @@
 // of the ones before) do not depend on one another and stand interleaved in one block: a
 // wave's exponentials run under its own products.  One barrier per 64 keys.
 //
-// Measured (bf16 q; us, with the join of segments): 4 chunks of 2048 rows behind 4096
-// positions, 16 x 128 heads: 346-365, 940-990 TFLOP/s (a large library product reaches 1220
+// Measured (bf16 q; us, with the join of segments; ranges over inputs and machines): 4 chunks of 2048 rows behind
+// 4096 positions, 16 x 128 heads: 346-372, 925-993 TFLOP/s (a large library product reaches 1220-1230
 // here; the instructions of a half alone take 690 cycles, of which the products 512); 62 single rows
-// and 2 chunks of 700-1000 behind 2048-4100: 302-306, 5.6 TB/s of K and V; 9 chunks of
-// 33-333 behind up to 2047, 55 x 96 heads: 92-98, 510-540 TFLOP/s; 13 rows behind 700: 13-13.5,
+// and 2 chunks of 700-1000 behind 2048-4100: 301-306, 5.6 TB/s of K and V; 9 chunks of
+// 33-333 behind up to 2047, 55 x 96 heads: 89-102, 480-555 TFLOP/s; 13 rows behind 700: 12.6-13.6,
 // latency; fp32 q, 512 rows behind 512: 29-34.
 #include <algorithm>
 #include <type_traits>
@@ -40,10 +40,13 @@ constexpr int kStep = 64;       // keys that a workgroup stages at a time, a pag
 // chunks of 700-1000 rows behind 2048-4100 89.4 / 71.9 / 75.4, 9 chunks of 33-333, 55 x 96 heads
 // 97 / 97 / 114, 2 of 1024 behind 2048, 55 x 96 heads 153 / 149 / 182.  Segments of kFill positions at least: of 512
 // the first two take 18.8 and 39.6.
-// Longer segments than kLong positions are cut whatever the launch's size, so that one long context does not
+// Longer segments than kLong positions are cut also where the launch is large, so that one long context does not
 // outlast the others; at 1536 the records cost long chunks more than that gives (62 rows and 2 chunks 347 against
 // 305, the last case above 187 against 149).  A chunk of kFewRows rows or fewer, one wave's, writes little of
 // them: 64 single rows behind 3000-4000 take 332 with kLongFew, 360 without.
+// All as far as there are records, which every row of a call has as many of: kChunkRecordRows / n_rows, so 2 up to 2048 rows and
+// none above, where a workgroup takes a head's whole context: 2048 rows take 53, one more behind 32768 makes it 537, and
+// alone that one takes 48.
 constexpr int kWant = 256, kFill = 64;
 constexpr int kLong = 8192, kLongFew = 1536, kFewRows = 32;
 
@@ -198,15 +201,17 @@ __device__ __forceinline__ bf16x8 scaled(bf16x8 p, float f) {
 }
 
 // PER_CU: workgroups that a compute unit can hold.  Two leave a wave 256 registers, 17 too few for heads of 128 with q in two
-// parts; one leaves it all it needs.  fp32 q, one against two (us; 16 heads): 2048 rows 74 / 91, 1024 behind 4096 96 / 114, 2
-// of 2048 behind 2048 214 / 234, 1024 rows 37 / 38, but 512 behind 512 35 / 34, 12 chunks of 100-300 94 / 84, 65 single
-// rows 363 / 340, where loads and starts are to be covered.  So long chunks take one (kLongChunk rows each on average).
+// parts; one leaves it all it needs.  fp32 q, one against two (us; 16 heads): 2048 rows 72 / 90, 1024 behind 4096 93 / 114, 2
+// of 2048 behind 2048 208 / 227, 1024 rows 36 / 37, but 512 behind 512 34.6 / 33.8, 12 chunks of 100-300 93 / 84, 65 single
+// rows 359 / 340, where loads and starts are to be covered.  So long chunks take one (kLongChunk rows each on average).
 constexpr int kLongChunk = 1024;
 template <int HD, bool SPLIT, int PER_CU>
 __global__ __launch_bounds__(256, PER_CU) void k_chunk_attn(ChunkAttnArgs a) {
     constexpr int NT = HD / 16, NB = HD / 32, NL = HD / 32, CPK = HD / 8;
-    constexpr int KP = HD + 8;                   // K row pitch: consecutive keys 4 banks apart (mod 64)
-    constexpr int VP = HD == 96 ? HD : HD + 32;  // V row pitch: consecutive keys 16 banks apart (mod 64)
+    // Row pitches, and how many banks apart (mod 64) consecutive keys are in heads of 64, 96 and 128.  Conflicts, of the
+    // cycles that LDS is read or written in: none, 5.7% (9 ragged chunks), none.
+    constexpr int KP = HD + 8;                   // K: 36, 52, 4
+    constexpr int VP = HD == 96 ? HD : HD + 32;  // V: 48, 48, 16
     __shared__ __align__(16) uint16_t sk[2][kStep * KP];
     __shared__ __align__(16) uint16_t sv[2][kStep * VP];
     __shared__ __align__(16) int s_there[2][4];  // by page of a step: whether it is mapped
@@ -611,7 +616,7 @@ __global__ __launch_bounds__(256, PER_CU) void k_chunk_attn(ChunkAttnArgs a) {
 }
 
 // Segments of a row joined, in order: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  Workgroup = row; its threads
-// take eight values of a head each.  A launch of its own, 4.7-5.5 us for small calls of which 2 are its launch; a
+// take eight values of a head each.  A launch of its own, 4.2-5.5 us for small calls of which 2 are its launch; a
 // join by the last workgroup of each (tile, head) was slower (13 rows behind 700: 14.3 against 13.1).
 constexpr int kBatch = 8;  // records on their way at a time
 template <int HD>

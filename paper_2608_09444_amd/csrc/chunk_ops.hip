@@ -5,9 +5,9 @@
 //
 // for a = x'[j], b = x'[j + hd / 2], t = position * base^(-2 j / hd).
 // Bound: every value is read and written once, and for few rows the chain row -> chunk ->
-// page id -> write.  Measured: 8 rows 4.2 us, of which 1.7 are the launch's own; 7 chunks of 3-201 rows, fp32,
-// 55 x 96 heads 17 us, 4.8 TB/s; 16 chunks of 384-512, bf16, 16 x 128 heads 30.6-32 us, 5.6 TB/s
-// (a large copy: 5.1).
+// page id -> write.  Measured: 8 rows 4.2-4.3 us, of which 1.7 are the launch's own; 7 chunks of 3-201 rows, fp32,
+// 55 x 96 heads 17.4 us, 4.7 TB/s; 16 chunks of 384-512, bf16, 16 x 128 heads 31.2-32.2 us, 5.5 TB/s
+// (a large copy: 5.1); 13 rows of 65536, the others nobody's, 23-25 us.
 #include <cmath>
 
 #include "cdb_internal.h"
@@ -50,7 +50,7 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
 // row0 tell by scalar loads whether any has the row; then its values are asked for, so that they come
 // while its chunk, its page and its angles are found.  Two heads to a group of lanes: the angles
 // (in 64 bits: a position of 10^5 keeps 2^-24 of a turn) and the search are paid once for 64 heads of 128, and enough
-// workgroups are left.  1, 2, 4 heads: 8 rows 7.3, 6.8, 7.2 us; 7 ragged chunks 18.7, 17.1, 17.5; 16 prompts 33.0, 31.6, 36.4.
+// workgroups are left.  1, 2, 4 heads (graphs): 8 rows 4.0, 4.3, 4.5 us; 7 ragged chunks 18.6, 17.2, 17.7; 16 prompts 31.4, 31.1, 35.5.
 constexpr int kTasks = 2;
 
 template <int HD, typename IN, typename OUT>

@@ -12,7 +12,7 @@
 // as a row has pieces for the first ones.  Nothing of the probabilities is stored, 2^x is cheaper
 // than reading it back.
 // Measured (statistics + walk, us): 64 trees of 4, 49152 tokens 26 + 25; 4 trees of 32-64, 65536 tokens
-// 25 + 2 x 22; 20 trees of 5-9, a sure drafter 9 + 14.5; one tree of 13 4.8 + 2 x 7.
+// 25 + 2 x 21-22; 20 trees of 5-9, a sure drafter 9-9.5 + 14.5; one tree of 13 4.8 + 2 x 7.2-7.4.
 #include <algorithm>
 
 #include "cdb_internal.h"
