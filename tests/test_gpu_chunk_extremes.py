@@ -12,8 +12,6 @@ import math
 import pytest
 import torch
 
-import paper_2608_09444_amd as cdb
-from paper_2608_09444_amd import chunk
 from test_gpu_chunk import PAGE, Case, _ragged, _say
 
 pytestmark = pytest.mark.gpu
